@@ -550,6 +550,109 @@ int ds_tune_tasks(const ds_task *tasks, int n_tasks, int total_trials, const ds_
 int droplet_tune(int op, const int64_t *shape, const ds_sched *start, int budget, ds_sched *best,
                  double *best_ms);
 
+/* ---- 8-bit floating point -------------------------------------------------- */
+
+/*
+ * Matrices of 8-bit floating-point values with one scale for each block of 128
+ * along a row: the operands that the chip's matrix cores multiply fastest, and a
+ * quarter to a half of the memory of what they stand for.  The value of element
+ * (r, c) is data[r * ld + c] * scale[(r / block_rows) * scale_ld + c / 128].
+ */
+enum {
+    DS_TYPE_F32 = 0,
+    DS_TYPE_F16 = 1,
+    DS_TYPE_BF16 = 2
+};
+
+enum {
+    DS_Q8_E4M3 = 0,          /* OCP e4m3: largest 448, no infinity */
+    DS_Q8_E5M2 = 1           /* OCP e5m2: largest 57344 */
+};
+
+enum {
+    DS_SCALE_POW2 = 0,       /* one byte b: 2^(b - 127), 255 is NaN (OCP e8m0) */
+    DS_SCALE_F32 = 1
+};
+
+#define DS_Q8_BLOCK 128
+
+/* An 8-bit matrix in device memory (a plain value; the buffers are the caller's).
+ * data: 16-byte aligned, ld >= cols a multiple of 16, below 2^24; bytes past cols
+ * in a row are never used.  scale: ceil(rows / block_rows) rows of ceil(cols / 128)
+ * entries, scale_ld >= that; F32 scales 4-byte aligned.  block_rows: 1, or 128 for
+ * scales of 128x128 squares (weights).  rows, cols: 0 to 2^31 - 1. */
+typedef struct {
+    void *data;
+    void *scale;
+    int64_t rows, cols, ld, scale_ld;
+    int32_t format;          /* DS_Q8_* */
+    int32_t scale_type;      /* DS_SCALE_* */
+    int32_t block_rows;
+    int32_t reserved;        /* 0 */
+} ds_q8;
+
+/*
+ * ds_q8_quantize -- x [rows, cols] (type DS_TYPE_*, rows ldx elements apart) in 8
+ * bits: in *row (rows x cols) and, in blocks along x's columns, transposed in
+ * *col (cols x rows); either may be null, and one read of x serves both.
+ * Per block, with m = max |x| over its finite values and max = 448 (e4m3) or 57344
+ * (e5m2): scale = the smallest 2^e with m <= max * 2^e (POW2) or m / max in fp32
+ * (F32), not below 2^-126; q = x * (1 / scale) in fp32, rounded to nearest even.
+ * NaN gives NaN, an infinity NaN in e4m3 and infinity in e5m2; other values of
+ * its block keep their precision.  Writes the scales of every block and no byte
+ * past a row's end.  x needs its type's alignment only (16-byte rows are faster).
+ * Asynchronous on stream; allocates nothing.  Errors: DS_EINVAL, DS_EHIP.
+ */
+int ds_q8_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t ldx,
+                   const ds_q8 *row, const ds_q8 *col, hipStream_t stream);
+
+/*
+ * ds_q8_matmul -- C [M, N] = A [M, K] * B [N, K]^T: sum over k of the values' products.
+ * The forward product of a layer is (X, W), its input's gradient (dY, W^T)
+ * and its weight's gradient (dY^T, X^T), the transposes as ds_q8_quantize writes
+ * them.  c: type DS_TYPE_*, rows ldc elements apart, overwritten; aligned to its
+ * type (16-byte rows are faster).  a and b have the same scale_type; formats and
+ * block_rows are free.
+ * Sums are held in fp32.  A 16-bit C of more than 16 rows comes from the 8-bit
+ * matrix instructions, which align each eight products to their largest and keep
+ * about 14 bits of them: 1e-5 to 1e-4 of the result for normal and for heavy-tailed
+ * values, against 2^-9 and 2^-12 of the rounding to bf16 and fp16.  An fp32 C, or
+ * one of up to 16 rows, comes from bf16 matrix instructions on the same values, whose
+ * sums are exact to fp32.  The product of two scales has to be an fp32 number.
+ * Few output tiles under a long reduction split it over workgroups and join the
+ * partial sums in order in a workspace as kernel_run keeps (and under the same rule
+ * for captures): two calls give the same bits.  Asynchronous on stream.
+ * Errors: DS_EINVAL (shapes, strides, types), DS_EHIP, DS_ENOMEM, DS_EUNSUPPORTED.
+ */
+int ds_q8_matmul(const ds_q8 *a, const ds_q8 *b, void *c, int type, int64_t ldc,
+                 hipStream_t stream);
+
+/*
+ * ds_swiglu8 -- the gated unit of a feed-forward layer, in 8 bits: of gu [rows, up +
+ * hidden] (gate in columns 0 .. hidden - 1, the other factor from column up, a multiple
+ * of 128 and at least hidden; the columns between are not read), h = silu(gate) *
+ * gu[up:] in *h (rows x hidden), silu(g) = g / (1 + exp(-g)), and, unless saved is
+ * null, gu itself in *saved (rows x (up + hidden), zeros in the columns between): the
+ * checkpoint that ds_swiglu8_grad reads.  Both as ds_q8_quantize would write them, from
+ * fp32 values.  block_rows 1.  Asynchronous; allocates nothing.
+ * Errors: DS_EINVAL, DS_EHIP.
+ */
+int ds_swiglu8(const void *gu, int type, int64_t rows, int64_t hidden, int64_t up, int64_t ldg,
+               const ds_q8 *h, const ds_q8 *saved, hipStream_t stream);
+
+/*
+ * ds_swiglu8_grad -- the backward pass of ds_swiglu8 from the checkpoint: with g and
+ * u the values of *saved and s = 1 / (1 + exp(-g)), the gradients dh * u * s * (1 + g * (1 -
+ * s)) of the gate and dh * g * s of the other factor, laid out as gu, in *dgu (rows x (up
+ * + hidden)) and transposed in *dgu_t; and silu(g) * u transposed in *h_t (hidden x rows),
+ * with which the next layer's weight gradient is taken.  Each output may be null.
+ * dh [rows, hidden]: type DS_TYPE_*, rows ldh elements apart.  block_rows 1 throughout.
+ * Asynchronous; allocates nothing.  Errors: DS_EINVAL, DS_EHIP.
+ */
+int ds_swiglu8_grad(const ds_q8 *saved, const void *dh, int type, int64_t hidden, int64_t up,
+                    int64_t ldh, const ds_q8 *dgu, const ds_q8 *dgu_t, const ds_q8 *h_t,
+                    hipStream_t stream);
+
 /* ---- misc ------------------------------------------------------------------ */
 
 const char *ds_last_error(void);

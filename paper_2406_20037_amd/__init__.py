@@ -5,8 +5,9 @@ exploration sampler and Droplet Search coordinate descent, behind the C ABI
 of ``include/droplet.h``.  ``_lib`` is the Python binding of that ABI; it is
 loaded on first use of any name below, and raises if the library is missing.
 """
-_EXPORTS = ["DS_OP_CONV2D_NCHW", "DS_OP_MATMUL_RM", "Space", "ansor_sample", "droplet_tune",
-            "droplet_tune_ex", "ds_empty_kernel_floor", "ds_measure", "ds_tune", "kernel_run",
+_EXPORTS = ["DS_OP_CONV2D_NCHW", "DS_OP_MATMUL_RM", "Q8", "Space", "ansor_sample", "droplet_tune",
+            "droplet_tune_ex", "ds_empty_kernel_floor", "ds_measure", "ds_q8_matmul",
+            "ds_q8_quantize", "ds_swiglu8", "ds_swiglu8_grad", "ds_tune", "kernel_run",
             "kernel_run_reference", "make_io", "measure_cfg", "tune_cfg"]
 
 __all__ = _EXPORTS + ["_lib"]

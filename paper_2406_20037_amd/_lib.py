@@ -46,6 +46,19 @@ DS_MAX_REPEATS = 64
 DS_NOALLOC_MAX_FLOATS = 8388608   # kernel_run_noalloc: split partials capacity
 
 
+DS_TYPE_F32, DS_TYPE_F16, DS_TYPE_BF16 = 0, 1, 2
+DS_Q8_E4M3, DS_Q8_E5M2 = 0, 1
+DS_SCALE_POW2, DS_SCALE_F32 = 0, 1
+DS_Q8_BLOCK = 128
+
+
+class ds_q8(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scale", C.c_void_p), ("rows", C.c_int64),
+                ("cols", C.c_int64), ("ld", C.c_int64), ("scale_ld", C.c_int64),
+                ("format", C.c_int32), ("scale_type", C.c_int32), ("block_rows", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
 class ds_sched(C.Structure):
     _fields_ = [("op", C.c_int32), ("nknobs", C.c_int32), ("shape", C.c_int64 * 9),
                 ("idx", C.c_int32 * DS_MAX_KNOBS)]
@@ -202,6 +215,14 @@ SIGNATURES = {
                                 C.POINTER(C.c_int), C.POINTER(C.c_double)]),
     "droplet_tune": (C.c_int, [C.c_int, C.POINTER(C.c_int64), C.POINTER(ds_sched), C.c_int,
                                C.POINTER(ds_sched), C.POINTER(C.c_double)]),
+    "ds_q8_quantize": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_void_p,
+                                 C.c_void_p, C.c_void_p]),
+    "ds_q8_matmul": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64,
+                               C.c_void_p]),
+    "ds_swiglu8": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int64,
+                             C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ds_swiglu8_grad": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64,
+                                  C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
     "ds_last_error": (C.c_char_p, []),
     "ds_gen_uniform": (C.c_int, [C.c_uint64, C.c_int64, C.POINTER(C.c_float)]),
     "ds_device_info": (C.c_int, [C.POINTER(C.c_int), C.POINTER(C.c_int), C.c_char_p, C.c_int]),
@@ -623,6 +644,118 @@ def droplet_tune(op, shape, start=None, budget=100):
     check("droplet_tune", lib.droplet_tune(op, sh, C.byref(start) if start is not None else None,
                                            budget, C.byref(best), C.byref(ms)))
     return best, ms.value
+
+
+class Q8:
+    """An 8-bit matrix with a scale for each block of 128 along a row (or, with
+    ``block_rows=128``, each 128x128 square): ``data`` [rows, cols] of
+    ``torch.float8_e4m3fn`` or ``float8_e5m2`` and ``scale`` [ceil(rows / block_rows),
+    ceil(cols / 128)] of ``torch.float8_e8m0fnu`` (powers of two) or ``float32``.
+    Q8(rows, cols) allocates both, uninitialised; Q8.of wraps tensors that exist."""
+
+    def __init__(self, rows, cols, dtype=None, *, scale=None, block_rows=1, device="cuda"):
+        dtype = dtype or _torch.float8_e4m3fn
+        scale = scale or _torch.float8_e8m0fnu
+        ld = max(16, (cols + 15) // 16 * 16)
+        data = _torch.empty(rows, ld, dtype=_torch.uint8, device=device).view(dtype)[:, :cols]
+        shape = -(-rows // block_rows), -(-cols // DS_Q8_BLOCK)
+        self._wrap(data, _torch.empty(shape, dtype=scale, device=device), block_rows)
+
+    @classmethod
+    def of(cls, data, scale, block_rows=1):
+        """The matrix held in data and scale, which it shares: rows of data a multiple
+        of 16 bytes apart, elements of a row side by side."""
+        m = cls.__new__(cls)
+        m._wrap(data, scale, block_rows)
+        return m
+
+    def _wrap(self, data, scale, block_rows):
+        fmt = {_torch.float8_e4m3fn: DS_Q8_E4M3, _torch.float8_e5m2: DS_Q8_E5M2}.get(data.dtype)
+        kind = {_torch.float8_e8m0fnu: DS_SCALE_POW2, _torch.float32: DS_SCALE_F32}.get(scale.dtype)
+        if fmt is None or kind is None:
+            raise TypeError(f"8-bit values of {data.dtype} with scales of {scale.dtype}")
+        if block_rows not in (1, DS_Q8_BLOCK):
+            raise ValueError(f"block_rows is 1 or {DS_Q8_BLOCK}, not {block_rows}")
+        rows, cols, ld = _plain_rows(data)
+        want = (-(-rows // block_rows), -(-cols // DS_Q8_BLOCK))
+        if tuple(scale.shape) != want:
+            raise ValueError(f"scales of shape {tuple(scale.shape)}, not {want}")
+        if scale.device != data.device:
+            raise ValueError(f"values on {data.device}, scales on {scale.device}")
+        sld = _plain_rows(scale)[2]
+        if rows == 1:                   # the stride of a single row says nothing
+            ld = max(ld, (cols + 15) // 16 * 16)
+        self.data, self.scale, self.rows, self.cols = data, scale, rows, cols
+        self.block_rows = block_rows
+        self._c = ds_q8(data.data_ptr(), scale.data_ptr(), rows, cols, ld, sld, fmt, kind, block_rows, 0)
+        self._p = C.addressof(self._c)
+
+    def values(self):
+        """The fp32 values that it stands for (a new tensor)."""
+        s = self.scale.to(_torch.float32)
+        if self.block_rows != 1:
+            s = s.repeat_interleave(self.block_rows, 0)[: self.rows]
+        return self.data.to(_torch.float32) * s.repeat_interleave(DS_Q8_BLOCK, 1)[:, : self.cols]
+
+
+_PLAIN = {} if _torch is None else {_torch.float32: DS_TYPE_F32, _torch.float16: DS_TYPE_F16,
+                                    _torch.bfloat16: DS_TYPE_BF16}
+
+
+def _plain_rows(t):
+    """(rows, cols, elements between rows) of a 2-D tensor whose rows' elements are side by side."""
+    rows, cols = t.shape
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError(f"elements of a row are {one} apart, not side by side")
+    return rows, cols, ld if rows > 1 else max(ld, cols)
+
+
+def _plain(t):
+    if t.dtype not in _PLAIN:
+        raise TypeError(f"fp32, fp16 or bf16, not {t.dtype}")
+    return (t.data_ptr(), _PLAIN[t.dtype], *_plain_rows(t))
+
+
+def _q8_stream(stream):
+    return _torch.cuda.current_stream().cuda_stream if stream is None else stream_handle(stream)
+
+
+def ds_q8_quantize(x, row=None, col=None, stream=None):
+    """x [rows, cols] (fp32, fp16, bf16) in 8 bits: in row (a Q8 of x's shape), transposed in
+    col (a Q8 of cols x rows), or both."""
+    p, t, rows, cols, ld = _plain(x)
+    return check("ds_q8_quantize", lib.ds_q8_quantize(p, t, rows, cols, ld, row and row._p,
+                                                      col and col._p, _q8_stream(stream)))
+
+
+def ds_q8_matmul(a, b, c, stream=None):
+    """c = a b^T of two Q8; c fp32, fp16 or bf16."""
+    p, t, rows, cols, ld = _plain(c)
+    if rows != a.rows or cols != b.rows:
+        raise ValueError(f"c is {rows} x {cols}, not {a.rows} x {b.rows}")
+    return check("ds_q8_matmul", lib.ds_q8_matmul(a._p, b._p, p, t, ld, _q8_stream(stream)))
+
+
+def ds_swiglu8(gu, h, saved=None, stream=None):
+    """silu(gate) * other of gu [rows, up + hidden] in the Q8 h [rows, hidden]; gu itself, the
+    checkpoint of the backward pass, in the Q8 saved unless that is None."""
+    p, t, rows, cols, ld = _plain(gu)
+    if rows != h.rows:
+        raise ValueError(f"gu has {rows} rows, h {h.rows}")
+    return check("ds_swiglu8", lib.ds_swiglu8(p, t, rows, h.cols, cols - h.cols, ld, h._p,
+                                              saved and saved._p, _q8_stream(stream)))
+
+
+def ds_swiglu8_grad(saved, dh, dgu=None, dgu_t=None, h_t=None, stream=None):
+    """The gradient of gu from the checkpoint and dh [rows, hidden], in dgu and transposed in
+    dgu_t, and the unit's output transposed in h_t (each a Q8 or None)."""
+    p, t, rows, cols, ld = _plain(dh)
+    if rows != saved.rows:
+        raise ValueError(f"dh has {rows} rows, saved {saved.rows}")
+    return check("ds_swiglu8_grad",
+                 lib.ds_swiglu8_grad(saved._p, p, t, cols, saved.cols - cols, ld, dgu and dgu._p,
+                                     dgu_t and dgu_t._p, h_t and h_t._p, _q8_stream(stream)))
 
 
 def ds_gen_uniform(seed, n):

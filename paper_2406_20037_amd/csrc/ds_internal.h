@@ -13,6 +13,14 @@ namespace ds {
 // ---- errors ---------------------------------------------------------------
 void set_error(const char *fmt, ...);
 const char *last_error();
+// false, with the error set, unless e is hipSuccess
+bool hip_ok(hipError_t e, const char *what);
+
+// ---- per-device state (harness.hip) -------------------------------------------
+// The workspace of split reductions on `stream`, at least `elems` floats.
+int split_workspace(int64_t elems, hipStream_t stream, float **out);
+// Allows `func` launches with `lds` bytes of dynamic LDS (above 64 KiB).
+int ensure_lds_attr(const void *func, int lds);
 
 // ---- lattice ----------------------------------------------------------------
 constexpr int kLdsLimit = 163840;     // bytes of LDS per workgroup on gfx950

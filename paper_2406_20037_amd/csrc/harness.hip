@@ -39,11 +39,15 @@ int log2_exact(int v) {
     return l;
 }
 
+}  // namespace
+
 bool hip_ok(hipError_t e, const char *what) {
     if (e == hipSuccess) return true;
     set_error("%s: %s", what, hipGetErrorString(e));
     return false;
 }
+
+namespace {
 
 // ---- small kernels ------------------------------------------------------------
 
@@ -218,6 +222,8 @@ int graph_stream(hipStream_t *out) {
     return DS_OK;
 }
 
+}  // namespace
+
 // The split-reduction workspace of `stream` on the current device, grown to at
 // least `elems` floats.  Growing allocates a new buffer (at least twice the
 // old size) and retires the old one after the stream's queued work is done;
@@ -258,6 +264,8 @@ int split_workspace(int64_t elems, hipStream_t stream, float **out) {
     return DS_OK;
 }
 
+namespace {
+
 // This device's address of `scratch`, looked up on the first call on the
 // device (with that device current) and kept.
 int scratch_ptr(float **out) {
@@ -279,6 +287,8 @@ int scratch_ptr(float **out) {
     return DS_OK;
 }
 
+}  // namespace
+
 int ensure_lds_attr(const void *func, int lds) {
     if (lds <= 65536) return DS_OK;
     int dev;
@@ -292,6 +302,8 @@ int ensure_lds_attr(const void *func, int lds) {
     g_lds_attr.insert({dev, func});
     return DS_OK;
 }
+
+namespace {
 
 void fill_conv_args(const Space &sp, const float *x, const float *w, float *y, ConvArgs &a) {
     std::memset(&a, 0, sizeof a);
