@@ -579,7 +579,7 @@ enum {
 /* An 8-bit matrix in device memory (a plain value; the buffers are the caller's).
  * data: 16-byte aligned, ld >= cols a multiple of 16, below 2^24; bytes past cols
  * in a row are never used.  scale: ceil(rows / block_rows) rows of ceil(cols / 128)
- * entries, scale_ld >= that; F32 scales 4-byte aligned.  block_rows: 1, or 128 for
+ * entries, scale_ld >= that, below 2^22; F32 scales 4-byte aligned.  block_rows: 1, or 128 for
  * scales of 128x128 squares (weights).  rows, cols: 0 to 2^31 - 1. */
 typedef struct {
     void *data;

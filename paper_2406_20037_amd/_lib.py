@@ -658,8 +658,10 @@ class Q8:
         scale = scale or _torch.float8_e8m0fnu
         ld = max(16, (cols + 15) // 16 * 16)
         data = _torch.empty(rows, ld, dtype=_torch.uint8, device=device).view(dtype)[:, :cols]
-        shape = -(-rows // block_rows), -(-cols // DS_Q8_BLOCK)
-        self._wrap(data, _torch.empty(shape, dtype=scale, device=device), block_rows)
+        nr, nc = -(-rows // block_rows), -(-cols // DS_Q8_BLOCK)
+        # rows of scales in whole 4-byte words: products copy them so
+        sc = _torch.empty(nr, (nc + 3) // 4 * 4, dtype=scale, device=device)[:, :nc]
+        self._wrap(data, sc, block_rows)
 
     @classmethod
     def of(cls, data, scale, block_rows=1):

@@ -22,8 +22,8 @@ int q8_check(const ds_q8 *m, const char *what) {
         return DS_EINVAL;
     }
     if (m->ld < m->cols || m->ld % 16 != 0 || m->ld >= (1 << 24) ||
-        m->scale_ld < q8_up(m->cols) || m->scale_ld > 0x7fffffff) {
-        set_error("%s: ld %lld of %lld columns (a multiple of 16 below 2^24), scale_ld %lld", what,
+        m->scale_ld < q8_up(m->cols) || m->scale_ld >= (1 << 22)) {
+        set_error("%s: ld %lld of %lld columns (a multiple of 16 below 2^24), scale_ld %lld (below 2^22)", what,
                   (long long)m->ld, (long long)m->cols, (long long)m->scale_ld);
         return DS_EINVAL;
     }

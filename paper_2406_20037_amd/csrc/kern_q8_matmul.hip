@@ -13,12 +13,36 @@ struct Q8MatArgs {
     int64_t ldc;
     int type;
     int M, N, K, nkt;
+    int tiles_m, tiles_n, group;   // tiles of C; workgroups walk `group` rows of tiles at a time
+    int ks, kps;                   // splits of the reduction, steps of 128 in each
+    float *part;                   // ks > 1: ks partial products, M x N each
+    int words;                     // power-of-two scales: words of four are aligned
+    int cvec, pvec;                // four columns of C, of a partial product, in one store
 };
 
 __device__ __forceinline__ void store_c(void *c, int type, int64_t i, float v) {
     if (type == DS_TYPE_F32) static_cast<float *>(c)[i] = v;
     else if (type == DS_TYPE_F16) static_cast<_Float16 *>(c)[i] = _Float16(v);
     else static_cast<__bf16 *>(c)[i] = __bf16(v);
+}
+
+// Four columns from `col` on of the row at `at`, as far as the row goes.
+__device__ __forceinline__ void store4(void *c, int type, int64_t at, int col, int cols, int vec, floatx4 v) {
+    if (vec && col + 4 <= cols) {
+        if (type == DS_TYPE_F32) {
+            *reinterpret_cast<floatx4 *>(static_cast<float *>(c) + at + col) = v;
+        } else if (type == DS_TYPE_F16) {
+            *reinterpret_cast<f16x4 *>(static_cast<_Float16 *>(c) + at + col) =
+                f16x4{_Float16(v[0]), _Float16(v[1]), _Float16(v[2]), _Float16(v[3])};
+        } else {
+            *reinterpret_cast<bf16x4 *>(static_cast<__bf16 *>(c) + at + col) =
+                bf16x4{__bf16(v[0]), __bf16(v[1]), __bf16(v[2]), __bf16(v[3])};
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (col + i < cols) store_c(c, type, at + col + i, v[i]);
+    }
 }
 
 // 32 bytes of a row from k on, 0 from K on.
@@ -81,6 +105,425 @@ __global__ __launch_bounds__(1024) void q8_few(Q8MatArgs a) {
     }
 }
 
+// ---- tiles -----------------------------------------------------------------------
+
+#define DS_GLOBAL(p) ((const __attribute__((address_space(1))) void *)(p))
+#define DS_LOCAL(p) ((__attribute__((address_space(3))) void *)(p))
+
+// Waits for all but the wave's newest N copies and for its LDS accesses, then for the workgroup.
+template <int N>
+__device__ __forceinline__ void stage_barrier() {
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4 << 14));   // vmcnt(N)
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+    __asm__ volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    __asm__ volatile("" ::: "memory");
+}
+
+// A buffer descriptor of n bytes from p on: loads past them give zeros.
+__device__ __forceinline__ intx4 buffer_of(const uint8_t *p, unsigned n) {
+    const uint64_t u = reinterpret_cast<uint64_t>(p);
+    return intx4{int(unsigned(u)), int(unsigned(u >> 32) & 0xffffu), int(n), 0x00020000};
+}
+
+// Copies 16 bytes a lane from d at off to LDS at dst + 16 lane.  The compiler does not see
+// an LDS write here that later reads would have to wait for: stage_barrier's wait and the
+// memory clobbers order the two.
+__device__ __forceinline__ void copy16(intx4 d, unsigned off, unsigned dst) {
+    __asm__ volatile("s_mov_b32 m0, %2\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+                     :: "v"(off), "s"(d), "s"(dst) : "memory", "m0");
+}
+
+// The same for four bytes a lane.
+__device__ __forceinline__ void copy4(intx4 d, unsigned off, unsigned dst) {
+    __asm__ volatile("s_mov_b32 m0, %2\n\tbuffer_load_dword %0, %1, 0 offen lds"
+                     :: "v"(off), "s"(d), "s"(dst) : "memory", "m0");
+}
+
+// How a tile's products are formed.
+enum {
+    MM_POW2 = 0,   // scaled 8-bit instructions, power-of-two scales in the instruction
+    MM_F32 = 1     // 8-bit instructions block by block, each block's sum times fp32 scales
+};
+
+// 32 FM x 32 FN of C a workgroup of four waves, 16 FM x 16 FN a wave.
+template <int FM, int FN, int MODE>
+struct MmShape {
+    static constexpr int BM = 32 * FM, BN = 32 * FN, ROWS = BM + BN;
+    static constexpr int STAGE = ROWS * kQ8Block;          // bytes of one 128-long step
+    // the scales of four steps: a word of exponents or four fp32 numbers a row
+    static constexpr int SCALES = ROWS * (MODE == MM_POW2 ? 4 : 16);
+    static constexpr int LDS = 2 * STAGE + 2 * SCALES;
+};
+
+template <int FM, int FN, int MODE, bool SQ, int FA, int FB>
+__global__ __launch_bounds__(256) void q8_mm(Q8MatArgs a) {
+    using S = MmShape<FM, FN, MODE>;
+    constexpr int BM = S::BM, BN = S::BN, ROWS = S::ROWS, STAGE = S::STAGE, HM = FM / 2, HN = FN / 2;
+    constexpr int LA = BM / 32, LB = BN / 32;              // copies a thread makes of either operand
+    extern __shared__ __align__(16) uint8_t smem[];
+
+    const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, lg = lane >> 4;
+    const int wid = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wid >> 1, wn = wid & 1;
+    // (quotients of scalars come out of the vector unit)
+    const auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    int t = xcd_tile(blockIdx.x, gridDim.x);
+    const int tiles = a.tiles_m * a.tiles_n, z = scalar(t / tiles);
+    t -= z * tiles;
+    const int per = a.group * a.tiles_n, g = scalar(t / per), first = g * a.group;
+    const int gm = min(a.tiles_m - first, a.group), r = t - g * per, rn = scalar(r / gm);
+    const int m0 = (first + r - rn * gm) * BM, n0 = rn * BN;
+    const int kt0 = z * a.kps, kt1 = min(a.nkt, kt0 + a.kps);
+    const int last = a.K % kQ8Block ? a.nkt - 1 : a.nkt;   // the step that reaches past K, if any
+
+    // A wave's copy j brings rows 32 j + 8 wid .. + 7 of the stage: lane l the 16 bytes at slot
+    // l % 8 of row l / 8.  Slot s of row r holds bytes 16 (s ^ (r / 2) % 8) .. + 15 of the step, so that
+    // 16 lanes that read one column of 16 rows use each of the 64 banks once.  Rows past the
+    // matrix are past the descriptor's end and arrive as zeros.
+    const int cr = 8 * wid + (lane >> 3), ck = 16 * ((lane & 7) ^ ((cr >> 1) & 7));
+    const unsigned oa = unsigned(cr) * unsigned(a.a.ld) + ck, ob = unsigned(cr) * unsigned(a.b.ld) + ck;
+    const uint8_t *const pa = a.a.data + int64_t(m0) * a.a.ld, *const pb = a.b.data + int64_t(n0) * a.b.ld;
+    const unsigned na = unsigned(min(BM, a.M - m0) - 1) * unsigned(a.a.ld) + kQ8Block;
+    const unsigned nb = unsigned(min(BN, a.N - n0) - 1) * unsigned(a.b.ld) + kQ8Block;
+    const unsigned lds0 = unsigned(uintptr_t(DS_LOCAL(smem))) + wid * 1024;
+
+    // one of a step's copies, given its operands' descriptors
+    auto copy1 = [&](intx4 da, intx4 db, unsigned st, int j) {
+        if (j < LA) copy16(da, oa + 32 * j * unsigned(a.a.ld), lds0 + st + j * 4096);
+        else copy16(db, ob + 32 * (j - LA) * unsigned(a.b.ld), lds0 + st + j * 4096);
+    };
+    auto desc_a = [&](int kt) { return buffer_of(pa + int64_t(kt) * kQ8Block, na); };
+    auto desc_b = [&](int kt) { return buffer_of(pb + int64_t(kt) * kQ8Block, nb); };
+    // A step's copies in two parts: what the waves' first halves of rows and columns need, and the rest.
+    constexpr int PART = (LA + LB) / 2;
+    auto part_copy = [](int r, int hi) {                   // copy r of a part
+        const int h = r < LA / 2 ? HM / 2 : HN / 2, x = r < LA / 2 ? r : r - LA / 2;
+        return (r < LA / 2 ? 0 : LA) + x / h * 2 * h + x % h + hi * h;
+    };
+    // a whole step; the one that reaches past K gets zeros from there on
+    auto copy_any = [&](int kt, unsigned st) {
+        if (kt < last) {
+            const intx4 da = desc_a(kt), db = desc_b(kt);
+#pragma unroll
+            for (int j = 0; j < 2 * PART; ++j) copy1(da, db, st, part_copy(j % PART, j / PART));
+            return;
+        }
+        const int left = a.K - kt * kQ8Block - ck;         // bytes of this lane's 16 that exist
+#pragma unroll 1
+        for (int j = 0; j < LA + LB; ++j) {
+            const int row = 32 * (j < LA ? j : j - LA) + cr;
+            const uint8_t *p = (j < LA ? pa + int64_t(min(row, a.M - 1 - m0)) * a.a.ld
+                                       : pb + int64_t(min(row, a.N - 1 - n0)) * a.b.ld) +
+                               int64_t(kt) * kQ8Block + ck;
+            intx4 v = {0, 0, 0, 0};
+            if (left >= 16) {
+                v = *reinterpret_cast<const intx4 *>(p);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (i < left) v[i >> 2] |= int(unsigned(p[i]) << (8 * (i & 3)));
+            }
+            *reinterpret_cast<intx4 *>(smem + st + wid * 1024 + j * 4096 + lane * 16) = v;
+        }
+    };
+
+    // Fragment f of an operand: lane l holds bytes 32 (l / 16) .. + 31 of row 16 f + l % 16, in halves.
+    const int slot = 16 * ((2 * lg) ^ (li >> 1));
+    const int fa0 = (16 * FM * wm + li) * kQ8Block + slot, fb0 = (BM + 16 * FN * wn + li) * kQ8Block + slot;
+    auto half = [&](unsigned st, int at, int f, int h) {
+        return *reinterpret_cast<const intx4 *>(smem + st + (h ? at ^ 16 : at) + f * 16 * kQ8Block);
+    };
+    struct Frag {
+        intx4 h[2];
+        __device__ operator intx8() const {
+            return __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    };
+
+    // Scales go through LDS four steps at a time: a word of four exponents a row, or four planes of
+    // fp32 numbers; a wave copies those of 64 rows at once.
+    uint8_t *const sbuf = smem + 2 * STAGE;
+    constexpr int ES = MODE == MM_POW2 ? 1 : 4;            // bytes of a scale
+    auto copy_scales = [&](int kt, int s) {
+        if (kt >= a.nkt) return;
+#pragma unroll
+        for (int i = 0; i < (ROWS / 64 + 3) / 4; ++i) {
+            const int r0 = 64 * (4 * i + wid);             // rows of the stage, all of A or all of B
+            if (r0 >= ROWS) break;
+            const bool isa = r0 < BM;
+            const Q8View &v = isa ? a.a : a.b;
+            const int o0 = isa ? m0 : n0, left = (isa ? a.M : a.N) - o0, row = (isa ? r0 : r0 - BM) + lane;
+            const int s0 = o0 >> v.shift;                  // scale rows from here on
+            const unsigned sld = unsigned(v.sld) * ES;
+            const int64_t at = int64_t(s0) * sld + int64_t(kt) * ES;
+            const unsigned end = unsigned(((o0 + min(isa ? BM : BN, left) - 1) >> v.shift) - s0) * sld +
+                                 (MODE == MM_POW2 ? (unsigned(a.nkt - kt) + 3u) & ~3u : unsigned(a.nkt - kt) * 4u);
+            const uint8_t *const p = static_cast<const uint8_t *>(v.scale) + at;
+            const unsigned off = unsigned(((o0 + row) >> v.shift) - s0) * sld;
+            uint8_t *const dst = sbuf + s * S::SCALES + 4 * r0;
+            if (MODE == MM_POW2 && !a.words) {             // not in whole words: byte by byte
+                int w = 0;
+#pragma unroll 1
+                for (int k = 0; k < 4 && kt + k < a.nkt; ++k)
+                    if (row < left) w |= int(unsigned(p[off + k]) << (8 * k));
+                *reinterpret_cast<int *>(dst + 4 * lane) = w;
+                continue;
+            }
+            const intx4 d = buffer_of(p, end);
+            const unsigned to = unsigned(uintptr_t(DS_LOCAL(dst)));
+#pragma unroll
+            for (int k = 0; k < (MODE == MM_POW2 ? 1 : 4); ++k) copy4(d, off + 4 * k, to + 4 * k * ROWS);
+        }
+    };
+
+    floatx4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0, 0, 0, 0};
+    Frag alo[HM], ahi[HM], b0[HN], b1[HN];
+    // The present step's scales: of A's rows and of B's columns.  MM_POW2: exponents in the low
+    // bytes, xn the words of the step after as read.  SQ: one of B for all columns.
+    constexpr int XN = FM + (MODE == MM_POW2 ? FN : 0);
+    int xs[XN], xn[MODE == MM_POW2 ? XN : 1];
+    floatx4 sb[MODE == MM_POW2 ? 1 : FN];
+    float sq = 0.f, sqn = 0.f;
+    auto scales_of = [&](int u) {
+        return reinterpret_cast<const int *>(sbuf + ((u >> 2) & 1) * S::SCALES) +
+               (MODE == MM_POW2 ? 0 : (u & 3) * ROWS);
+    };
+    auto scale_of_a = [&](const int *sc, int f) { return sc[16 * (FM * wm + f) + li]; };
+    auto word_of = [&](const int *sc, int f) {
+        return f < FM ? scale_of_a(sc, f) : sc[BM + 16 * (FN * wn + f - FM) + li];
+    };
+    auto scale_of_b = [&](const int *sc, int f) {
+        return *reinterpret_cast<const floatx4 *>(sc + BM + 16 * (FN * wn + f) + 4 * lg);
+    };
+
+    // MM_F32: a block's product waits for two more to be issued before it is scaled and added.
+    constexpr int NQ = HM * HN;
+    floatx4 p0 = {0, 0, 0, 0}, p1 = {0, 0, 0, 0}, s0 = {0, 0, 0, 0}, s1 = {0, 0, 0, 0};
+    // A quarter of the wave's tile, fragments i0 .. of A by j0 .. of B; beside(q) issues what goes
+    // between its products q and q + 1.  pi, pj: the block that is waiting (and the one after it).
+    auto quarter = [&](const Frag (&fa)[HM], const Frag (&fb)[HN], int i0, int j0, auto beside, int wi, int wj) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const int i = q / HN, j = q % HN;
+            if constexpr (MODE == MM_POW2) {
+                acc[i0 + i][j0 + j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                    fb[j], fa[i], acc[i0 + i][j0 + j], FB, FA, 0, xs[FM + j0 + j], 0, xs[i0 + i]);
+            } else {
+                const floatx4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                    fb[j], fa[i], floatx4{0, 0, 0, 0}, FB, FA, 0, 0, 0, 0);
+                const int o = q < 2 ? NQ - 2 + q : q - 2;  // place of the block that is due, in its quarter
+                const int oi = (q < 2 ? wi : i0) + o / HN, oj = (q < 2 ? wj : j0) + o % HN;
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                    acc[oi][oj][v] = fmaf(p0[v], SQ ? s0[0] : s0[v], acc[oi][oj][v]);
+                p0 = p1;
+                s0 = s1;
+                p1 = p;
+                const float x = __int_as_float(xs[i0 + i]);
+                if constexpr (SQ) s1[0] = x * sq;
+                else s1 = x * sb[j0 + j];
+            }
+            beside(q);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // step kt, whose first fragments are in alo and b0; COPY: the whole of step kt + 2 is copied
+    auto step = [&]<bool COPY>(std::bool_constant<COPY>, int kt) {
+        const int u = kt - kt0;
+        const unsigned cur = (u & 1) * STAGE, nxt = STAGE - cur;
+        if ((u & 3) == 0) copy_scales(kt + 4, ((u >> 2) & 1) ^ 1);
+        __builtin_amdgcn_sched_barrier(0);
+        // n parts spread over a quarter's first products, at most two after each
+        auto spread = [](int q, int n, auto part) {
+            const int each = 2 * NQ < n ? (n + NQ - 1) / NQ : n > NQ ? 2 : 1;
+#pragma unroll
+            for (int r = q * each; r < (q + 1) * each; ++r)
+                if (r < n) part(r);
+        };
+        // A part is copied a step and a half before it is needed: the two parts copied since may be
+        // on their way (the scales' copies among them only make a wait longer).
+        constexpr int LEFT = COPY ? 2 * PART : 0;
+        intx4 da, db;
+        if constexpr (COPY) {
+            da = desc_a(kt + 2);
+            db = desc_b(kt + 2);
+        }
+        const int *const sc = scales_of(u), *const scn = scales_of(u + 1);
+        const int sh = 8 * (u & 3), shn = 8 * ((u + 1) & 3);
+        // Each half of the fragments and scales is replaced once its last product is issued
+        quarter(alo, b0, 0, 0, [&](int q) {
+            spread(q, 2 * HN, [&](int r) { b1[r >> 1].h[r & 1] = half(cur, fb0, HN + (r >> 1), r & 1); });
+            if constexpr (COPY) spread(q, PART, [&](int r) { copy1(da, db, cur, part_copy(r, 0)); });
+            if constexpr (MODE == MM_POW2) {
+                spread(q, HM, [&](int f) { xs[HM + f] = int(unsigned(xn[HM + f]) >> sh); });
+                spread(q, HN, [&](int f) { xs[FM + HN + f] = int(unsigned(xn[FM + HN + f]) >> sh); });
+            } else {
+                if constexpr (!SQ) spread(q, HN, [&](int f) { sb[HN + f] = scale_of_b(sc, HN + f); });
+                spread(q, HM, [&](int f) { xs[HM + f] = scale_of_a(sc, HM + f); });
+            }
+        }, HM, HN);
+        quarter(alo, b1, 0, HN, [&](int q) {
+            spread(q, 2 * HM, [&](int r) { ahi[r >> 1].h[r & 1] = half(cur, fa0, HM + (r >> 1), r & 1); });
+            if constexpr (MODE == MM_POW2) spread(q, XN, [&](int f) { xn[f] = word_of(scn, f); });
+        }, 0, 0);
+        // Every wave has read the second part of this step, which is copied over now, and the first
+        // part of the next has arrived.
+        stage_barrier<LEFT>();
+        quarter(ahi, b0, HM, 0, [&](int q) {
+            if constexpr (COPY) spread(q, PART, [&](int r) { copy1(da, db, cur, part_copy(r, 1)); });
+            spread(q, 2 * HM, [&](int r) { alo[r >> 1].h[r & 1] = half(nxt, fa0, r >> 1, r & 1); });
+            if constexpr (MODE != MM_POW2) {
+                spread(q, HM, [&](int f) { xs[f] = scale_of_a(scn, f); });
+                if (SQ && q == 0) sqn = __int_as_float(scn[BM + 16 * FN * wn]);
+            }
+        }, 0, HN);
+        quarter(ahi, b1, HM, HN, [&](int q) {
+            spread(q, 2 * HN, [&](int r) { b0[r >> 1].h[r & 1] = half(nxt, fb0, r >> 1, r & 1); });
+            if constexpr (MODE == MM_POW2) {
+                spread(q, HM, [&](int f) { xs[f] = int(unsigned(xn[f]) >> shn); });
+                spread(q, HN, [&](int f) { xs[FM + f] = int(unsigned(xn[FM + f]) >> shn); });
+            } else if constexpr (!SQ) {
+                spread(q, HN, [&](int f) { sb[f] = scale_of_b(scn, f); });
+            }
+        }, HM, 0);
+        if constexpr (SQ) sq = sqn;
+        // likewise the first part of the next step, and the second has arrived
+        stage_barrier<LEFT>();
+    };
+
+    if (kt0 < kt1) {
+        copy_scales(kt0, 0);
+        copy_any(kt0, 0);
+        if (kt0 + 1 < kt1) copy_any(kt0 + 1, STAGE);
+        // (with fewer steps, or one that reaches past K among them, fewer copies are on their way)
+        if (kt0 + 1 < min(kt1, last)) stage_barrier<2 * PART>();
+        else stage_barrier<0>();
+#pragma unroll
+        for (int f = 0; f < HM; ++f)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) alo[f].h[h] = half(0, fa0, f, h);
+#pragma unroll
+        for (int f = 0; f < HN; ++f)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) b0[f].h[h] = half(0, fb0, f, h);
+        const int *const sc = scales_of(0);
+#pragma unroll
+        for (int f = 0; f < XN; ++f) xs[f] = word_of(sc, f);
+        if constexpr (MODE == MM_POW2) {
+#pragma unroll
+            for (int f = 0; f < XN; ++f) xn[f] = xs[f];
+        } else if constexpr (SQ) {
+            sq = __int_as_float(sc[BM + 16 * FN * wn]);
+        } else {
+#pragma unroll
+            for (int f = 0; f < FN; ++f) sb[f] = scale_of_b(sc, f);
+        }
+        int kt = kt0;
+#pragma unroll 1
+        for (; kt + 2 < min(kt1, last); ++kt) step(std::true_type{}, kt);
+#pragma unroll 1
+        for (; kt < kt1; ++kt) {
+            step(std::false_type{}, kt);
+            // the step that reaches past K, half a step later than the others
+            if (kt + 2 < kt1) copy_any(kt + 2, ((kt - kt0) & 1) * STAGE);
+        }
+        // the last step read ahead into a stage that nothing was copied to; its values are unused
+        if constexpr (MODE == MM_F32) {
+            for (int w = 0; w < 2; ++w) {
+                const int o = NQ - 2 + w, i = HM + o / HN, j = HN + o % HN;
+                const floatx4 p = w ? p1 : p0, s = w ? s1 : s0;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[i][j][v] = fmaf(p[v], SQ ? s[0] : s[v], acc[i][j][v]);
+            }
+        }
+    }
+
+    // Lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of each 16 x 16 block.
+    void *const out = a.part ? a.part + int64_t(z) * a.M * a.N : a.c;
+    const int type = a.part ? DS_TYPE_F32 : a.type, vec = a.part ? a.pvec : a.cvec;
+    const int64_t ldc = a.part ? a.N : a.ldc;
+    const int rm = m0 + 16 * FM * wm, cn = n0 + 16 * FN * wn;
+    if (vec && m0 + BM <= a.M && n0 + BN <= a.N) {
+        // whole tiles: straight from the registers, 32 or 64 bytes of a row at once
+        auto whole = [&](auto *c, auto conv) {
+            c += (rm + li) * ldc + cn + 4 * lg;
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    *reinterpret_cast<decltype(conv(acc[0][0])) *>(c + i * 16 * ldc + j * 16) = conv(acc[i][j]);
+        };
+        if (type == DS_TYPE_BF16)
+            whole(static_cast<__bf16 *>(out), [](floatx4 v) {
+                return bf16x4{__bf16(v[0]), __bf16(v[1]), __bf16(v[2]), __bf16(v[3])};
+            });
+        else if (type == DS_TYPE_F16)
+            whole(static_cast<_Float16 *>(out), [](floatx4 v) {
+                return f16x4{_Float16(v[0]), _Float16(v[1]), _Float16(v[2]), _Float16(v[3])};
+            });
+        else
+            whole(static_cast<float *>(out), [](floatx4 v) { return v; });
+        return;
+    }
+    // Edges and rows that are not 16-byte aligned: through the wave's part of LDS (free since the last
+    // barrier), a lane a column.  One copy of the loop: straight-line it would outgrow the
+    // instruction cache.
+    constexpr int ROW = 16 * FN + 4;                       // floats; 16 bytes aside from bank to bank
+    static_assert(4 * 16 * ROW * 4 <= S::LDS, "a row of blocks of every wave");
+    float *const own = reinterpret_cast<float *>(smem) + wid * 16 * ROW;
+#pragma unroll 1
+    for (int i = 0; i < FM; ++i) {
+#pragma unroll
+        for (int k = 0; k < FM; ++k)
+            if (i == k)
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    *reinterpret_cast<floatx4 *>(own + li * ROW + 16 * j + 4 * lg) = acc[k][j];
+        __builtin_amdgcn_wave_barrier();
+        const int rows = min(16, a.M - rm - 16 * i), cols = min(16 * FN, a.N - cn);
+        auto edge = [&](auto *c) {
+            using T = std::remove_pointer_t<decltype(c)>;
+            c += (rm + 16 * i) * ldc + cn;
+#pragma unroll 4
+            for (int r = 0; r < rows; ++r)
+#pragma unroll
+                for (int x = 0; x < FN / 4; ++x)
+                    if (64 * x + lane < cols) c[r * ldc + 64 * x + lane] = T(own[r * ROW + 64 * x + lane]);
+        };
+        if (type == DS_TYPE_BF16) edge(static_cast<__bf16 *>(out));
+        else if (type == DS_TYPE_F16) edge(static_cast<_Float16 *>(out));
+        else edge(static_cast<float *>(out));
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// C from the partial sums of ks splits, in their order.
+__global__ __launch_bounds__(256) void q8_join(Q8MatArgs a) {
+    const int per = (a.N + 3) / 4;
+    const int64_t total = int64_t(a.M) * per, mn = int64_t(a.M) * a.N;
+    for (int64_t e = int64_t(blockIdx.x) * 256 + threadIdx.x; e < total; e += int64_t(gridDim.x) * 256) {
+        const int row = int(e / per), col = 4 * int(e - int64_t(row) * per);
+        const float *p = a.part + int64_t(row) * a.N + col;
+        floatx4 v = {0, 0, 0, 0};
+        for (int z = 0; z < a.ks; ++z, p += mn) {
+            if (a.pvec) {
+                v += *reinterpret_cast<const floatx4 *>(p);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (col + i < a.N) v[i] += p[i];
+            }
+        }
+        store4(a.c, a.type, int64_t(row) * a.ldc, col, a.N, a.cvec, v);
+    }
+}
+
 template <int V>
 using Fmt = std::integral_constant<int, V>;
 
@@ -90,6 +533,39 @@ int by_formats(int fa, int fb, Fn fn) {
     if (fa == DS_Q8_E4M3) fb == DS_Q8_E4M3 ? fn(Fmt<0>{}, Fmt<0>{}) : fn(Fmt<0>{}, Fmt<1>{});
     else fb == DS_Q8_E4M3 ? fn(Fmt<1>{}, Fmt<0>{}) : fn(Fmt<1>{}, Fmt<1>{});
     return hip_ok(hipGetLastError(), "8-bit matmul launch") ? DS_OK : DS_EHIP;
+}
+
+template <int FM, int FN, int MODE, bool SQ>
+int mm_launch(Q8MatArgs &g, hipStream_t stream) {
+    using S = MmShape<FM, FN, MODE>;
+    g.tiles_m = (g.M + S::BM - 1) / S::BM;
+    g.tiles_n = (g.N + S::BN - 1) / S::BN;
+    g.group = 8;
+    const int64_t grid = int64_t(g.tiles_m) * g.tiles_n * g.ks;
+    if (grid > kGridLimit) {
+        set_error("ds_q8_matmul: %lld workgroups", (long long)grid);
+        return DS_EUNSUPPORTED;
+    }
+    int rc = DS_OK;
+    const int done = by_formats(g.a.fmt, g.b.fmt, [&](auto fa, auto fb) {
+        auto *k = &q8_mm<FM, FN, MODE, SQ, fa.value, fb.value>;
+        rc = ensure_lds_attr(reinterpret_cast<const void *>(k), S::LDS);
+        if (rc == DS_OK) k<<<unsigned(grid), 256, S::LDS, stream>>>(g);
+    });
+    if (rc != DS_OK || done != DS_OK) return rc != DS_OK ? rc : done;
+    if (g.ks == 1) return DS_OK;
+    const int64_t quads = int64_t(g.M) * ((g.N + 3) / 4);
+    q8_join<<<unsigned(std::min<int64_t>((quads + 255) / 256, 4096)), 256, 0, stream>>>(g);
+    return hip_ok(hipGetLastError(), "8-bit matmul join") ? DS_OK : DS_EHIP;
+}
+
+int mm_tiles(Q8MatArgs &g, hipStream_t stream) {
+    g.ks = 1;
+    g.kps = g.nkt;
+    if (g.a.stype == DS_SCALE_POW2) return mm_launch<8, 8, MM_POW2, false>(g, stream);
+    // squares: one scale of B for all columns of a wave
+    if (g.b.shift) return mm_launch<8, 4, MM_F32, true>(g, stream);
+    return mm_launch<8, 4, MM_F32, false>(g, stream);
 }
 
 }  // namespace
@@ -108,8 +584,24 @@ extern "C" int ds_q8_matmul(const ds_q8 *a, const ds_q8 *b, void *c, int type, i
     }
     if ((rc = plain_check(c, type, a->rows, b->rows, ldc, "c")) != DS_OK) return rc;
     if (a->rows == 0 || b->rows == 0) return DS_OK;
-    Q8MatArgs g{q8_view(a), q8_view(b), c, ldc, type, int(a->rows), int(b->rows), int(a->cols),
-                int(q8_up(a->cols))};
+    Q8MatArgs g{};
+    g.a = q8_view(a);
+    g.b = q8_view(b);
+    g.c = c;
+    g.ldc = ldc;
+    g.type = type;
+    g.M = int(a->rows);
+    g.N = int(b->rows);
+    g.K = int(a->cols);
+    g.nkt = int(q8_up(a->cols));
+    const int unit = 4 * type_bytes(type);
+    g.cvec = reinterpret_cast<uintptr_t>(c) % unit == 0 && ldc % 4 == 0;
+    g.pvec = g.N % 4 == 0;
+    auto words = [](const ds_q8 *m) {
+        return reinterpret_cast<uintptr_t>(m->scale) % 4 == 0 && m->scale_ld % 4 == 0;
+    };
+    g.words = words(a) && words(b);
+    if (g.M > 16 && type != DS_TYPE_F32) return mm_tiles(g, stream);
     const int64_t tm = (a->rows + 15) / 16, tn = (b->rows + 15) / 16;
     if (tm > 65535) {
         set_error("ds_q8_matmul: %lld rows", (long long)a->rows);
