@@ -145,8 +145,13 @@ __device__ __forceinline__ void copy4(intx4 d, unsigned off, unsigned dst) {
 // How a tile's products are formed.
 enum {
     MM_POW2 = 0,   // scaled 8-bit instructions, power-of-two scales in the instruction
-    MM_F32 = 1     // 8-bit instructions block by block, each block's sum times fp32 scales
+    MM_F32 = 1,    // 8-bit instructions block by block, each block's sum times fp32 scales
+    // the same through bf16 instructions on the decoded values, whose sums are exact to fp32
+    MM_EXACT_POW2 = 2,
+    MM_EXACT_F32 = 3
 };
+constexpr bool mm_exact(int mode) { return mode >= MM_EXACT_POW2; }
+constexpr bool mm_words(int mode) { return mode == MM_POW2 || mode == MM_EXACT_POW2; }
 
 // 32 FM x 32 FN of C a workgroup of four waves, 16 FM x 16 FN a wave.
 template <int FM, int FN, int MODE>
@@ -154,13 +159,16 @@ struct MmShape {
     static constexpr int BM = 32 * FM, BN = 32 * FN, ROWS = BM + BN;
     static constexpr int STAGE = ROWS * kQ8Block;          // bytes of one 128-long step
     // the scales of four steps: a word of exponents or four fp32 numbers a row
-    static constexpr int SCALES = ROWS * (MODE == MM_POW2 ? 4 : 16);
+    static constexpr int SCALES = ROWS * (mm_words(MODE) ? 4 : 16);
     static constexpr int LDS = 2 * STAGE + 2 * SCALES;
 };
 
+// SQ: B's scales are of squares, one for all columns of a wave.  A tile of 256 columns or rows leaves
+// one wave a SIMD unit; the smaller ones two.
 template <int FM, int FN, int MODE, bool SQ, int FA, int FB>
-__global__ __launch_bounds__(256) void q8_mm(Q8MatArgs a) {
+__global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) {
     using S = MmShape<FM, FN, MODE>;
+    constexpr bool EXACT = mm_exact(MODE), WORDS = mm_words(MODE);
     constexpr int BM = S::BM, BN = S::BN, ROWS = S::ROWS, STAGE = S::STAGE, HM = FM / 2, HN = FN / 2;
     constexpr int LA = BM / 32, LB = BN / 32;              // copies a thread makes of either operand
     extern __shared__ __align__(16) uint8_t smem[];
@@ -245,7 +253,7 @@ __global__ __launch_bounds__(256) void q8_mm(Q8MatArgs a) {
     // Scales go through LDS four steps at a time: a word of four exponents a row, or four planes of
     // fp32 numbers; a wave copies those of 64 rows at once.
     uint8_t *const sbuf = smem + 2 * STAGE;
-    constexpr int ES = MODE == MM_POW2 ? 1 : 4;            // bytes of a scale
+    constexpr int ES = WORDS ? 1 : 4;           // bytes of a scale
     auto copy_scales = [&](int kt, int s) {
         if (kt >= a.nkt) return;
 #pragma unroll
@@ -259,11 +267,11 @@ __global__ __launch_bounds__(256) void q8_mm(Q8MatArgs a) {
             const unsigned sld = unsigned(v.sld) * ES;
             const int64_t at = int64_t(s0) * sld + int64_t(kt) * ES;
             const unsigned end = unsigned(((o0 + min(isa ? BM : BN, left) - 1) >> v.shift) - s0) * sld +
-                                 (MODE == MM_POW2 ? (unsigned(a.nkt - kt) + 3u) & ~3u : unsigned(a.nkt - kt) * 4u);
+                                 (WORDS ? (unsigned(a.nkt - kt) + 3u) & ~3u : unsigned(a.nkt - kt) * 4u);
             const uint8_t *const p = static_cast<const uint8_t *>(v.scale) + at;
             const unsigned off = unsigned(((o0 + row) >> v.shift) - s0) * sld;
             uint8_t *const dst = sbuf + s * S::SCALES + 4 * r0;
-            if (MODE == MM_POW2 && !a.words) {             // not in whole words: byte by byte
+            if (WORDS && !a.words) {             // not in whole words: byte by byte
                 int w = 0;
 #pragma unroll 1
                 for (int k = 0; k < 4 && kt + k < a.nkt; ++k)
@@ -274,7 +282,7 @@ __global__ __launch_bounds__(256) void q8_mm(Q8MatArgs a) {
             const intx4 d = buffer_of(p, end);
             const unsigned to = unsigned(uintptr_t(DS_LOCAL(dst)));
 #pragma unroll
-            for (int k = 0; k < (MODE == MM_POW2 ? 1 : 4); ++k) copy4(d, off + 4 * k, to + 4 * k * ROWS);
+            for (int k = 0; k < (WORDS ? 1 : 4); ++k) copy4(d, off + 4 * k, to + 4 * k * ROWS);
         }
     };
 
@@ -285,49 +293,81 @@ __global__ __launch_bounds__(256) void q8_mm(Q8MatArgs a) {
         for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0, 0, 0, 0};
     Frag alo[HM], ahi[HM], b0[HN], b1[HN];
     // The present step's scales: of A's rows and of B's columns.  MM_POW2: exponents in the low
-    // bytes, xn the words of the step after as read.  SQ: one of B for all columns.
+    // bytes, xn the words of the step after as read.  Otherwise fp32.
     constexpr int XN = FM + (MODE == MM_POW2 ? FN : 0);
     int xs[XN], xn[MODE == MM_POW2 ? XN : 1];
-    floatx4 sb[MODE == MM_POW2 ? 1 : FN];
+    floatx4 sb[MODE == MM_POW2 || SQ ? 1 : FN];
     float sq = 0.f, sqn = 0.f;
     auto scales_of = [&](int u) {
-        return reinterpret_cast<const int *>(sbuf + ((u >> 2) & 1) * S::SCALES) +
-               (MODE == MM_POW2 ? 0 : (u & 3) * ROWS);
+        return reinterpret_cast<const int *>(sbuf + ((u >> 2) & 1) * S::SCALES) + (WORDS ? 0 : (u & 3) * ROWS);
     };
-    auto scale_of_a = [&](const int *sc, int f) { return sc[16 * (FM * wm + f) + li]; };
-    auto word_of = [&](const int *sc, int f) {
-        return f < FM ? scale_of_a(sc, f) : sc[BM + 16 * (FN * wn + f - FM) + li];
+    auto word_of = [&](const int *sc, int f) {             // MM_POW2: of fragment f, B's after A's
+        return f < FM ? sc[16 * (FM * wm + f) + li] : sc[BM + 16 * (FN * wn + f - FM) + li];
     };
-    auto scale_of_b = [&](const int *sc, int f) {
-        return *reinterpret_cast<const floatx4 *>(sc + BM + 16 * (FN * wn + f) + 4 * lg);
+    // as fp32 bits; sh: the step's byte of the word
+    auto value = [](int v, int sh) { return WORDS ? int(max((unsigned(v) >> sh & 255u) << 23, 0x400000u)) : v; };
+    auto scale_of_a = [&](const int *sc, int f, int sh) { return value(sc[16 * (FM * wm + f) + li], sh); };
+    auto scale_of_b = [&](const int *sc, int f, int sh) {
+        const intx4 v = *reinterpret_cast<const intx4 *>(sc + BM + 16 * (FN * wn + f) + 4 * lg);
+        return floatx4{__int_as_float(value(v[0], sh)), __int_as_float(value(v[1], sh)),
+                       __int_as_float(value(v[2], sh)), __int_as_float(value(v[3], sh))};
+    };
+    auto scale_of_square = [&](const int *sc, int sh) {
+        return __int_as_float(value(sc[BM + 16 * FN * wn], sh));
     };
 
-    // MM_F32: a block's product waits for two more to be issued before it is scaled and added.
-    constexpr int NQ = HM * HN;
-    floatx4 p0 = {0, 0, 0, 0}, p1 = {0, 0, 0, 0}, s0 = {0, 0, 0, 0}, s1 = {0, 0, 0, 0};
+    // Sums of blocks wait for D more to be issued before they are scaled and added.
+    constexpr int NQ = HM * HN, D = EXACT ? 1 : 2;
+    floatx4 wp[D], ws[D];
+#pragma unroll
+    for (int d = 0; d < D; ++d) wp[d] = ws[d] = floatx4{0, 0, 0, 0};
+    auto add_block = [&](int i, int j, floatx4 p, floatx4 w) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[i][j][v] = fmaf(p[v], SQ ? w[0] : w[v], acc[i][j][v]);
+    };
+    // place of a quarter's q-th product; EXACT: down a column, so that B's fragment is decoded once
+    auto qi = [](int q) { return EXACT ? q % HM : q / HN; };
+    auto qj = [](int q) { return EXACT ? q / HM : q % HN; };
+    bf16x8 da[EXACT ? HM : 1][4], db[4];                   // EXACT: decoded fragments
     // A quarter of the wave's tile, fragments i0 .. of A by j0 .. of B; beside(q) issues what goes
-    // between its products q and q + 1.  pi, pj: the block that is waiting (and the one after it).
+    // between its products q and q + 1.  wi, wj: the quarter before.
     auto quarter = [&](const Frag (&fa)[HM], const Frag (&fb)[HN], int i0, int j0, auto beside, int wi, int wj) {
+        if constexpr (EXACT)
+            if (j0 == 0)
+#pragma unroll
+                for (int i = 0; i < HM; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        da[i][k] = to_bf16<FA>(fa[i].h[k >> 1][2 * (k & 1)], fa[i].h[k >> 1][2 * (k & 1) + 1]);
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
-            const int i = q / HN, j = q % HN;
+            const int i = qi(q), j = qj(q);
             if constexpr (MODE == MM_POW2) {
                 acc[i0 + i][j0 + j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
                     fb[j], fa[i], acc[i0 + i][j0 + j], FB, FA, 0, xs[FM + j0 + j], 0, xs[i0 + i]);
             } else {
-                const floatx4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                    fb[j], fa[i], floatx4{0, 0, 0, 0}, FB, FA, 0, 0, 0, 0);
-                const int o = q < 2 ? NQ - 2 + q : q - 2;  // place of the block that is due, in its quarter
-                const int oi = (q < 2 ? wi : i0) + o / HN, oj = (q < 2 ? wj : j0) + o % HN;
+                floatx4 p = {0, 0, 0, 0};
+                if constexpr (EXACT) {
+                    if (i == 0)
 #pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    acc[oi][oj][v] = fmaf(p0[v], SQ ? s0[0] : s0[v], acc[oi][oj][v]);
-                p0 = p1;
-                s0 = s1;
-                p1 = p;
+                        for (int k = 0; k < 4; ++k)
+                            db[k] = to_bf16<FB>(fb[j].h[k >> 1][2 * (k & 1)], fb[j].h[k >> 1][2 * (k & 1) + 1]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(db[k], da[i][k], p, 0, 0, 0);
+                } else {
+                    p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i], p, FB, FA, 0, 0, 0, 0);
+                }
+                const int o = q < D ? NQ - D + q : q - D;  // place of the block that is due
+                add_block((q < D ? wi : i0) + qi(o), (q < D ? wj : j0) + qj(o), wp[0], ws[0]);
+                if constexpr (D == 2) {
+                    wp[0] = wp[D - 1];
+                    ws[0] = ws[D - 1];
+                }
+                wp[D - 1] = p;
                 const float x = __int_as_float(xs[i0 + i]);
-                if constexpr (SQ) s1[0] = x * sq;
-                else s1 = x * sb[j0 + j];
+                if constexpr (SQ) ws[D - 1][0] = x * sq;
+                else ws[D - 1] = x * sb[j0 + j];
             }
             beside(q);
             __builtin_amdgcn_sched_barrier(0);
@@ -364,8 +404,8 @@ __global__ __launch_bounds__(256) void q8_mm(Q8MatArgs a) {
                 spread(q, HM, [&](int f) { xs[HM + f] = int(unsigned(xn[HM + f]) >> sh); });
                 spread(q, HN, [&](int f) { xs[FM + HN + f] = int(unsigned(xn[FM + HN + f]) >> sh); });
             } else {
-                if constexpr (!SQ) spread(q, HN, [&](int f) { sb[HN + f] = scale_of_b(sc, HN + f); });
-                spread(q, HM, [&](int f) { xs[HM + f] = scale_of_a(sc, HM + f); });
+                if constexpr (!SQ) spread(q, HN, [&](int f) { sb[HN + f] = scale_of_b(sc, HN + f, sh); });
+                spread(q, HM, [&](int f) { xs[HM + f] = scale_of_a(sc, HM + f, sh); });
             }
         }, HM, HN);
         quarter(alo, b1, 0, HN, [&](int q) {
@@ -379,8 +419,8 @@ __global__ __launch_bounds__(256) void q8_mm(Q8MatArgs a) {
             if constexpr (COPY) spread(q, PART, [&](int r) { copy1(da, db, cur, part_copy(r, 1)); });
             spread(q, 2 * HM, [&](int r) { alo[r >> 1].h[r & 1] = half(nxt, fa0, r >> 1, r & 1); });
             if constexpr (MODE != MM_POW2) {
-                spread(q, HM, [&](int f) { xs[f] = scale_of_a(scn, f); });
-                if (SQ && q == 0) sqn = __int_as_float(scn[BM + 16 * FN * wn]);
+                spread(q, HM, [&](int f) { xs[f] = scale_of_a(scn, f, shn); });
+                if (SQ && q == 0) sqn = scale_of_square(scn, shn);
             }
         }, 0, HN);
         quarter(ahi, b1, HM, HN, [&](int q) {
@@ -389,7 +429,7 @@ __global__ __launch_bounds__(256) void q8_mm(Q8MatArgs a) {
                 spread(q, HM, [&](int f) { xs[f] = int(unsigned(xn[f]) >> shn); });
                 spread(q, HN, [&](int f) { xs[FM + f] = int(unsigned(xn[FM + f]) >> shn); });
             } else if constexpr (!SQ) {
-                spread(q, HN, [&](int f) { sb[f] = scale_of_b(scn, f); });
+                spread(q, HN, [&](int f) { sb[f] = scale_of_b(scn, f, shn); });
             }
         }, HM, 0);
         if constexpr (SQ) sq = sqn;
@@ -413,16 +453,18 @@ __global__ __launch_bounds__(256) void q8_mm(Q8MatArgs a) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) b0[f].h[h] = half(0, fb0, f, h);
         const int *const sc = scales_of(0);
-#pragma unroll
-        for (int f = 0; f < XN; ++f) xs[f] = word_of(sc, f);
         if constexpr (MODE == MM_POW2) {
 #pragma unroll
-            for (int f = 0; f < XN; ++f) xn[f] = xs[f];
-        } else if constexpr (SQ) {
-            sq = __int_as_float(sc[BM + 16 * FN * wn]);
+            for (int f = 0; f < XN; ++f) xs[f] = xn[f] = word_of(sc, f);
         } else {
 #pragma unroll
-            for (int f = 0; f < FN; ++f) sb[f] = scale_of_b(sc, f);
+            for (int f = 0; f < FM; ++f) xs[f] = scale_of_a(sc, f, 0);
+            if constexpr (SQ) {
+                sq = scale_of_square(sc, 0);
+            } else {
+#pragma unroll
+                for (int f = 0; f < FN; ++f) sb[f] = scale_of_b(sc, f, 0);
+            }
         }
         int kt = kt0;
 #pragma unroll 1
@@ -434,14 +476,9 @@ __global__ __launch_bounds__(256) void q8_mm(Q8MatArgs a) {
             if (kt + 2 < kt1) copy_any(kt + 2, ((kt - kt0) & 1) * STAGE);
         }
         // the last step read ahead into a stage that nothing was copied to; its values are unused
-        if constexpr (MODE == MM_F32) {
-            for (int w = 0; w < 2; ++w) {
-                const int o = NQ - 2 + w, i = HM + o / HN, j = HN + o % HN;
-                const floatx4 p = w ? p1 : p0, s = w ? s1 : s0;
+        if constexpr (MODE != MM_POW2)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) acc[i][j][v] = fmaf(p[v], SQ ? s[0] : s[v], acc[i][j][v]);
-            }
-        }
+            for (int d = 0; d < D; ++d) add_block(HM + qi(NQ - D + d), HN + qj(NQ - D + d), wp[d], ws[d]);
     }
 
     // Lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of each 16 x 16 block.
@@ -540,7 +577,7 @@ int mm_launch(Q8MatArgs &g, hipStream_t stream) {
     using S = MmShape<FM, FN, MODE>;
     g.tiles_m = (g.M + S::BM - 1) / S::BM;
     g.tiles_n = (g.N + S::BN - 1) / S::BN;
-    g.group = 8;
+    g.group = 4;
     const int64_t grid = int64_t(g.tiles_m) * g.tiles_n * g.ks;
     if (grid > kGridLimit) {
         set_error("ds_q8_matmul: %lld workgroups", (long long)grid);
@@ -559,13 +596,19 @@ int mm_launch(Q8MatArgs &g, hipStream_t stream) {
     return hip_ok(hipGetLastError(), "8-bit matmul join") ? DS_OK : DS_EHIP;
 }
 
+// SQ: squares, one scale of B for all columns of a wave
+template <int FM, int FN, int MODE>
+int mm_square(Q8MatArgs &g, hipStream_t stream) {
+    return g.b.shift ? mm_launch<FM, FN, MODE, true>(g, stream) : mm_launch<FM, FN, MODE, false>(g, stream);
+}
+
 int mm_tiles(Q8MatArgs &g, hipStream_t stream) {
     g.ks = 1;
     g.kps = g.nkt;
-    if (g.a.stype == DS_SCALE_POW2) return mm_launch<8, 8, MM_POW2, false>(g, stream);
-    // squares: one scale of B for all columns of a wave
-    if (g.b.shift) return mm_launch<8, 4, MM_F32, true>(g, stream);
-    return mm_launch<8, 4, MM_F32, false>(g, stream);
+    const bool pow2 = g.a.stype == DS_SCALE_POW2;
+    if (g.type == DS_TYPE_F32)
+        return pow2 ? mm_square<4, 4, MM_EXACT_POW2>(g, stream) : mm_square<4, 4, MM_EXACT_F32>(g, stream);
+    return pow2 ? mm_launch<8, 8, MM_POW2, false>(g, stream) : mm_square<8, 4, MM_F32>(g, stream);
 }
 
 }  // namespace
@@ -601,7 +644,7 @@ extern "C" int ds_q8_matmul(const ds_q8 *a, const ds_q8 *b, void *c, int type, i
         return reinterpret_cast<uintptr_t>(m->scale) % 4 == 0 && m->scale_ld % 4 == 0;
     };
     g.words = words(a) && words(b);
-    if (g.M > 16 && type != DS_TYPE_F32) return mm_tiles(g, stream);
+    if (g.M > 16) return mm_tiles(g, stream);
     const int64_t tm = (a->rows + 15) / 16, tn = (b->rows + 15) / 16;
     if (tm > 65535) {
         set_error("ds_q8_matmul: %lld rows", (long long)a->rows);
