@@ -45,63 +45,138 @@ __device__ __forceinline__ void store4(void *c, int type, int64_t at, int col, i
     }
 }
 
-// 32 bytes of a row from k on, 0 from K on.
-__device__ __forceinline__ intx8 load32(const uint8_t *row, int k, int K) {
-    intx8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (k + 32 <= K) {
-        const intx4 *p = reinterpret_cast<const intx4 *>(row + k);
-        const intx4 x = p[0], y = p[1];
-        v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-    } else {
+// 16 bytes from a 16-byte aligned p, zeros from the n-th on.  They are loaded whole where one of
+// them exists: an aligned 16 bytes never reach past the page, or the allocation, of any one.
+__device__ __forceinline__ intx4 first16(const uint8_t *p, int n) {
+    intx4 v = {0, 0, 0, 0};
+    if (n > 0) v = *reinterpret_cast<const intx4 *>(p);
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (k + i < K) v[i >> 2] |= int(unsigned(row[k + i]) << (8 * (i & 3)));
+    for (int i = 0; i < 4; ++i)
+        v[i] &= n >= 4 * i + 4 ? -1 : n > 4 * i ? (1 << (8 * (n - 4 * i))) - 1 : 0;
+    return v;
+}
+__device__ __forceinline__ intx8 whole32(const uint8_t *p) {
+    const intx4 x = reinterpret_cast<const intx4 *>(p)[0], y = reinterpret_cast<const intx4 *>(p)[1];
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+__device__ __forceinline__ intx8 first32(const uint8_t *p, int n) {
+    const intx4 x = first16(p, n), y = first16(p + 16, n - 16);
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// Scales i .. i + 3 as fp32.
+__device__ __forceinline__ floatx4 scales4(const void *s, int stype, int64_t i) {
+    floatx4 v;
+    if (stype == DS_SCALE_F32) {
+        __builtin_memcpy(&v, static_cast<const float *>(s) + i, 16);   // aligned to 4
+        return v;
     }
+    unsigned w;
+    __builtin_memcpy(&w, static_cast<const uint8_t *>(s) + i, 4);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(max((w >> (8 * k) & 255u) << 23, 0x400000u));
     return v;
 }
 
 // One 128-long step of a 16 x 16 product, lane l holding bytes 32 (l / 16) .. + 31 of row
 // l % 16 of either operand: the same 8 bytes of both make one bf16 instruction, so it does
 // not matter which k those are.  Result: row 4 (l / 16) + i of `b`, row l % 16 of `a`.
-template <int FA, int FB>
-__device__ __forceinline__ floatx4 dot128(intx8 a, intx8 b) {
+template <int FB>
+__device__ __forceinline__ floatx4 dot128(const bf16x8 (&a)[4], intx8 b) {
     floatx4 p = {0, 0, 0, 0};
 #pragma unroll
     for (int u = 0; u < 4; ++u)
-        p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16<FB>(b[2 * u], b[2 * u + 1]),
-                                                    to_bf16<FA>(a[2 * u], a[2 * u + 1]), p, 0, 0, 0);
+        p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16<FB>(b[2 * u], b[2 * u + 1]), a[u], p, 0, 0, 0);
     return p;
 }
 
-// 16 x 16 of C a workgroup; its waves take the steps of the reduction in turn.
-template <int FA, int FB>
-__global__ __launch_bounds__(1024) void q8_few(Q8MatArgs a) {
-    __shared__ float red[16 * 256];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
-    const int li = lane & 15, lg = lane >> 4;
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
-    const int m = min(m0 + li, a.M - 1), n = min(n0 + li, a.N - 1);
-    const uint8_t *pa = a.a.data + int64_t(m) * a.a.ld, *pb = a.b.data + int64_t(n) * a.b.ld;
+constexpr int kFewWaves = 8;
+
+// Up to 16 rows of A: the weight passes once from memory to registers, in the layout of the
+// matrix instructions, and bounds the time.  A workgroup has 16 NT columns; each of its waves
+// takes a run of the reduction's steps, 4 / NT at a time in flight, and their sums meet in LDS.
+// SQ: B's scales are of squares, one for the workgroup's columns.
+template <int NT, bool SQ, int FA, int FB>
+__global__ __launch_bounds__(64 * kFewWaves) void q8_few(Q8MatArgs a) {
+    constexpr int U = 4 / NT, SB = SQ ? 1 : 4 * NT;
+    __shared__ float red[kFewWaves * 256];
+    const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4, nw = blockDim.x >> 6;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16;
+    const int m = min(m0 + li, a.M - 1);
+    const uint8_t *const pa = a.a.data + int64_t(m) * a.a.ld + 32 * lg;
+    const uint8_t *pb[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) pb[j] = a.b.data + int64_t(min(n0 + 16 * j + li, a.N - 1)) * a.b.ld + 32 * lg;
     const int64_t sa = int64_t(m >> a.a.shift) * a.a.sld;
-    int64_t sb[4];
+    auto sb = [&](int i) {
+        return int64_t(min(n0 + (SQ ? 0 : 16 * (i / 4) + 4 * lg + i % 4), a.N - 1) >> a.b.shift) * a.b.sld;
+    };
+
+    floatx4 acc[NT];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        sb[i] = int64_t(min(n0 + 4 * lg + i, a.N - 1) >> a.b.shift) * a.b.sld;
-    floatx4 acc = {0, 0, 0, 0};
-    for (int kt = w; kt < a.nkt; kt += nw) {
-        const int k = kt * kQ8Block + 32 * lg;
-        const floatx4 p = dot128<FA, FB>(load32(pa, k, a.K), load32(pb, k, a.K));
-        const float s = scale_at(a.a.scale, a.a.stype, sa + kt);
+    for (int j = 0; j < NT; ++j) acc[j] = floatx4{0, 0, 0, 0};
+    // a wave's run of steps in whole fours, whose scales are read together
+    const int z = blockIdx.z, kz = min(a.nkt, (z + 1) * a.kps);
+    const int per = ((a.kps + nw - 1) / nw + 3) & ~3, k0 = z * a.kps + w * per, k1 = min(kz, k0 + per);
+    auto add = [&](intx8 va, const intx8 (&vb)[NT], float s, auto t) {
+        bf16x8 da[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] += p[i] * (s * scale_at(a.b.scale, a.b.stype, sb[i] + kt));
+        for (int i = 0; i < 4; ++i) da[i] = to_bf16<FA>(va[2 * i], va[2 * i + 1]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const floatx4 p = dot128<FB>(da, vb[j]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[j][i] = fmaf(p[i], s * t(SQ ? 0 : 4 * j + i), acc[j][i]);
+        }
+    };
+    int kt = k0;
+#pragma unroll 1
+    for (; kt + 4 <= k1 && (kt + 4) * kQ8Block <= a.K; kt += 4) {
+        const floatx4 s = scales4(a.a.scale, a.a.stype, sa + kt);
+        floatx4 t[SB];
+#pragma unroll
+        for (int i = 0; i < SB; ++i) t[i] = scales4(a.b.scale, a.b.stype, sb(i) + kt);
+#pragma unroll
+        for (int h = 0; h < 4; h += U) {
+            intx8 va[U], vb[U][NT];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t k = int64_t(kt + h + u) * kQ8Block;
+#pragma unroll
+                for (int j = 0; j < NT; ++j) vb[u][j] = whole32(pb[j] + k);
+                va[u] = whole32(pa + k);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) add(va[u], vb[u], s[h + u], [&](int i) { return t[i][h + u]; });
+        }
     }
-    *reinterpret_cast<floatx4 *>(red + w * 256 + li * 16 + 4 * lg) = acc;
-    __syncthreads();
-    for (int e = threadIdx.x; e < 256; e += blockDim.x) {
-        float v = 0.f;
-        for (int i = 0; i < nw; ++i) v += red[i * 256 + e];
-        const int r = m0 + (e >> 4), c = n0 + (e & 15);
-        if (r < a.M && c < a.N) store_c(a.c, a.type, int64_t(r) * a.ldc + c, v);
+#pragma unroll 1
+    for (; kt < k1; ++kt) {                                // the last steps, which may reach past K
+        const int k = kt * kQ8Block, n = a.K - k - 32 * lg;
+        intx8 vb[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) vb[j] = first32(pb[j] + k, n);
+        float t[SB];
+#pragma unroll
+        for (int i = 0; i < SB; ++i) t[i] = scale_at(a.b.scale, a.b.stype, sb(i) + kt);
+        add(first32(pa + k, n), vb, scale_at(a.a.scale, a.a.stype, sa + kt), [&](int i) { return t[i]; });
+    }
+    // the waves' sums, in their order, 16 columns at a time
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        if (j) __syncthreads();
+        *reinterpret_cast<floatx4 *>(red + (w * 16 + li) * 16 + 4 * lg) = acc[j];
+        __syncthreads();
+        for (int e = threadIdx.x; e < 256; e += blockDim.x) {
+            float v = 0.f;
+#pragma unroll
+            for (int i = 0; i < kFewWaves; ++i) v += i < nw ? red[i * 256 + e] : 0.f;
+            const int r = m0 + e / 16, c = n0 + 16 * j + e % 16;
+            if (r >= a.M || c >= a.N) continue;
+            if (a.part) a.part[(int64_t(z) * a.M + r) * a.N + c] = v;
+            else store_c(a.c, a.type, int64_t(r) * a.ldc + c, v);
+        }
     }
 }
 
@@ -225,15 +300,7 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
             const uint8_t *p = (j < LA ? pa + int64_t(min(row, a.M - 1 - m0)) * a.a.ld
                                        : pb + int64_t(min(row, a.N - 1 - n0)) * a.b.ld) +
                                int64_t(kt) * kQ8Block + ck;
-            intx4 v = {0, 0, 0, 0};
-            if (left >= 16) {
-                v = *reinterpret_cast<const intx4 *>(p);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (i < left) v[i >> 2] |= int(unsigned(p[i]) << (8 * (i & 3)));
-            }
-            *reinterpret_cast<intx4 *>(smem + st + wid * 1024 + j * 4096 + lane * 16) = v;
+            *reinterpret_cast<intx4 *>(smem + st + wid * 1024 + j * 4096 + lane * 16) = first16(p, left);
         }
     };
 
@@ -572,6 +639,22 @@ int by_formats(int fa, int fb, Fn fn) {
     return hip_ok(hipGetLastError(), "8-bit matmul launch") ? DS_OK : DS_EHIP;
 }
 
+// Splits the reduction into `ks` runs of a multiple of `unit` steps, whose partial products go to
+// the stream's workspace.
+int split(Q8MatArgs &g, int ks, int unit, hipStream_t stream) {
+    if (ks <= 1) return DS_OK;
+    g.kps = ((g.nkt + ks - 1) / ks + unit - 1) / unit * unit;
+    g.ks = (g.nkt + g.kps - 1) / g.kps;
+    return g.ks > 1 ? split_workspace(int64_t(g.ks) * g.M * g.N, stream, &g.part) : DS_OK;
+}
+
+int join(const Q8MatArgs &g, hipStream_t stream) {
+    if (g.ks == 1) return DS_OK;
+    const int64_t quads = int64_t(g.M) * ((g.N + 3) / 4);
+    q8_join<<<unsigned(std::min<int64_t>((quads + 255) / 256, 4096)), 256, 0, stream>>>(g);
+    return hip_ok(hipGetLastError(), "8-bit matmul join") ? DS_OK : DS_EHIP;
+}
+
 template <int FM, int FN, int MODE, bool SQ>
 int mm_launch(Q8MatArgs &g, hipStream_t stream) {
     using S = MmShape<FM, FN, MODE>;
@@ -590,10 +673,7 @@ int mm_launch(Q8MatArgs &g, hipStream_t stream) {
         if (rc == DS_OK) k<<<unsigned(grid), 256, S::LDS, stream>>>(g);
     });
     if (rc != DS_OK || done != DS_OK) return rc != DS_OK ? rc : done;
-    if (g.ks == 1) return DS_OK;
-    const int64_t quads = int64_t(g.M) * ((g.N + 3) / 4);
-    q8_join<<<unsigned(std::min<int64_t>((quads + 255) / 256, 4096)), 256, 0, stream>>>(g);
-    return hip_ok(hipGetLastError(), "8-bit matmul join") ? DS_OK : DS_EHIP;
+    return join(g, stream);
 }
 
 // SQ: squares, one scale of B for all columns of a wave
@@ -602,13 +682,70 @@ int mm_square(Q8MatArgs &g, hipStream_t stream) {
     return g.b.shift ? mm_launch<FM, FN, MODE, true>(g, stream) : mm_launch<FM, FN, MODE, false>(g, stream);
 }
 
+// The split of a reduction over tiles of 128 x 128, by what each took on the chip: a step of 128 about
+// `step` us in a workgroup that has its SIMD units to itself, and the join 3 us and the partial sums'
+// writing and reading.  32x4096x4096 20.7 -> 13.9 us by four, 64x16384x8192 49 -> 38; 512x4096x4096
+// would go from 21.8 to 22.8 and stays whole.
+int mm_splits(const Q8MatArgs &g, double step) {
+    const int64_t tiles = int64_t((g.M + 127) / 128) * ((g.N + 127) / 128);
+    const double sums = double(g.M) * g.N * 10 / 4.5e6;
+    int best = 1;
+    double least = g.nkt * step;
+    for (int ks = 2; ks <= 8 && tiles * ks <= 512 && g.nkt >= 4 * ks; ks *= 2) {
+        const double t = double(g.nkt) / ks * step + 3 + ks * sums;
+        if (t < least) {
+            least = t;
+            best = ks;
+        }
+    }
+    return best;
+}
+
 int mm_tiles(Q8MatArgs &g, hipStream_t stream) {
-    g.ks = 1;
-    g.kps = g.nkt;
-    const bool pow2 = g.a.stype == DS_SCALE_POW2;
-    if (g.type == DS_TYPE_F32)
-        return pow2 ? mm_square<4, 4, MM_EXACT_POW2>(g, stream) : mm_square<4, 4, MM_EXACT_F32>(g, stream);
-    return pow2 ? mm_launch<8, 8, MM_POW2, false>(g, stream) : mm_square<8, 4, MM_F32>(g, stream);
+    const bool pow2 = g.a.stype == DS_SCALE_POW2, exact = g.type == DS_TYPE_F32;
+    auto tiles = [&](int bm, int bn) { return int64_t((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn); };
+    if (pow2 && !exact) {
+        // Rounds of workgroups over 256 CUs times a round's time: a step of 1.47, 0.95, 1.1 us (two
+        // workgroups a CU, 0.62 for one) and what comes before and after.  2048x4096x8192: 92, 66
+        // and 71 us; 4096x4096x4096: 61, 73 and 69; 1024x4096x4096: 51, 33 and 23.
+        const double n = g.nkt;
+        const int64_t t = tiles(128, 128);
+        const double large = double((tiles(256, 256) + 255) / 256) * (1.47 * n + 14);
+        const double tall = double((tiles(256, 128) + 255) / 256) * (0.95 * n + 6);
+        const double small = double(t / 512) * (1.1 * n + 5) +
+                             (t % 512 > 256 ? 1.1 * n + 5 : t % 512 ? 0.62 * n + 5 : 0);
+        if (large <= tall && large <= small) return mm_launch<8, 8, MM_POW2, false>(g, stream);
+        if (tall <= small) return mm_launch<8, 4, MM_POW2, false>(g, stream);
+    }
+    const int rc = split(g, mm_splits(g, exact ? 1.0 : 0.5), 4, stream);
+    if (rc != DS_OK) return rc;
+    if (exact) return pow2 ? mm_square<4, 4, MM_EXACT_POW2>(g, stream) : mm_square<4, 4, MM_EXACT_F32>(g, stream);
+    return pow2 ? mm_launch<4, 4, MM_POW2, false>(g, stream) : mm_square<4, 4, MM_F32>(g, stream);
+}
+
+template <int NT, bool SQ>
+int few_launch(Q8MatArgs &g, int waves, hipStream_t stream) {
+    const unsigned tn = unsigned((g.N + 16 * NT - 1) / (16 * NT)), tm = unsigned((g.M + 15) / 16);
+    const int rc = by_formats(g.a.fmt, g.b.fmt, [&](auto fa, auto fb) {
+        q8_few<NT, SQ, fa.value, fb.value><<<dim3(tn, tm, unsigned(g.ks)), 64 * waves, 0, stream>>>(g);
+    });
+    return rc == DS_OK ? join(g, stream) : rc;
+}
+
+int few(Q8MatArgs &g, hipStream_t stream) {
+    // Few columns under a long reduction leave most CUs idle: it is split over workgroups too
+    // (8x512x16384 17.8 -> 10.4 us, 16x2048x8192 12.6 -> 11.5; 16x4096x16384 would go from 25 to 28).
+    if (g.N <= 2048 && g.nkt >= 64) {
+        const int rc = split(g, std::min(g.nkt / 16, 8), 4, stream);
+        if (rc != DS_OK) return rc;
+    }
+    // 32 columns a workgroup read A half as often and are enough workgroups in wide layers
+    // (16x16384x8192 39 -> 32 us, 16x8192x8192 23.1 -> 21.6; 1x8192x8192 would go from 18.4 to 21.2)
+    const bool two = g.N >= 16384 || (g.N >= 8192 && (g.M > 4 || !g.b.shift));
+    // at least four steps a wave, and with 32 columns 16 of them
+    const int waves = std::clamp((g.kps + 3) / 4, 1, two && g.kps <= 64 ? 4 : kFewWaves);
+    if (two) return g.b.shift ? few_launch<2, true>(g, waves, stream) : few_launch<2, false>(g, waves, stream);
+    return g.b.shift ? few_launch<1, true>(g, waves, stream) : few_launch<1, false>(g, waves, stream);
 }
 
 }  // namespace
@@ -637,6 +774,8 @@ extern "C" int ds_q8_matmul(const ds_q8 *a, const ds_q8 *b, void *c, int type, i
     g.N = int(b->rows);
     g.K = int(a->cols);
     g.nkt = int(q8_up(a->cols));
+    g.ks = 1;
+    g.kps = g.nkt;
     const int unit = 4 * type_bytes(type);
     g.cvec = reinterpret_cast<uintptr_t>(c) % unit == 0 && ldc % 4 == 0;
     g.pvec = g.N % 4 == 0;
@@ -644,14 +783,7 @@ extern "C" int ds_q8_matmul(const ds_q8 *a, const ds_q8 *b, void *c, int type, i
         return reinterpret_cast<uintptr_t>(m->scale) % 4 == 0 && m->scale_ld % 4 == 0;
     };
     g.words = words(a) && words(b);
-    if (g.M > 16) return mm_tiles(g, stream);
-    const int64_t tm = (a->rows + 15) / 16, tn = (b->rows + 15) / 16;
-    if (tm > 65535) {
-        set_error("ds_q8_matmul: %lld rows", (long long)a->rows);
-        return DS_EUNSUPPORTED;
-    }
-    const int waves = std::clamp(g.nkt, 1, 8);
-    return by_formats(g.a.fmt, g.b.fmt, [&](auto fa, auto fb) {
-        q8_few<fa.value, fb.value><<<dim3(unsigned(tn), unsigned(tm)), 64 * waves, 0, stream>>>(g);
-    });
+    // (32 rows of a short reduction too: 32x4096x4096 12.6 us, in tiles 13.9)
+    if (g.M > (g.nkt <= 32 ? 32 : 16)) return mm_tiles(g, stream);
+    return few(g, stream);
 }
