@@ -17,5 +17,7 @@ def __getattr__(name):
     if name == "_lib" or name in _EXPORTS:
         import importlib
         lib = importlib.import_module("._lib", __name__)
-        return lib if name == "_lib" else getattr(lib, name)
+        value = lib if name == "_lib" else getattr(lib, name)
+        globals()[name] = value          # found without this function from now on
+        return value
     raise AttributeError(name)

@@ -70,10 +70,20 @@ __device__ __forceinline__ void load8(const T *row, int c, int cols, bool vec, f
     }
 }
 
-__device__ __forceinline__ unsigned max8(const float (&v)[8]) {
+// The largest magnitude of the values as bits, NaN and infinities above all.
+template <int N>
+__device__ __forceinline__ unsigned max_bits(const float (&v)[N]) {
     unsigned m = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, finite_abs(v[i]));
+    for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+}
+// The same of the finite ones.
+template <int N>
+__device__ __forceinline__ unsigned max_finite(const float (&v)[N]) {
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = max(m, finite_abs(v[i]));
     return m;
 }
 
@@ -95,7 +105,10 @@ __device__ __forceinline__ void store8(uint8_t *row, int c, int cols, intx2 q) {
 
 // One 1x128 block of row r at columns c0 .. c0+127, held by 16 lanes of eight values each.
 __device__ __forceinline__ void emit_block(const Q8View &m, int r, int blk, int cl, const float (&v)[8]) {
-    const BlockScale s = block_scale(max16(max8(v)), m.fmt, m.stype);
+    unsigned top = max16(max_bits(v));
+    // what is not finite sets no scale: only a wave that holds some looks at each value
+    if (__any(top >= 0x7f800000u)) top = max16(max_finite(v));
+    const BlockScale s = block_scale(top, m.fmt, m.stype);
     store8(m.data + int64_t(r) * m.ld, blk * kQ8Block + 8 * cl, m.cols, pack8(v, s.inv, m.fmt));
     if (cl == 0) store_scale(m, int64_t(r) * m.sld + blk, s.bits);
 }
@@ -115,109 +128,127 @@ __global__ __launch_bounds__(256) void q8_rows(const T *x, int64_t ldx, int vec,
 }
 
 // ---- tiles of 128 x 128 -----------------------------------------------------------
-// 256 threads; thread t holds rows 8 (t / 16) .. + 7 of columns 8 (t % 16) .. + 7.
+// 512 threads; thread t holds rows 4 (t / 16) .. + 3 of columns 8 (t % 16) .. + 7.
+constexpr int kTileThreads = 512, kRows = 4, kTileWaves = kTileThreads / 64;
 
 struct TileLds {
-    unsigned colmax[4][128];
+    unsigned colmax[kTileWaves][128];
     BlockScale cs[128];
-    intx2 t[128 * 17];           // transposed bytes: column c's rows 8 g .. + 7 at c * 17 + g
+    // transposed bytes: column c's 16 rows of wave w are the 16 bytes at c * 8 + (w ^ c / 8 % 8), so
+    // that the 16 columns a wave writes at once lie in different banks
+    intx4 t[128 * 8];
 };
 
-// Writes a tile's values to `row` at (r0, c0) and transposed to `col` at (c0, r0); either has
+// Largest over the wave's 16 rows of column 8 (lane % 16) + c, for each c.
+__device__ __forceinline__ unsigned over_rows(unsigned m) {
+    m = max(m, unsigned(__shfl_xor(int(m), 16)));
+    return max(m, unsigned(__shfl_xor(int(m), 32)));
+}
+
+// Writes a tile's values to `row` at (r0, c0) and transposed to `col` at (rc0, r0); either has
 // data == null when not wanted.  Elements outside the matrices hold 0.
-__device__ __forceinline__ void emit_tile(const float (&v)[8][8], const Q8View &row, const Q8View &col,
+__device__ __forceinline__ void emit_tile(const float (&v)[kRows][8], const Q8View &row, const Q8View &col,
                                           int r0, int c0, int rc0, TileLds &lds) {
-    const int tid = threadIdx.x, cl = tid & 15, rg = tid >> 4;
+    const int tid = threadIdx.x, cl = tid & 15, rg = tid >> 4, w = tid >> 6;
     const bool square = (row.data ? row.shift : col.shift) != 0;
-    // r0, c0: place in `row`; rc0: the row of `col` that column 0 goes to
-    if (col.data || square) {
-        unsigned m[8];
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            m[c] = 0;
-#pragma unroll
-            for (int r = 0; r < 8; ++r) m[c] = max(m[c], finite_abs(v[r][c]));
-            m[c] = max(m[c], unsigned(__shfl_xor(int(m[c]), 16)));
-            m[c] = max(m[c], unsigned(__shfl_xor(int(m[c]), 32)));
-        }
-        if ((tid & 48) == 0)
-#pragma unroll
-            for (int c = 0; c < 8; ++c) lds.colmax[tid >> 6][8 * cl + c] = m[c];
-        __syncthreads();
-        unsigned all = 0;
-        if (square) {
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) all = max(all, lds.colmax[w][8 * cl + c]);
-            all = max16(all);
-            if (row.data) {
-                const BlockScale s = block_scale(all, row.fmt, row.stype);
-                if (tid == 0) store_scale(row, int64_t(r0 >> 7) * row.sld + (c0 >> 7), s.bits);
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    const int rr = r0 + 8 * rg + r;
-                    if (rr < row.rows)
-                        store8(row.data + int64_t(rr) * row.ld, c0 + 8 * cl, row.cols,
-                               pack8(v[r], s.inv, row.fmt));
-                }
-            }
-            if (col.data && tid == 0) {
-                const BlockScale s = block_scale(all, col.fmt, col.stype);
-                store_scale(col, int64_t(rc0 >> 7) * col.sld + (r0 >> 7), s.bits);
-            }
-        }
-        if (col.data) {
-            if (tid < 128) {
-                unsigned m1 = all;
-                if (!square)
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) m1 = max(m1, lds.colmax[w][tid]);
-                const BlockScale s = block_scale(m1, col.fmt, col.stype);
-                lds.cs[tid] = s;
-                if (!square && rc0 + tid < col.rows)
-                    store_scale(col, int64_t(rc0 + tid) * col.sld + (r0 >> 7), s.bits);
-            }
-            __syncthreads();
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                const float inv = lds.cs[8 * cl + c].inv;
-                const float u[8] = {v[0][c], v[1][c], v[2][c], v[3][c],
-                                    v[4][c], v[5][c], v[6][c], v[7][c]};
-                lds.t[(8 * cl + c) * 17 + rg] = pack8(u, inv, col.fmt);
-            }
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int i = j * 256 + tid, c = i >> 3, g = i & 7;
-                if (rc0 + c < col.rows) {
-                    uint8_t *p = col.data + int64_t(rc0 + c) * col.ld;
-                    store8(p, r0 + 16 * g, col.cols, lds.t[c * 17 + 2 * g]);
-                    store8(p, r0 + 16 * g + 8, col.cols, lds.t[c * 17 + 2 * g + 1]);
-                }
-            }
-            __syncthreads();   // the LDS is free for the next tile
-        }
-    }
     if (row.data && !square)
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            const int rr = r0 + 8 * rg + r;
+        for (int r = 0; r < kRows; ++r) {
+            const int rr = r0 + kRows * rg + r;
             if (rr < row.rows) emit_block(row, rr, c0 >> 7, cl, v[r]);
         }
+    if (!col.data && !square) return;
+    unsigned m[8], any = 0;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const float u[kRows] = {v[0][c], v[1][c], v[2][c], v[3][c]};
+        m[c] = max_bits(u);
+        any = max(any, m[c]);
+    }
+    if (__any(any >= 0x7f800000u))
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const float u[kRows] = {v[0][c], v[1][c], v[2][c], v[3][c]};
+            m[c] = max_finite(u);
+        }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) m[c] = over_rows(m[c]);
+    if ((tid & 48) == 0) {
+        unsigned *p = lds.colmax[w] + 8 * cl;
+        reinterpret_cast<intx4 *>(p)[0] = intx4{int(m[0]), int(m[1]), int(m[2]), int(m[3])};
+        reinterpret_cast<intx4 *>(p)[1] = intx4{int(m[4]), int(m[5]), int(m[6]), int(m[7])};
+    }
+    __syncthreads();
+    unsigned all = 0;
+    if (square) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int i = 0; i < kTileWaves; ++i) all = max(all, lds.colmax[i][8 * cl + c]);
+        all = max16(all);
+        if (row.data) {
+            const BlockScale s = block_scale(all, row.fmt, row.stype);
+            if (tid == 0) store_scale(row, int64_t(r0 >> 7) * row.sld + (c0 >> 7), s.bits);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const int rr = r0 + kRows * rg + r;
+                if (rr < row.rows)
+                    store8(row.data + int64_t(rr) * row.ld, c0 + 8 * cl, row.cols, pack8(v[r], s.inv, row.fmt));
+            }
+        }
+        if (!col.data) return;
+        if (tid == 0) {
+            const BlockScale s = block_scale(all, col.fmt, col.stype);
+            store_scale(col, int64_t(rc0 >> 7) * col.sld + (r0 >> 7), s.bits);
+        }
+    }
+    if (tid < 128) {
+        unsigned top = all;
+        if (!square)
+#pragma unroll
+            for (int i = 0; i < kTileWaves; ++i) top = max(top, lds.colmax[i][tid]);
+        const BlockScale s = block_scale(top, col.fmt, col.stype);
+        lds.cs[tid] = s;
+        if (!square && rc0 + tid < col.rows)
+            store_scale(col, int64_t(rc0 + tid) * col.sld + (r0 >> 7), s.bits);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const int cc = 8 * cl + c;
+        const float inv = lds.cs[cc].inv;
+        reinterpret_cast<int *>(lds.t)[(cc * 8 + (w ^ (cl & 7))) * 4 + (rg & 3)] =
+            pack4(v[0][c] * inv, v[1][c] * inv, v[2][c] * inv, v[3][c] * inv, col.fmt);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int i = j * kTileThreads + tid, c = i >> 3, g = i & 7, at = r0 + 16 * g;
+        if (rc0 + c < col.rows && at < col.cols) {
+            uint8_t *p = col.data + int64_t(rc0 + c) * col.ld;
+            const intx4 q = lds.t[c * 8 + (g ^ (c >> 3 & 7))];
+            if (at + 16 <= col.cols) {
+                *reinterpret_cast<intx4 *>(p + at) = q;
+            } else {
+                store8(p, at, col.cols, intx2{q[0], q[1]});
+                store8(p, at + 8, col.cols, intx2{q[2], q[3]});
+            }
+        }
+    }
+    // the next tile's first writes here come after a barrier that follows these reads
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void q8_tile(const T *x, int64_t ldx, int vec, int rows, int cols,
-                                               int tiles_c, Q8View row, Q8View col) {
+__global__ __launch_bounds__(kTileThreads) void q8_tile(const T *x, int64_t ldx, int vec, int rows, int cols,
+                                                        int tiles_c, Q8View row, Q8View col) {
     __shared__ TileLds lds;
     const int cl = threadIdx.x & 15, rg = threadIdx.x >> 4;
     const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
     const int r0 = tr * 128, c0 = tc * 128;
-    float v[8][8];
+    float v[kRows][8];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        const int rr = r0 + 8 * rg + r;
+    for (int r = 0; r < kRows; ++r) {
+        const int rr = r0 + kRows * rg + r;
         if (rr < rows) {
             load8(x + int64_t(rr) * ldx, c0 + 8 * cl, cols, vec, v[r]);
         } else {
@@ -302,61 +333,49 @@ __device__ __forceinline__ intx2 bytes8(const uint8_t *row, int c, int cols) {
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void swiglu8_grad_tile(Q8View saved, const T *dh, int64_t ldh, int vec,
-                                                         int hidden, int up, int tiles_c, Q8View dgu,
-                                                         Q8View dgu_t, Q8View h_t) {
+__global__ __launch_bounds__(kTileThreads, 4) void swiglu8_grad_tile(Q8View saved, const T *dh, int64_t ldh,
+                                                                  int vec, int hidden, int up, int tiles_c,
+                                                                  Q8View dgu, Q8View dgu_t, Q8View h_t) {
     __shared__ TileLds lds;
     const int cl = threadIdx.x & 15, rg = threadIdx.x >> 4;
     const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
     const int r0 = tr * 128, c0 = tc * 128, c = c0 + 8 * cl;
-    const int rows = saved.rows;
-    Q8View none = dgu;
-    none.data = nullptr;
-    none.shift = 0;
-    auto part = [&](int which, float (&v)[8][8]) {
+    float dg[kRows][8], du[kRows][8], h[kRows][8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            const int rr = r0 + 8 * rg + r;
-            if (rr < rows && c0 < hidden) {
-                const uint8_t *q = saved.data + int64_t(rr) * saved.ld;
-                const int64_t si = int64_t(rr) * saved.sld + tc;
-                float g[8], u[8], d[8];
-                values8(bytes8(q, c, hidden), scale_at(saved.scale, saved.stype, si), saved.fmt, c,
-                        hidden, g);
-                if (which != 1)
-                    values8(bytes8(q + up, c, hidden),
-                            scale_at(saved.scale, saved.stype, si + up / kQ8Block), saved.fmt, c, hidden,
-                            u);
-                if (which != 2) load8(dh + int64_t(rr) * ldh, c, hidden, vec, d);
+    for (int r = 0; r < kRows; ++r) {
+        const int rr = r0 + kRows * rg + r;
+        if (rr < saved.rows && c0 < hidden) {
+            const uint8_t *q = saved.data + int64_t(rr) * saved.ld;
+            const int64_t si = int64_t(rr) * saved.sld + tc;
+            float g[8], u[8], d[8];
+            values8(bytes8(q, c, hidden), scale_at(saved.scale, saved.stype, si), saved.fmt, c, hidden, g);
+            values8(bytes8(q + up, c, hidden), scale_at(saved.scale, saved.stype, si + up / kQ8Block), saved.fmt,
+                    c, hidden, u);
+            load8(dh + int64_t(rr) * ldh, c, hidden, vec, d);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float s = sigmoid(g[k]);
-                    if (which == 0) v[r][k] = d[k] * u[k] * (s * (1.f + g[k] * (1.f - s)));
-                    else if (which == 1) v[r][k] = d[k] * (g[k] * s);
-                    else v[r][k] = g[k] * s * u[k];
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) v[r][k] = 0.f;
+            for (int k = 0; k < 8; ++k) {
+                const float s = sigmoid(g[k]), silu = g[k] * s;
+                dg[r][k] = d[k] * u[k] * (s * (1.f + g[k] * (1.f - s)));
+                du[r][k] = d[k] * silu;
+                h[r][k] = silu * u[k];
             }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dg[r][k] = du[r][k] = h[r][k] = 0.f;
         }
-    };
-    float v[8][8];
+    }
     if (dgu.data || dgu_t.data) {
-        part(0, v);
         // the gate's columns end at `up` here, zeros from `hidden` on
         Q8View a = dgu, b = dgu_t;
         a.cols = up;
         b.rows = up;
-        emit_tile(v, a, b, r0, c0, c0, lds);
-        if (c0 < hidden) {
-            part(1, v);
-            emit_tile(v, dgu, dgu_t, r0, up + c0, up + c0, lds);
-        }
+        emit_tile(dg, a, b, r0, c0, c0, lds);
+        if (c0 < hidden) emit_tile(du, dgu, dgu_t, r0, up + c0, up + c0, lds);
     }
     if (h_t.data && c0 < hidden) {
-        part(2, v);
-        emit_tile(v, none, h_t, r0, c0, c0, lds);
+        Q8View none = h_t;
+        none.data = nullptr;
+        emit_tile(h, none, h_t, r0, c0, c0, lds);
     }
 }
 
@@ -453,7 +472,7 @@ int ds_q8_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t 
     if ((rc = tile_grid(rows, cols, &grid)) != DS_OK) return rc;
     return by_type(type, [&](auto *t) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(t)>>;
-        q8_tile<T><<<grid, 256, 0, stream>>>(static_cast<const T *>(x), ldx, vec, int(rows), int(cols),
+        q8_tile<T><<<grid, kTileThreads, 0, stream>>>(static_cast<const T *>(x), ldx, vec, int(rows), int(cols),
                                              int(q8_up(cols)), vr, vc);
     });
 }
@@ -501,7 +520,7 @@ int ds_swiglu8_grad(const ds_q8 *saved, const void *dh, int type, int64_t hidden
     const int vec = rows16(dh, type, ldh);
     return by_type(type, [&](auto *t) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(t)>>;
-        swiglu8_grad_tile<T><<<grid, 256, 0, stream>>>(vs, static_cast<const T *>(dh), ldh, vec,
+        swiglu8_grad_tile<T><<<grid, kTileThreads, 0, stream>>>(vs, static_cast<const T *>(dh), ldh, vec,
                                                        int(hidden), int(up), int(up / kQ8Block), vd, vt, vh);
     });
 }

@@ -94,11 +94,11 @@ constexpr int kFewWaves = 8;
 
 // Up to 16 rows of A: the weight passes once from memory to registers, in the layout of the
 // matrix instructions, and bounds the time.  A workgroup has 16 NT columns; each of its waves
-// takes a run of the reduction's steps, 4 / NT at a time in flight, and their sums meet in LDS.
+// takes a run of the reduction's steps, two at a time in flight, and their sums meet in LDS.
 // SQ: B's scales are of squares, one for the workgroup's columns.
 template <int NT, bool SQ, int FA, int FB>
 __global__ __launch_bounds__(64 * kFewWaves) void q8_few(Q8MatArgs a) {
-    constexpr int U = 4 / NT, SB = SQ ? 1 : 4 * NT;
+    constexpr int U = 2, SB = SQ ? 1 : 4 * NT;
     __shared__ float red[kFewWaves * 256];
     const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4, nw = blockDim.x >> 6;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -147,6 +147,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void q8_few(Q8MatArgs a) {
                 for (int j = 0; j < NT; ++j) vb[u][j] = whole32(pb[j] + k);
                 va[u] = whole32(pa + k);
             }
+            // every load is under way before the first value is used: the compiler would wait for the
+            // scales first (16x16384x8192 with 1x128 scales 43 -> 33 us)
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int u = 0; u < U; ++u) add(va[u], vb[u], s[h + u], [&](int i) { return t[i][h + u]; });
         }
