@@ -570,7 +570,7 @@ enum {
 };
 
 enum {
-    DS_SCALE_POW2 = 0,       /* one byte b: 2^(b - 127), 255 is NaN (OCP e8m0) */
+    DS_SCALE_POW2 = 0,       /* one byte b, 0 to 254: 2^(b - 127) (OCP e8m0) */
     DS_SCALE_F32 = 1
 };
 

@@ -1,6 +1,8 @@
 // Quantization to 8 bits in blocks of 128, and the gated unit with its activations kept
 // in 8 bits.  Both move memory and little else: every input is read once and every
 // output, transposes too, written once by the same launch.
+#include <type_traits>
+
 #include "q8.h"
 
 namespace ds {
@@ -54,29 +56,58 @@ int plain_check(const void *p, int type, int64_t rows, int64_t cols, int64_t ld,
 
 namespace {
 
-// Loads eight elements of a row of `cols` as fp32, 0 past its end; vec: rows are 16-byte aligned.
+// FULL, here and below: the caller has seen that all rows and columns exist and that rows of plain
+// matrices are 16-byte aligned.
+
+// Eight elements of a row of `cols`, 0 past its end; vec: rows are 16-byte aligned.
 template <typename T>
-__device__ __forceinline__ void load8(const T *row, int c, int cols, bool vec, float (&v)[8]) {
-    if (vec && c + 8 <= cols) {
-        T t[8];
+struct Eight {
+    T t[8];
+    // as loaded: a use after this is not one of values the compiler has already
+    __device__ __forceinline__ void forget() {
+        intx4 *p = reinterpret_cast<intx4 *>(t);
 #pragma unroll
-        for (size_t i = 0; i < sizeof(t) / 16; ++i)
-            reinterpret_cast<intx4 *>(t)[i] = reinterpret_cast<const intx4 *>(row + c)[i];
+        for (size_t i = 0; i < sizeof(t) / 16; ++i) {
+            intx4 w = p[i];
+            __asm__ volatile("" : "+v"(w));
+            p[i] = w;
+        }
+    }
+};
+template <bool FULL, typename T>
+__device__ __forceinline__ Eight<T> raw8(const T *row, int c, int cols, bool vec) {
+    Eight<T> e;
+    if (FULL || (vec && c + 8 <= cols)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = float(t[i]);
+        for (size_t i = 0; i < sizeof(e) / 16; ++i)
+            reinterpret_cast<intx4 *>(e.t)[i] = reinterpret_cast<const intx4 *>(row + c)[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? float(row[c + i]) : 0.f;
+        for (int i = 0; i < 8; ++i) e.t[i] = c + i < cols ? row[c + i] : T(0.f);
     }
+    return e;
+}
+template <bool FULL, typename T>
+__device__ __forceinline__ void load8(const T *row, int c, int cols, bool vec, float (&v)[8]) {
+    const Eight<T> e = raw8<FULL>(row, c, cols, vec);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = float(e.t[i]);
 }
 
-// The largest magnitude of the values as bits, NaN and infinities above all.
+// The bits of the largest magnitude, kInf or more where some value is not finite: the largest as
+// signed numbers is the largest positive one, as unsigned the most negative one if there is any
+// (one instruction for two values each, where taking signs off first would cost one a value).
+constexpr unsigned kInf = 0x7f800000u;
 template <int N>
 __device__ __forceinline__ unsigned max_bits(const float (&v)[N]) {
-    unsigned m = 0;
+    int pos = 0;
+    unsigned neg = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
-    return m;
+    for (int i = 0; i < N; i += 2) {
+        pos = max(max(pos, __float_as_int(v[i])), __float_as_int(v[i + 1]));
+        neg = max(max(neg, __float_as_uint(v[i])), __float_as_uint(v[i + 1]));
+    }
+    return max(unsigned(pos), neg & 0x7fffffffu);
 }
 // The same of the finite ones.
 template <int N>
@@ -87,14 +118,10 @@ __device__ __forceinline__ unsigned max_finite(const float (&v)[N]) {
     return m;
 }
 
-__device__ __forceinline__ intx2 pack8(const float (&v)[8], float inv, int fmt) {
-    return intx2{pack4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv, fmt),
-                 pack4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv, fmt)};
-}
-
 // Eight bytes to columns c .. of a row that ends at `cols`.
+template <bool FULL>
 __device__ __forceinline__ void store8(uint8_t *row, int c, int cols, intx2 q) {
-    if (c + 8 <= cols) {
+    if (FULL || c + 8 <= cols) {
         *reinterpret_cast<intx2 *>(row + c) = q;
     } else {
 #pragma unroll
@@ -103,14 +130,28 @@ __device__ __forceinline__ void store8(uint8_t *row, int c, int cols, intx2 q) {
     }
 }
 
+template <int FMT, bool FULL>
+__device__ __forceinline__ void store_values(uint8_t *row, int c, int cols, const float (&v)[8], float inv) {
+    store8<FULL>(row, c, cols, intx2{pack4<FMT>(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                                     pack4<FMT>(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)});
+}
+
 // One 1x128 block of row r at columns c0 .. c0+127, held by 16 lanes of eight values each.
+template <int FMT, bool FULL>
 __device__ __forceinline__ void emit_block(const Q8View &m, int r, int blk, int cl, const float (&v)[8]) {
-    unsigned top = max16(max_bits(v));
+    unsigned top = max_bits(v);
     // what is not finite sets no scale: only a wave that holds some looks at each value
-    if (__any(top >= 0x7f800000u)) top = max16(max_finite(v));
-    const BlockScale s = block_scale(top, m.fmt, m.stype);
-    store8(m.data + int64_t(r) * m.ld, blk * kQ8Block + 8 * cl, m.cols, pack8(v, s.inv, m.fmt));
+    if (__any(top >= kInf)) top = max_finite(v);
+    const BlockScale s = block_scale(max16(top), FMT, m.stype);
+    store_values<FMT, FULL>(m.data + int64_t(r) * m.ld, blk * kQ8Block + 8 * cl, m.cols, v, s.inv);
     if (cl == 0) store_scale(m, int64_t(r) * m.sld + blk, s.bits);
+}
+
+// Calls fn with the format as a constant.
+template <typename Fn>
+__device__ __forceinline__ void by_fmt(int fmt, Fn fn) {
+    if (fmt == DS_Q8_E4M3) fn(std::integral_constant<int, DS_Q8_E4M3>{});
+    else fn(std::integral_constant<int, DS_Q8_E5M2>{});
 }
 
 // Rows alone: 16 lanes a block.
@@ -122,8 +163,8 @@ __global__ __launch_bounds__(256) void q8_rows(const T *x, int64_t ldx, int vec,
     for (int64_t i = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4); i < total; i += step) {
         const int r = int(i / nb), b = int(i - int64_t(r) * nb);
         float v[8];
-        load8(x + int64_t(r) * ldx, b * kQ8Block + 8 * cl, m.cols, vec, v);
-        emit_block(m, r, b, cl, v);
+        load8<false>(x + int64_t(r) * ldx, b * kQ8Block + 8 * cl, m.cols, vec, v);
+        by_fmt(m.fmt, [&](auto f) { emit_block<f.value, false>(m, r, b, cl, v); });
     }
 }
 
@@ -133,31 +174,43 @@ constexpr int kTileThreads = 512, kRows = 4, kTileWaves = kTileThreads / 64;
 
 struct TileLds {
     unsigned colmax[kTileWaves][128];
-    BlockScale cs[128];
+    float inv[128];
     // transposed bytes: column c's 16 rows of wave w are the 16 bytes at c * 8 + (w ^ c / 8 % 8), so
     // that the 16 columns a wave writes at once lie in different banks
     intx4 t[128 * 8];
 };
 
-// Largest over the wave's 16 rows of column 8 (lane % 16) + c, for each c.
+// Largest over the wave's 16 rows of lanes' column, in all four rows of 16 lanes.
 __device__ __forceinline__ unsigned over_rows(unsigned m) {
-    m = max(m, unsigned(__shfl_xor(int(m), 16)));
-    return max(m, unsigned(__shfl_xor(int(m), 32)));
+    typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
+    const uintx2 a = __builtin_amdgcn_permlane16_swap(m, m, false, false);   // rows 0 0 2 2 and 1 1 3 3
+    m = max(a[0], a[1]);
+    const uintx2 b = __builtin_amdgcn_permlane32_swap(m, m, false, false);   // halves 0 0 and 1 1
+    return max(b[0], b[1]);
 }
 
-// Writes a tile's values to `row` at (r0, c0) and transposed to `col` at (rc0, r0); either has
-// data == null when not wanted.  Elements outside the matrices hold 0.
-__device__ __forceinline__ void emit_tile(const float (&v)[kRows][8], const Q8View &row, const Q8View &col,
-                                          int r0, int c0, int rc0, TileLds &lds) {
-    const int tid = threadIdx.x, cl = tid & 15, rg = tid >> 4, w = tid >> 6;
-    const bool square = (row.data ? row.shift : col.shift) != 0;
-    if (row.data && !square)
+// One tile and where it goes: to `row` at (r0, c0) and transposed to `col` at (rc0, r0); either has
+// data == null when not wanted.
+struct TileOut {
+    Q8View row, col;
+    int c0, rc0;
+};
+
+template <bool FULL>
+__device__ __forceinline__ void emit_rows(const float (&v)[kRows][8], const TileOut &o, int r0) {
+    const int cl = threadIdx.x & 15, rg = threadIdx.x >> 4;
+    by_fmt(o.row.fmt, [&](auto f) {
 #pragma unroll
         for (int r = 0; r < kRows; ++r) {
             const int rr = r0 + kRows * rg + r;
-            if (rr < row.rows) emit_block(row, rr, c0 >> 7, cl, v[r]);
+            if (FULL || rr < o.row.rows) emit_block<f.value, FULL>(o.row, rr, o.c0 >> 7, cl, v[r]);
         }
-    if (!col.data && !square) return;
+    });
+}
+
+// The thread's largest magnitudes of its eight columns, then the wave's to `lds`.
+__device__ __forceinline__ void column_max(const float (&v)[kRows][8], unsigned (*lds)[128]) {
+    const int tid = threadIdx.x;
     unsigned m[8], any = 0;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
@@ -165,7 +218,7 @@ __device__ __forceinline__ void emit_tile(const float (&v)[kRows][8], const Q8Vi
         m[c] = max_bits(u);
         any = max(any, m[c]);
     }
-    if (__any(any >= 0x7f800000u))
+    if (__any(any >= kInf))
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
             const float u[kRows] = {v[0][c], v[1][c], v[2][c], v[3][c]};
@@ -174,89 +227,130 @@ __device__ __forceinline__ void emit_tile(const float (&v)[kRows][8], const Q8Vi
 #pragma unroll
     for (int c = 0; c < 8; ++c) m[c] = over_rows(m[c]);
     if ((tid & 48) == 0) {
-        unsigned *p = lds.colmax[w] + 8 * cl;
-        reinterpret_cast<intx4 *>(p)[0] = intx4{int(m[0]), int(m[1]), int(m[2]), int(m[3])};
-        reinterpret_cast<intx4 *>(p)[1] = intx4{int(m[4]), int(m[5]), int(m[6]), int(m[7])};
+        intx4 *p = reinterpret_cast<intx4 *>(lds[tid >> 6] + 8 * (tid & 15));
+        p[0] = intx4{int(m[0]), int(m[1]), int(m[2]), int(m[3])};
+        p[1] = intx4{int(m[4]), int(m[5]), int(m[6]), int(m[7])};
     }
-    __syncthreads();
-    unsigned all = 0;
-    if (square) {
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-            for (int i = 0; i < kTileWaves; ++i) all = max(all, lds.colmax[i][8 * cl + c]);
-        all = max16(all);
-        if (row.data) {
-            const BlockScale s = block_scale(all, row.fmt, row.stype);
-            if (tid == 0) store_scale(row, int64_t(r0 >> 7) * row.sld + (c0 >> 7), s.bits);
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                const int rr = r0 + kRows * rg + r;
-                if (rr < row.rows)
-                    store8(row.data + int64_t(rr) * row.ld, c0 + 8 * cl, row.cols, pack8(v[r], s.inv, row.fmt));
-            }
-        }
-        if (!col.data) return;
-        if (tid == 0) {
-            const BlockScale s = block_scale(all, col.fmt, col.stype);
-            store_scale(col, int64_t(rc0 >> 7) * col.sld + (r0 >> 7), s.bits);
-        }
-    }
-    if (tid < 128) {
-        unsigned top = all;
-        if (!square)
-#pragma unroll
-            for (int i = 0; i < kTileWaves; ++i) top = max(top, lds.colmax[i][tid]);
-        const BlockScale s = block_scale(top, col.fmt, col.stype);
-        lds.cs[tid] = s;
-        if (!square && rc0 + tid < col.rows)
-            store_scale(col, int64_t(rc0 + tid) * col.sld + (r0 >> 7), s.bits);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        const int cc = 8 * cl + c;
-        const float inv = lds.cs[cc].inv;
-        reinterpret_cast<int *>(lds.t)[(cc * 8 + (w ^ (cl & 7))) * 4 + (rg & 3)] =
-            pack4(v[0][c] * inv, v[1][c] * inv, v[2][c] * inv, v[3][c] * inv, col.fmt);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int i = j * kTileThreads + tid, c = i >> 3, g = i & 7, at = r0 + 16 * g;
-        if (rc0 + c < col.rows && at < col.cols) {
-            uint8_t *p = col.data + int64_t(rc0 + c) * col.ld;
-            const intx4 q = lds.t[c * 8 + (g ^ (c >> 3 & 7))];
-            if (at + 16 <= col.cols) {
-                *reinterpret_cast<intx4 *>(p + at) = q;
-            } else {
-                store8(p, at, col.cols, intx2{q[0], q[1]});
-                store8(p, at + 8, col.cols, intx2{q[2], q[3]});
-            }
-        }
-    }
-    // the next tile's first writes here come after a barrier that follows these reads
 }
 
-template <typename T>
-__global__ __launch_bounds__(kTileThreads) void q8_tile(const T *x, int64_t ldx, int vec, int rows, int cols,
-                                                        int tiles_c, Q8View row, Q8View col) {
-    __shared__ TileLds lds;
+// The columns' scales, once the waves' column_max are in.
+__device__ __forceinline__ void column_scales(const TileOut &o, int r0, TileLds &lds) {
+    const int c = threadIdx.x;
+    if (c >= 128) return;
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < kTileWaves; ++i) top = max(top, lds.colmax[i][c]);
+    const BlockScale s = block_scale(top, o.col.fmt, o.col.stype);
+    lds.inv[c] = s.inv;
+    if (o.rc0 + c < o.col.rows) store_scale(o.col, int64_t(o.rc0 + c) * o.col.sld + (r0 >> 7), s.bits);
+}
+
+// The tile's columns times inv, as bytes to `t`; inv the same for all where `one` is not 0.
+__device__ __forceinline__ void transpose_in(const float (&v)[kRows][8], const float *inv, float one, int fmt,
+                                             intx4 *t) {
+    const int cl = threadIdx.x & 15, rg = threadIdx.x >> 4, w = threadIdx.x >> 6;
+    by_fmt(fmt, [&](auto f) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const int cc = 8 * cl + c;
+            const float s = one != 0.f ? one : inv[cc];
+            reinterpret_cast<int *>(t)[(cc * 8 + (w ^ (cl & 7))) * 4 + (rg & 3)] =
+                pack4<f.value>(v[0][c] * s, v[1][c] * s, v[2][c] * s, v[3][c] * s);
+        }
+    });
+}
+
+template <bool FULL>
+__device__ __forceinline__ void transpose_out(const TileOut &o, int r0, const intx4 *t) {
+#pragma unroll
+    for (int j = 0; j < 1024 / kTileThreads; ++j) {
+        const int i = j * kTileThreads + threadIdx.x, c = i >> 3, g = i & 7, at = r0 + 16 * g;
+        if (!FULL && (o.rc0 + c >= o.col.rows || at >= o.col.cols)) continue;
+        uint8_t *p = o.col.data + int64_t(o.rc0 + c) * o.col.ld;
+        const intx4 q = t[c * 8 + (g ^ (c >> 3 & 7))];
+        if (FULL || at + 16 <= o.col.cols) {
+            *reinterpret_cast<intx4 *>(p + at) = q;
+        } else {
+            store8<false>(p, at, o.col.cols, intx2{q[0], q[1]});
+            store8<false>(p, at + 8, o.col.cols, intx2{q[2], q[3]});
+        }
+    }
+}
+
+// Column by column: a tile's transpose.  The LDS is free again after a barrier that follows.
+template <bool FULL>
+__device__ __forceinline__ void emit_columns(const float (&v)[kRows][8], const TileOut &o, int r0, TileLds &lds) {
+    column_max(v, lds.colmax);
+    __syncthreads();
+    column_scales(o, r0, lds);
+    __syncthreads();
+    transpose_in(v, lds.inv, 0.f, o.col.fmt, lds.t);
+    __syncthreads();
+    transpose_out<FULL>(o, r0, lds.t);
+}
+
+template <bool FULL, typename T>
+__device__ __forceinline__ void tile_body(const T *x, int64_t ldx, int vec, int rows, int cols, int tr, int tc,
+                                          const Q8View &row, const Q8View &col, TileLds &lds) {
     const int cl = threadIdx.x & 15, rg = threadIdx.x >> 4;
-    const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
     const int r0 = tr * 128, c0 = tc * 128;
+    const TileOut o = {row, col, c0, c0};
     float v[kRows][8];
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
         const int rr = r0 + kRows * rg + r;
-        if (rr < rows) {
-            load8(x + int64_t(rr) * ldx, c0 + 8 * cl, cols, vec, v[r]);
+        if (FULL || rr < rows) {
+            load8<FULL>(x + int64_t(rr) * ldx, c0 + 8 * cl, cols, vec, v[r]);
         } else {
 #pragma unroll
             for (int c = 0; c < 8; ++c) v[r][c] = 0.f;
         }
     }
-    emit_tile(v, row, col, r0, c0, c0, lds);
+    if (!(row.data ? row.shift : col.shift)) {
+        if (row.data) emit_rows<FULL>(v, o, r0);
+        if (!col.data) return;
+        emit_columns<FULL>(v, o, r0, lds);
+        return;
+    }
+    // one scale for the square
+    column_max(v, lds.colmax);
+    __syncthreads();
+    unsigned all = 0;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+#pragma unroll
+        for (int i = 0; i < kTileWaves; ++i) all = max(all, lds.colmax[i][8 * cl + c]);
+    all = max16(all);
+    if (row.data) {
+        const BlockScale s = block_scale(all, row.fmt, row.stype);
+        if (threadIdx.x == 0) store_scale(row, int64_t(tr) * row.sld + tc, s.bits);
+        by_fmt(row.fmt, [&](auto f) {
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const int rr = r0 + kRows * rg + r;
+                if (FULL || rr < row.rows)
+                    store_values<f.value, FULL>(row.data + int64_t(rr) * row.ld, c0 + 8 * cl, row.cols, v[r], s.inv);
+            }
+        });
+    }
+    if (!col.data) return;
+    const BlockScale s = block_scale(all, col.fmt, col.stype);
+    if (threadIdx.x == 0) store_scale(col, int64_t(tc) * col.sld + tr, s.bits);
+    transpose_in(v, nullptr, s.inv, col.fmt, lds.t);
+    __syncthreads();
+    transpose_out<FULL>(o, r0, lds.t);
+}
+
+// (six waves a SIMD unit hide the memory's latency: 117 us for 16384x8192 both ways, 125 with five)
+template <typename T>
+__global__ __launch_bounds__(kTileThreads, 6) void q8_tile(const T *x, int64_t ldx, int vec, int rows, int cols,
+                                                           int tiles_c, Q8View row, Q8View col) {
+    __shared__ TileLds lds;
+    const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
+    if (vec && tr * 128 + 128 <= rows && tc * 128 + 128 <= cols)
+        tile_body<true>(x, ldx, vec, rows, cols, tr, tc, row, col, lds);
+    else
+        tile_body<false>(x, ldx, vec, rows, cols, tr, tc, row, col, lds);
 }
 
 // ---- gated unit -----------------------------------------------------------------
@@ -271,10 +365,9 @@ __device__ __forceinline__ float sigmoid(float g) {
     float e = __builtin_amdgcn_exp2f(hi);
     // e * 2^lo; where e is 0 or infinite the result is 1 or 0 whatever lo says
     e = fabsf(hi) < 127.9f ? fmaf(e, lo * 0.693147181f, e) : e;
-    const float d = 1.f + e;
+    const float d = 1.f + fminf(e, 3e38f);                 // finite, as the step wants it
     const float r = __builtin_amdgcn_rcpf(d);
-    const float n = fmaf(fmaf(-d, r, 1.f), r, r);
-    return d < 1e38f ? n : r;                              // infinite d: r is 0 already
+    return fmaf(fmaf(-d, r, 1.f), r, r);
 }
 
 template <typename T>
@@ -287,21 +380,22 @@ __global__ __launch_bounds__(256) void swiglu8_rows(const T *gu, int64_t ldg, in
         const T *p = gu + int64_t(r) * ldg;
         const int c = b * kQ8Block + 8 * cl;
         float g[8], u[8], v[8];
-        load8(p, c, hidden, vec, g);
-        load8(p + up, c, hidden, vec, u);
+        load8<false>(p, c, hidden, vec, g);
+        load8<false>(p + up, c, hidden, vec, u);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = g[k] * sigmoid(g[k]) * u[k];
         const bool in = b * kQ8Block < hidden;             // not a block between the two
-        if (in) emit_block(h, r, b, cl, v);
-        if (saved.data) {
-            emit_block(saved, r, b, cl, g);
-            if (in) emit_block(saved, r, b + up / kQ8Block, cl, u);
-        }
+        if (in) by_fmt(h.fmt, [&](auto f) { emit_block<f.value, false>(h, r, b, cl, v); });
+        if (saved.data)
+            by_fmt(saved.fmt, [&](auto f) {
+                emit_block<f.value, false>(saved, r, b, cl, g);
+                if (in) emit_block<f.value, false>(saved, r, b + up / kQ8Block, cl, u);
+            });
     }
 }
 
-// Eight 8-bit values times their scale; columns from `cols` on are 0.
-__device__ __forceinline__ void values8(intx2 q, float s, int fmt, int c, int cols, float (&v)[8]) {
+// Eight 8-bit values times their scale.
+__device__ __forceinline__ void values8(intx2 q, float s, int fmt, float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         typedef float f2 __attribute__((ext_vector_type(2)));
@@ -318,13 +412,12 @@ __device__ __forceinline__ void values8(intx2 q, float s, int fmt, int c, int co
         v[4 * i + 2] = b[0] * s;
         v[4 * i + 3] = b[1] * s;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? v[i] : 0.f;
 }
 
 // Eight bytes of a row that ends at `cols`, 0 past it.
+template <bool FULL>
 __device__ __forceinline__ intx2 bytes8(const uint8_t *row, int c, int cols) {
-    if (c + 8 <= cols) return *reinterpret_cast<const intx2 *>(row + c);
+    if (FULL || c + 8 <= cols) return *reinterpret_cast<const intx2 *>(row + c);
     intx2 q = {0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -332,51 +425,95 @@ __device__ __forceinline__ intx2 bytes8(const uint8_t *row, int c, int cols) {
     return q;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kTileThreads, 4) void swiglu8_grad_tile(Q8View saved, const T *dh, int64_t ldh,
-                                                                  int vec, int hidden, int up, int tiles_c,
-                                                                  Q8View dgu, Q8View dgu_t, Q8View h_t) {
-    __shared__ TileLds lds;
+template <bool FULL, typename T>
+__device__ __forceinline__ void grad_body(const Q8View &saved, const T *dh, int64_t ldh, int vec, int hidden,
+                                          int up, int tr, int tc, const Q8View &dgu, const Q8View &dgu_t,
+                                          const Q8View &h_t, TileLds &lds) {
     const int cl = threadIdx.x & 15, rg = threadIdx.x >> 4;
-    const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
     const int r0 = tr * 128, c0 = tc * 128, c = c0 + 8 * cl;
-    float dg[kRows][8], du[kRows][8], h[kRows][8];
-#pragma unroll
-    for (int r = 0; r < kRows; ++r) {
-        const int rr = r0 + kRows * rg + r;
-        if (rr < saved.rows && c0 < hidden) {
+    // The gate's columns end at `up` here, zeros from `hidden` on; a tile past `hidden` has those alone.
+    const bool in = FULL || c0 < hidden;
+    TileOut o[3] = {{dgu, dgu_t, c0, c0}, {dgu, dgu_t, up + c0, up + c0}, {Q8View{}, h_t, c0, c0}};
+    o[0].row.cols = up;
+    o[0].col.rows = up;
+    if (!in) o[1].row.data = o[1].col.data = o[2].col.data = nullptr;
+
+    struct Raw {
+        intx2 g, u;
+        float sg, su;
+        Eight<T> d;
+    };
+    auto fetch = [&](int rr) {
+        Raw x{};
+        if (FULL || (in && rr < saved.rows)) {
             const uint8_t *q = saved.data + int64_t(rr) * saved.ld;
             const int64_t si = int64_t(rr) * saved.sld + tc;
-            float g[8], u[8], d[8];
-            values8(bytes8(q, c, hidden), scale_at(saved.scale, saved.stype, si), saved.fmt, c, hidden, g);
-            values8(bytes8(q + up, c, hidden), scale_at(saved.scale, saved.stype, si + up / kQ8Block), saved.fmt,
-                    c, hidden, u);
-            load8(dh + int64_t(rr) * ldh, c, hidden, vec, d);
+            x.g = bytes8<FULL>(q, c, hidden);
+            x.u = bytes8<FULL>(q + up, c, hidden);
+            x.sg = scale_at(saved.scale, saved.stype, si);
+            x.su = scale_at(saved.scale, saved.stype, si + up / kQ8Block);
+            x.d = raw8<FULL>(dh + int64_t(rr) * ldh, c, hidden, vec);
+        }
+        return x;
+    };
+    Raw x[kRows];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float s = sigmoid(g[k]), silu = g[k] * s;
-                dg[r][k] = d[k] * u[k] * (s * (1.f + g[k] * (1.f - s)));
-                du[r][k] = d[k] * silu;
-                h[r][k] = silu * u[k];
-            }
-        } else {
+    for (int r = 0; r < kRows; ++r) x[r] = fetch(r0 + kRows * rg + r);
+    // One output after another, with silu(g) and the loaded bytes held: all three at once do not fit
+    // the registers of two workgroups a CU.
+    float silu[kRows][8], v[kRows][8];
+    auto emit = [&](int n) {
+        if (o[n].row.data) emit_rows<FULL>(v, o[n], r0);
+        // (the tile before is read out of LDS before the first of these barriers and written after)
+        if (o[n].col.data) emit_columns<FULL>(v, o[n], r0, lds);
+    };
 #pragma unroll
-            for (int k = 0; k < 8; ++k) dg[r][k] = du[r][k] = h[r][k] = 0.f;
+    for (int r = 0; r < kRows; ++r) {
+        float g[8], u[8];
+        values8(x[r].g, x[r].sg, saved.fmt, g);
+        values8(x[r].u, x[r].su, saved.fmt, u);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float s = sigmoid(g[k]);
+            silu[r][k] = g[k] * s;
+            v[r][k] = float(x[r].d.t[k]) * u[k] * (s * (1.f + g[k] * (1.f - s)));
         }
     }
-    if (dgu.data || dgu_t.data) {
-        // the gate's columns end at `up` here, zeros from `hidden` on
-        Q8View a = dgu, b = dgu_t;
-        a.cols = up;
-        b.rows = up;
-        emit_tile(dg, a, b, r0, c0, c0, lds);
-        if (c0 < hidden) emit_tile(du, dgu, dgu_t, r0, up + c0, up + c0, lds);
+    emit(0);
+    // (decoded again below: kept, the decoded values would not fit)
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        x[r].d.forget();
+        __asm__ volatile("" : "+v"(x[r].u));
     }
-    if (h_t.data && c0 < hidden) {
-        Q8View none = h_t;
-        none.data = nullptr;
-        emit_tile(h, none, h_t, r0, c0, c0, lds);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[r][k] = float(x[r].d.t[k]) * silu[r][k];
+    emit(1);
+    if (!o[2].col.data) return;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        float u[8];
+        values8(x[r].u, x[r].su, saved.fmt, u);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[r][k] = silu[r][k] * u[k];
     }
+    emit(2);
+}
+
+// 8192x8192, bf16 dh: 229 us with two workgroups a CU and what that leaves out of registers, 263 with
+// one; fp32 dh, whose loaded rows take twice the registers, 281 and 237.
+template <typename T>
+__global__ __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 3 : 4) void swiglu8_grad_tile(Q8View saved, const T *dh, int64_t ldh,
+                                                                     int vec, int hidden, int up, int tiles_c,
+                                                                     Q8View dgu, Q8View dgu_t, Q8View h_t) {
+    __shared__ TileLds lds;
+    const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
+    if (vec && tr * 128 + 128 <= saved.rows && tc * 128 + 128 <= hidden)
+        grad_body<true>(saved, dh, ldh, vec, hidden, up, tr, tc, dgu, dgu_t, h_t, lds);
+    else
+        grad_body<false>(saved, dh, ldh, vec, hidden, up, tr, tc, dgu, dgu_t, h_t, lds);
 }
 
 bool rows16(const void *p, int type, int64_t ld) {

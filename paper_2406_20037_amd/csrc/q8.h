@@ -48,8 +48,7 @@ inline Q8View q8_view(const ds_q8 *m) {
 __device__ __forceinline__ float scale_at(const void *s, int stype, int64_t i) {
     if (stype == DS_SCALE_F32) return static_cast<const float *>(s)[i];
     const unsigned b = static_cast<const uint8_t *>(s)[i];
-    // 2^-127 is the subnormal 0x00400000; 255 is NaN
-    return __uint_as_float(b == 0 ? 0x400000u : b == 255 ? 0x7fc00000u : b << 23);
+    return __uint_as_float(max(b << 23, 0x400000u));   // 2^-127 is the subnormal 0x00400000
 }
 
 struct BlockScale {
@@ -82,14 +81,17 @@ __device__ __forceinline__ unsigned finite_abs(float v) {
 }
 
 // Four values to 8 bits, nearest even, first in the low byte.
-__device__ __forceinline__ int pack4(float a, float b, float c, float d, int fmt) {
+template <int FMT>
+__device__ __forceinline__ int pack4(float a, float b, float c, float d) {
     int r;
-    if (fmt == DS_Q8_E4M3) {
-        r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    __asm__("" : "=v"(r));                       // both halves are written: no need to clear it
+    if constexpr (FMT == DS_Q8_E4M3) {
+        r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, r, false);
         return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+    } else {
+        r = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, r, false);
+        return __builtin_amdgcn_cvt_pk_bf8_f32(c, d, r, true);
     }
-    r = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, 0, false);
-    return __builtin_amdgcn_cvt_pk_bf8_f32(c, d, r, true);
 }
 
 // Eight 8-bit values as bf16, exactly (both formats have fewer bits and a narrower range).
