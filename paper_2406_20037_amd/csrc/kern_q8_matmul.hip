@@ -356,6 +356,27 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
         }
     };
 
+    // whether an exponent of the thread's row of the stage is over 167, the byte of 2^40
+    auto scales_past_2_40 = [&]() {
+        static_assert(ROWS <= 256 || MODE != MM_EXACT_POW2, "a row a thread");
+        if (tid >= ROWS) return 0;
+        const bool isa = tid < BM;
+        const Q8View &v = isa ? a.a : a.b;
+        const int row = isa ? min(m0 + tid, a.M - 1) : min(n0 + tid - BM, a.N - 1);
+        const uint8_t *const p = static_cast<const uint8_t *>(v.scale) + int64_t(row >> v.shift) * v.sld;
+        unsigned bad = 0;
+        int k = kt0;
+        if (a.words)
+#pragma unroll 4
+            for (; k + 4 <= kt1; k += 4) {
+                const unsigned w = *reinterpret_cast<const unsigned *>(p + k);
+                bad |= ((w & 0x7f7f7f7fu) + 0x58585858u) & w & 0x80808080u;   // 168 = 128 + 40
+            }
+#pragma unroll 1
+        for (; k < kt1; ++k) bad |= p[k] > 167;
+        return int(bad != 0);
+    };
+
     floatx4 acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -364,14 +385,14 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
     Frag alo[HM], ahi[HM], b0[HN], b1[HN];
     // The present step's scales: of A's rows and of B's columns.  MM_POW2: exponents in the low
     // bytes, xn the words of the step after as read.  Otherwise fp32.
-    constexpr int XN = FM + (MODE == MM_POW2 ? FN : 0);
+    constexpr int XN = FM + (WORDS ? FN : 0);
     int xs[XN], xn[MODE == MM_POW2 ? XN : 1];
     floatx4 sb[MODE == MM_POW2 || SQ ? 1 : FN];
     float sq = 0.f, sqn = 0.f;
     auto scales_of = [&](int u) {
         return reinterpret_cast<const int *>(sbuf + ((u >> 2) & 1) * S::SCALES) + (WORDS ? 0 : (u & 3) * ROWS);
     };
-    auto word_of = [&](const int *sc, int f) {             // MM_POW2: of fragment f, B's after A's
+    auto word_of = [&](const int *sc, int f) {             // of fragment f, B's after A's
         return f < FM ? sc[16 * (FM * wm + f) + li] : sc[BM + 16 * (FN * wn + f - FM) + li];
     };
     // as fp32 bits; sh: the step's byte of the word
@@ -395,20 +416,22 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
 #pragma unroll
         for (int v = 0; v < 4; ++v) acc[i][j][v] = fmaf(p[v], SQ ? w[0] : w[v], acc[i][j][v]);
     };
-    // place of a quarter's q-th product; EXACT: down a column, so that B's fragment is decoded once
+    // place of a quarter's q-th product; EXACT: down a column, so that B's next fragment is decoded late
     auto qi = [](int q) { return EXACT ? q % HM : q / HN; };
     auto qj = [](int q) { return EXACT ? q / HM : q % HN; };
-    bf16x8 da[EXACT ? HM : 1][4], db[4];                   // EXACT: decoded fragments
+    bf16x8 da[EXACT ? HM : 1][4], db[EXACT ? FN : 1][4];   // EXACT: decoded fragments, once a step
     // A quarter of the wave's tile, fragments i0 .. of A by j0 .. of B; beside(q) issues what goes
     // between its products q and q + 1.  wi, wj: the quarter before.
-    auto quarter = [&](const Frag (&fa)[HM], const Frag (&fb)[HN], int i0, int j0, auto beside, int wi, int wj) {
+    auto quarter = [&]<bool FOLD>(std::bool_constant<FOLD>, const Frag (&fa)[HM], const Frag (&fb)[HN], int i0,
+                                  int j0, auto beside, int wi, int wj) {
         if constexpr (EXACT)
             if (j0 == 0)
 #pragma unroll
                 for (int i = 0; i < HM; ++i)
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        da[i][k] = to_bf16<FA>(fa[i].h[k >> 1][2 * (k & 1)], fa[i].h[k >> 1][2 * (k & 1) + 1]);
+                        da[i][k] = to_bf16<FA>(fa[i].h[k >> 1][2 * (k & 1)], fa[i].h[k >> 1][2 * (k & 1) + 1],
+                                               FOLD ? __int_as_float(xs[i0 + i]) : 1.f);
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
             const int i = qi(q), j = qj(q);
@@ -418,33 +441,40 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
             } else {
                 floatx4 p = {0, 0, 0, 0};
                 if constexpr (EXACT) {
-                    if (i == 0)
+                    if (i == 0 && i0 == 0)
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            db[k] = to_bf16<FB>(fb[j].h[k >> 1][2 * (k & 1)], fb[j].h[k >> 1][2 * (k & 1) + 1]);
+                            db[j0 + j][k] = to_bf16<FB>(fb[j].h[k >> 1][2 * (k & 1)],
+                                                        fb[j].h[k >> 1][2 * (k & 1) + 1],
+                                                        FOLD ? __int_as_float(xs[FM + j0 + j]) : 1.f);
+                    if constexpr (FOLD) p = acc[i0 + i][j0 + j];
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(db[k], da[i][k], p, 0, 0, 0);
+                        p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(db[j0 + j][k], da[i][k], p, 0, 0, 0);
                 } else {
                     p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[j], fa[i], p, FB, FA, 0, 0, 0, 0);
                 }
-                const int o = q < D ? NQ - D + q : q - D;  // place of the block that is due
-                add_block((q < D ? wi : i0) + qi(o), (q < D ? wj : j0) + qj(o), wp[0], ws[0]);
-                if constexpr (D == 2) {
-                    wp[0] = wp[D - 1];
-                    ws[0] = ws[D - 1];
+                if constexpr (FOLD) {
+                    acc[i0 + i][j0 + j] = p;
+                } else {
+                    const int o = q < D ? NQ - D + q : q - D;  // place of the block that is due
+                    add_block((q < D ? wi : i0) + qi(o), (q < D ? wj : j0) + qj(o), wp[0], ws[0]);
+                    if constexpr (D == 2) {
+                        wp[0] = wp[D - 1];
+                        ws[0] = ws[D - 1];
+                    }
+                    wp[D - 1] = p;
+                    const float x = __int_as_float(xs[i0 + i]);
+                    if constexpr (SQ) ws[D - 1][0] = x * sq;
+                    else ws[D - 1] = x * sb[j0 + j];
                 }
-                wp[D - 1] = p;
-                const float x = __int_as_float(xs[i0 + i]);
-                if constexpr (SQ) ws[D - 1][0] = x * sq;
-                else ws[D - 1] = x * sb[j0 + j];
             }
             beside(q);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
     // step kt, whose first fragments are in alo and b0; COPY: the whole of step kt + 2 is copied
-    auto step = [&]<bool COPY>(std::bool_constant<COPY>, int kt) {
+    auto step = [&]<bool COPY, bool FOLD>(std::bool_constant<COPY>, std::bool_constant<FOLD> fold, int kt) {
         const int u = kt - kt0;
         const unsigned cur = (u & 1) * STAGE, nxt = STAGE - cur;
         if ((u & 3) == 0) copy_scales(kt + 4, ((u >> 2) & 1) ^ 1);
@@ -467,50 +497,90 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
         const int *const sc = scales_of(u), *const scn = scales_of(u + 1);
         const int sh = 8 * (u & 3), shn = 8 * ((u + 1) & 3);
         // Each half of the fragments and scales is replaced once its last product is issued
-        quarter(alo, b0, 0, 0, [&](int q) {
+        quarter(fold, alo, b0, 0, 0, [&](int q) {
             spread(q, 2 * HN, [&](int r) { b1[r >> 1].h[r & 1] = half(cur, fb0, HN + (r >> 1), r & 1); });
             if constexpr (COPY) spread(q, PART, [&](int r) { copy1(da, db, cur, part_copy(r, 0)); });
             if constexpr (MODE == MM_POW2) {
                 spread(q, HM, [&](int f) { xs[HM + f] = int(unsigned(xn[HM + f]) >> sh); });
                 spread(q, HN, [&](int f) { xs[FM + HN + f] = int(unsigned(xn[FM + HN + f]) >> sh); });
             } else {
-                if constexpr (!SQ) spread(q, HN, [&](int f) { sb[HN + f] = scale_of_b(sc, HN + f, sh); });
+                if constexpr (FOLD) spread(q, HN, [&](int f) { xs[FM + HN + f] = value(word_of(sc, FM + HN + f), sh); });
+                else if constexpr (!SQ) spread(q, HN, [&](int f) { sb[HN + f] = scale_of_b(sc, HN + f, sh); });
                 spread(q, HM, [&](int f) { xs[HM + f] = scale_of_a(sc, HM + f, sh); });
             }
         }, HM, HN);
-        quarter(alo, b1, 0, HN, [&](int q) {
+        quarter(fold, alo, b1, 0, HN, [&](int q) {
             spread(q, 2 * HM, [&](int r) { ahi[r >> 1].h[r & 1] = half(cur, fa0, HM + (r >> 1), r & 1); });
             if constexpr (MODE == MM_POW2) spread(q, XN, [&](int f) { xn[f] = word_of(scn, f); });
         }, 0, 0);
         // Every wave has read the second part of this step, which is copied over now, and the first
         // part of the next has arrived.
         stage_barrier<LEFT>();
-        quarter(ahi, b0, HM, 0, [&](int q) {
+        quarter(fold, ahi, b0, HM, 0, [&](int q) {
             if constexpr (COPY) spread(q, PART, [&](int r) { copy1(da, db, cur, part_copy(r, 1)); });
             spread(q, 2 * HM, [&](int r) { alo[r >> 1].h[r & 1] = half(nxt, fa0, r >> 1, r & 1); });
             if constexpr (MODE != MM_POW2) {
                 spread(q, HM, [&](int f) { xs[f] = scale_of_a(scn, f, shn); });
-                if (SQ && q == 0) sqn = scale_of_square(scn, shn);
+                if (SQ && !FOLD && q == 0) sqn = scale_of_square(scn, shn);
             }
         }, 0, HN);
-        quarter(ahi, b1, HM, HN, [&](int q) {
+        quarter(fold, ahi, b1, HM, HN, [&](int q) {
             spread(q, 2 * HN, [&](int r) { b0[r >> 1].h[r & 1] = half(nxt, fb0, r >> 1, r & 1); });
             if constexpr (MODE == MM_POW2) {
                 spread(q, HM, [&](int f) { xs[f] = int(unsigned(xn[f]) >> shn); });
                 spread(q, HN, [&](int f) { xs[FM + f] = int(unsigned(xn[FM + f]) >> shn); });
+            } else if constexpr (FOLD) {
+                spread(q, HN, [&](int f) { xs[FM + f] = value(word_of(scn, FM + f), shn); });
             } else if constexpr (!SQ) {
                 spread(q, HN, [&](int f) { sb[f] = scale_of_b(scn, f, shn); });
             }
         }, HM, 0);
-        if constexpr (SQ) sq = sqn;
+        if constexpr (SQ && !FOLD) sq = sqn;
         // likewise the first part of the next step, and the second has arrived
         stage_barrier<LEFT>();
     };
 
+    auto run = [&]<bool FOLD>(std::bool_constant<FOLD> fold) {
+        const int *const sc = scales_of(0);
+        if constexpr (MODE == MM_POW2) {
+#pragma unroll
+            for (int f = 0; f < XN; ++f) xs[f] = xn[f] = word_of(sc, f);
+        } else {
+#pragma unroll
+            for (int f = 0; f < FM; ++f) xs[f] = scale_of_a(sc, f, 0);
+            if constexpr (FOLD) {
+#pragma unroll
+                for (int f = FM; f < XN; ++f) xs[f] = value(word_of(sc, f), 0);
+            } else if constexpr (SQ) {
+                sq = scale_of_square(sc, 0);
+            } else {
+#pragma unroll
+                for (int f = 0; f < FN; ++f) sb[f] = scale_of_b(sc, f, 0);
+            }
+        }
+        int kt = kt0;
+#pragma unroll 1
+        for (; kt + 2 < min(kt1, last); ++kt) step(std::true_type{}, fold, kt);
+#pragma unroll 1
+        for (; kt < kt1; ++kt) {
+            step(std::false_type{}, fold, kt);
+            // the step that reaches past K, half a step later than the others
+            if (kt + 2 < kt1) copy_any(kt + 2, ((kt - kt0) & 1) * STAGE);
+        }
+        // the last step read ahead into a stage that nothing was copied to; its values are unused
+        if constexpr (MODE != MM_POW2 && !FOLD)
+#pragma unroll
+            for (int d = 0; d < D; ++d) add_block(HM + qi(NQ - D + d), HN + qj(NQ - D + d), wp[d], ws[d]);
+    };
     if (kt0 < kt1) {
         copy_scales(kt0, 0);
         copy_any(kt0, 0);
         if (kt0 + 1 < kt1) copy_any(kt0 + 1, STAGE);
+        // MM_EXACT_POW2: scales of at most 2^40 go into the decoded operands, which then meet neither
+        // the largest bf16 number nor, while the values that they stand for are normal fp32 numbers,
+        // the smallest; the sums need no scaling any more (4096x8192x8192, both operands 1x128: 611 -> 521 us).
+        bool small = false;
+        if constexpr (MODE == MM_EXACT_POW2) small = !__syncthreads_or(scales_past_2_40());
         // (with fewer steps, or one that reaches past K among them, fewer copies are on their way)
         if (kt0 + 1 < min(kt1, last)) stage_barrier<2 * PART>();
         else stage_barrier<0>();
@@ -522,33 +592,12 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
         for (int f = 0; f < HN; ++f)
 #pragma unroll
             for (int h = 0; h < 2; ++h) b0[f].h[h] = half(0, fb0, f, h);
-        const int *const sc = scales_of(0);
-        if constexpr (MODE == MM_POW2) {
-#pragma unroll
-            for (int f = 0; f < XN; ++f) xs[f] = xn[f] = word_of(sc, f);
+        if constexpr (MODE == MM_EXACT_POW2) {
+            if (small) run(std::true_type{});
+            else run(std::false_type{});
         } else {
-#pragma unroll
-            for (int f = 0; f < FM; ++f) xs[f] = scale_of_a(sc, f, 0);
-            if constexpr (SQ) {
-                sq = scale_of_square(sc, 0);
-            } else {
-#pragma unroll
-                for (int f = 0; f < FN; ++f) sb[f] = scale_of_b(sc, f, 0);
-            }
+            run(std::false_type{});
         }
-        int kt = kt0;
-#pragma unroll 1
-        for (; kt + 2 < min(kt1, last); ++kt) step(std::true_type{}, kt);
-#pragma unroll 1
-        for (; kt < kt1; ++kt) {
-            step(std::false_type{}, kt);
-            // the step that reaches past K, half a step later than the others
-            if (kt + 2 < kt1) copy_any(kt + 2, ((kt - kt0) & 1) * STAGE);
-        }
-        // the last step read ahead into a stage that nothing was copied to; its values are unused
-        if constexpr (MODE != MM_POW2)
-#pragma unroll
-            for (int d = 0; d < D; ++d) add_block(HM + qi(NQ - D + d), HN + qj(NQ - D + d), wp[d], ws[d]);
     }
 
     // Lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of each 16 x 16 block.

@@ -94,20 +94,21 @@ __device__ __forceinline__ int pack4(float a, float b, float c, float d) {
     }
 }
 
-// Eight 8-bit values as bf16, exactly (both formats have fewer bits and a narrower range).
+// Eight 8-bit values times a power of two as bf16: exact where the results are normal numbers (both
+// formats have fewer bits).
 template <int FMT>
-__device__ __forceinline__ bf16x8 to_bf16(int lo, int hi) {
+__device__ __forceinline__ bf16x8 to_bf16(int lo, int hi, float scale = 1.f) {
     const int w[2] = {lo, hi};
     bf16x8 r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         bf16x2 t;
         if constexpr (FMT == DS_Q8_E4M3) {
-            t = (i & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i >> 1], 1.f, true)
-                        : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i >> 1], 1.f, false);
+            t = (i & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i >> 1], scale, true)
+                        : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i >> 1], scale, false);
         } else {
-            t = (i & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w[i >> 1], 1.f, true)
-                        : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w[i >> 1], 1.f, false);
+            t = (i & 1) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w[i >> 1], scale, true)
+                        : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(w[i >> 1], scale, false);
         }
         r[2 * i] = t[0];
         r[2 * i + 1] = t[1];
