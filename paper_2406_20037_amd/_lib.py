@@ -719,8 +719,16 @@ def _plain(t):
     return (t.data_ptr(), _PLAIN[t.dtype], *_plain_rows(t))
 
 
+# the current stream's handle without a Stream object (2.5 us of a call's 7)
+_raw_stream = getattr(getattr(_torch, "_C", None), "_cuda_getCurrentRawStream", None)
+
+
 def _q8_stream(stream):
-    return _torch.cuda.current_stream().cuda_stream if stream is None else stream_handle(stream)
+    if stream is not None:
+        return stream_handle(stream)
+    if _raw_stream is not None:
+        return _raw_stream(_torch.cuda.current_device())
+    return _torch.cuda.current_stream().cuda_stream
 
 
 def ds_q8_quantize(x, row=None, col=None, stream=None):

@@ -284,6 +284,7 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
     auto desc_b = [&](int kt) { return buffer_of(pb + int64_t(kt) * kQ8Block, nb); };
     // A step's copies in two parts: what the waves' first halves of rows and columns need, and the rest.
     constexpr int PART = (LA + LB) / 2;
+    static_assert(PART % 2 == 0);
     auto part_copy = [](int r, int hi) {                   // copy r of a part
         const int h = r < LA / 2 ? HM / 2 : HN / 2, x = r < LA / 2 ? r : r - LA / 2;
         return (r < LA / 2 ? 0 : LA) + x / h * 2 * h + x % h + hi * h;
@@ -297,13 +298,28 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
             return;
         }
         const int left = a.K - kt * kQ8Block - ck;         // bytes of this lane's 16 that exist
+        if (left >= 16) {                                  // (rows may be shorter than a step here)
+            const unsigned cut = kQ8Block - unsigned(a.K - kt * kQ8Block);
+            const intx4 da = buffer_of(pa + int64_t(kt) * kQ8Block, na - cut);
+            const intx4 db = buffer_of(pb + int64_t(kt) * kQ8Block, nb - cut);
+#pragma unroll
+            for (int j = 0; j < 2 * PART; ++j) copy1(da, db, st, j);
+            return;
+        }
 #pragma unroll 1
-        for (int j = 0; j < LA + LB; ++j) {
-            const int row = 32 * (j < LA ? j : j - LA) + cr;
-            const uint8_t *p = (j < LA ? pa + int64_t(min(row, a.M - 1 - m0)) * a.a.ld
-                                       : pb + int64_t(min(row, a.N - 1 - n0)) * a.b.ld) +
-                               int64_t(kt) * kQ8Block + ck;
-            *reinterpret_cast<intx4 *>(smem + st + wid * 1024 + j * 4096 + lane * 16) = first16(p, left);
+        for (int j = 0; j < 2 * PART; j += 4) {
+            intx4 v[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const bool isa = j + u < LA;
+                const int row = 32 * (isa ? j + u : j + u - LA) + cr;
+                v[u] = first16((isa ? pa + int64_t(min(row, a.M - 1 - m0)) * a.a.ld
+                                    : pb + int64_t(min(row, a.N - 1 - n0)) * a.b.ld) +
+                               int64_t(kt) * kQ8Block + ck, left);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                *reinterpret_cast<intx4 *>(smem + st + wid * 1024 + (j + u) * 4096 + lane * 16) = v[u];
         }
     };
 
