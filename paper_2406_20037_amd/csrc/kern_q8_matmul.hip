@@ -438,8 +438,9 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
     bf16x8 da[EXACT ? HM : 1][4], db[EXACT ? FN : 1][4];   // EXACT: decoded fragments, once a step
     // A quarter of the wave's tile, fragments i0 .. of A by j0 .. of B; beside(q) issues what goes
     // between its products q and q + 1.  wi, wj: the quarter before.
-    auto quarter = [&]<bool FOLD>(std::bool_constant<FOLD>, const Frag (&fa)[HM], const Frag (&fb)[HN], int i0,
-                                  int j0, auto beside, int wi, int wj) {
+    auto quarter = [&]<bool FOLD, int U4>(std::bool_constant<FOLD>, std::integral_constant<int, U4>,
+                                          const Frag (&fa)[HM], const Frag (&fb)[HN], int i0, int j0, auto beside,
+                                          int wi, int wj) {
         if constexpr (EXACT)
             if (j0 == 0)
 #pragma unroll
@@ -453,7 +454,8 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
             const int i = qi(q), j = qj(q);
             if constexpr (MODE == MM_POW2) {
                 acc[i0 + i][j0 + j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-                    fb[j], fa[i], acc[i0 + i][j0 + j], FB, FA, 0, xs[FM + j0 + j], 0, xs[i0 + i]);
+                    fb[j], fa[i], acc[i0 + i][j0 + j], FB, FA, U4 > 0 ? U4 : 0,
+                    xs[FM + j0 + j], U4 > 0 ? U4 : 0, xs[i0 + i]);
             } else {
                 floatx4 p = {0, 0, 0, 0};
                 if constexpr (EXACT) {
@@ -489,11 +491,14 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // step kt, whose first fragments are in alo and b0; COPY: the whole of step kt + 2 is copied
-    auto step = [&]<bool COPY, bool FOLD>(std::bool_constant<COPY>, std::bool_constant<FOLD> fold, int kt) {
+    // Step kt, whose first fragments are in alo and b0; COPY: the whole of step kt + 2 is copied.
+    // U4: its place among the four steps of a word of scales, -1 if that is not a constant (MM_POW2:
+    // a constant picks the word's byte in the instruction, else words are read and shifted each step).
+    auto step = [&]<bool COPY, bool FOLD, int U4>(std::bool_constant<COPY>, std::bool_constant<FOLD> fold,
+                                                  std::integral_constant<int, U4> u4, int kt) {
         const int u = kt - kt0;
         const unsigned cur = (u & 1) * STAGE, nxt = STAGE - cur;
-        if ((u & 3) == 0) copy_scales(kt + 4, ((u >> 2) & 1) ^ 1);
+        if (U4 < 0 ? (u & 3) == 0 : U4 == 0) copy_scales(kt + 4, ((u >> 2) & 1) ^ 1);
         __builtin_amdgcn_sched_barrier(0);
         // n parts spread over a quarter's first products, at most two after each
         auto spread = [](int q, int n, auto part) {
@@ -513,10 +518,14 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
         const int *const sc = scales_of(u), *const scn = scales_of(u + 1);
         const int sh = 8 * (u & 3), shn = 8 * ((u + 1) & 3);
         // Each half of the fragments and scales is replaced once its last product is issued
-        quarter(fold, alo, b0, 0, 0, [&](int q) {
+        quarter(fold, u4, alo, b0, 0, 0, [&](int q) {
             spread(q, 2 * HN, [&](int r) { b1[r >> 1].h[r & 1] = half(cur, fb0, HN + (r >> 1), r & 1); });
             if constexpr (COPY) spread(q, PART, [&](int r) { copy1(da, db, cur, part_copy(r, 0)); });
-            if constexpr (MODE == MM_POW2) {
+            if constexpr (U4 == 0) {
+                spread(q, HN, [&](int f) { xs[FM + HN + f] = word_of(sc, FM + HN + f); });
+                spread(q, HM, [&](int f) { xs[HM + f] = word_of(sc, HM + f); });
+            } else if constexpr (U4 > 0) {
+            } else if constexpr (MODE == MM_POW2) {
                 spread(q, HM, [&](int f) { xs[HM + f] = int(unsigned(xn[HM + f]) >> sh); });
                 spread(q, HN, [&](int f) { xs[FM + HN + f] = int(unsigned(xn[FM + HN + f]) >> sh); });
             } else {
@@ -525,24 +534,27 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
                 spread(q, HM, [&](int f) { xs[HM + f] = scale_of_a(sc, HM + f, sh); });
             }
         }, HM, HN);
-        quarter(fold, alo, b1, 0, HN, [&](int q) {
+        quarter(fold, u4, alo, b1, 0, HN, [&](int q) {
             spread(q, 2 * HM, [&](int r) { ahi[r >> 1].h[r & 1] = half(cur, fa0, HM + (r >> 1), r & 1); });
-            if constexpr (MODE == MM_POW2) spread(q, XN, [&](int f) { xn[f] = word_of(scn, f); });
+            if constexpr (MODE == MM_POW2 && U4 < 0) spread(q, XN, [&](int f) { xn[f] = word_of(scn, f); });
         }, 0, 0);
         // Every wave has read the second part of this step, which is copied over now, and the first
         // part of the next has arrived.
         stage_barrier<LEFT>();
-        quarter(fold, ahi, b0, HM, 0, [&](int q) {
+        quarter(fold, u4, ahi, b0, HM, 0, [&](int q) {
             if constexpr (COPY) spread(q, PART, [&](int r) { copy1(da, db, cur, part_copy(r, 1)); });
             spread(q, 2 * HM, [&](int r) { alo[r >> 1].h[r & 1] = half(nxt, fa0, r >> 1, r & 1); });
+            if constexpr (U4 == 3) spread(q, HM, [&](int f) { xs[f] = word_of(scn, f); });
             if constexpr (MODE != MM_POW2) {
                 spread(q, HM, [&](int f) { xs[f] = scale_of_a(scn, f, shn); });
                 if (SQ && !FOLD && q == 0) sqn = scale_of_square(scn, shn);
             }
         }, 0, HN);
-        quarter(fold, ahi, b1, HM, HN, [&](int q) {
+        quarter(fold, u4, ahi, b1, HM, HN, [&](int q) {
             spread(q, 2 * HN, [&](int r) { b0[r >> 1].h[r & 1] = half(nxt, fb0, r >> 1, r & 1); });
-            if constexpr (MODE == MM_POW2) {
+            if constexpr (U4 >= 0) {
+                if constexpr (U4 == 3) spread(q, HN, [&](int f) { xs[FM + f] = word_of(scn, FM + f); });
+            } else if constexpr (MODE == MM_POW2) {
                 spread(q, HM, [&](int f) { xs[f] = int(unsigned(xn[f]) >> shn); });
                 spread(q, HN, [&](int f) { xs[FM + f] = int(unsigned(xn[FM + f]) >> shn); });
             } else if constexpr (FOLD) {
@@ -575,11 +587,26 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
             }
         }
         int kt = kt0;
+        const int whole = min(kt1, last);
+        const std::integral_constant<int, -1> any;
+        // (in larger tiles four steps in one are more than the register allocator keeps in place)
+        if constexpr (MODE == MM_POW2 && FM * FN <= 16) {
 #pragma unroll 1
-        for (; kt + 2 < min(kt1, last); ++kt) step(std::true_type{}, fold, kt);
+            for (; kt + 5 < whole; kt += 4) {
+                step(std::true_type{}, fold, std::integral_constant<int, 0>{}, kt);
+                step(std::true_type{}, fold, std::integral_constant<int, 1>{}, kt + 1);
+                step(std::true_type{}, fold, std::integral_constant<int, 2>{}, kt + 2);
+                step(std::true_type{}, fold, std::integral_constant<int, 3>{}, kt + 3);
+            }
+            const int *const next = scales_of(kt - kt0);
+#pragma unroll
+            for (int f = 0; f < XN; ++f) xn[f] = word_of(next, f);
+        }
+#pragma unroll 1
+        for (; kt + 2 < whole; ++kt) step(std::true_type{}, fold, any, kt);
 #pragma unroll 1
         for (; kt < kt1; ++kt) {
-            step(std::false_type{}, fold, kt);
+            step(std::false_type{}, fold, any, kt);
             // the step that reaches past K, half a step later than the others
             if (kt + 2 < kt1) copy_any(kt + 2, ((kt - kt0) & 1) * STAGE);
         }

@@ -240,6 +240,53 @@ def test_matmul(env, mkn, kind):
         assert torch.isnan(c[M:]).all() and torch.isnan(c[:, N:]).all(), "wrote past C"
 
 
+# Shapes that go to each of the other launches: tiles of 256 x 256 and of 256 x 128 (whole,
+# ragged and with a reduction that no step of 128 ends), a reduction split over workgroups
+# in tiles and under few rows, 32 columns a workgroup.
+OTHERS = [(4096, 1024, 4096), (3900, 1000, 4001), (4096, 700, 4096), (2048, 1152, 4096), (2001, 1111, 4000),
+          (100, 5000, 200), (300, 2600, 129), (7, 9000, 70), (16, 16300, 33), (3, 300, 8200), (16, 1300, 16390),
+          (24, 520, 1000)]
+
+
+@pytest.mark.parametrize("mkn", OTHERS)
+@pytest.mark.parametrize("kind", [q8.POW2, q8.F32])
+def test_matmul_every_launch(env, mkn, kind):
+    torch, L = env
+    M, K, N = mkn
+    rng = np.random.default_rng(M + K + N + kind)
+    for fa, rb, name in ((0, 128, "bfloat16"), (1, 1, "bfloat16"), (1, 1, "float32")):
+        if M * N * K > 1 << 32 and (name == "float32" or (fa and kind)):
+            continue                                   # the same launch as smaller shapes
+        print("matmul", mkn, kind, fa, rb, name, flush=True)
+        a, av = operand(torch, L, rng, M, K, fa, kind, 1)
+        b, bv = operand(torch, L, rng, N, K, 0, kind, rb)
+        c = torch.full((M + 1, (N + 15) // 8 * 8), float("nan"), dtype=getattr(torch, name), device="cuda")
+        L.ds_q8_matmul(a, b, c[:M, :N])
+        torch.cuda.synchronize()
+        check_product(c[:M, :N], av, bv, name, M)
+        assert torch.isnan(c[M:]).all() and torch.isnan(c[:, N:]).all(), "wrote past C"
+
+
+def test_matmul_scales_in_unaligned_words(env):
+    """Scales whose rows do not start at words of four, and a split at such a place."""
+    torch, L = env
+    rng = np.random.default_rng(41)
+    for M, K, N in ((40, 1700, 130), (70, 5000, 64), (300, 900, 260)):
+        for name in ("bfloat16", "float32"):
+            a, av = operand(torch, L, rng, M, K, 0, q8.POW2, 1)
+            b, bv = operand(torch, L, rng, N, K, 0, q8.POW2, 1)
+            nb = -(-K // 128)
+            for m in (a, b):                           # rows nb bytes apart, from an odd address
+                raw = torch.empty(1 + m.rows * nb, dtype=torch.uint8, device="cuda")
+                view = raw[1:].view(m.rows, nb)
+                view.copy_(m.scale.view(torch.uint8))
+                m.tight = L.Q8.of(m.data, view.view(torch.float8_e8m0fnu))
+            c = torch.empty(M, N, dtype=getattr(torch, name), device="cuda")
+            L.ds_q8_matmul(a.tight, b.tight, c)
+            torch.cuda.synchronize()
+            check_product(c, av, bv, name, M)
+
+
 @pytest.mark.parametrize("name", ["bfloat16", "float32"])
 def test_matmul_sums_nothing(env, name):
     """K = 0: zeros.  M = 0 or N = 0: nothing is launched."""
