@@ -580,7 +580,7 @@ enum {
  * data: 16-byte aligned, ld >= cols a multiple of 16, below 2^24; bytes past cols
  * in a row are never used.  scale: ceil(rows / block_rows) rows of ceil(cols / 128)
  * entries, scale_ld >= that, below 2^22; F32 scales 4-byte aligned.  block_rows: 1, or 128 for
- * scales of 128x128 squares (weights).  rows, cols: 0 to 2^31 - 1. */
+ * scales of 128x128 squares (weights).  rows: 0 to 2^31 - 512. */
 typedef struct {
     void *data;
     void *scale;
@@ -613,12 +613,13 @@ int ds_q8_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t 
  * them.  c: type DS_TYPE_*, rows ldc elements apart, overwritten; aligned to its
  * type (16-byte rows are faster).  a and b have the same scale_type; formats and
  * block_rows are free.
- * Sums are held in fp32.  A 16-bit C of more than 16 rows comes from the 8-bit
- * matrix instructions, which align each eight products to their largest and keep
- * about 14 bits of them: 1e-5 to 1e-4 of the result for normal and for heavy-tailed
- * values, against 2^-9 and 2^-12 of the rounding to bf16 and fp16.  An fp32 C, or
- * one of up to 16 rows, comes from bf16 matrix instructions on the same values, whose
- * sums are exact to fp32.  The product of two scales has to be an fp32 number.
+ * Sums are held in fp32.  A 16-bit C of more than 16 rows (32 of a reduction of up to 4096)
+ * comes from the 8-bit matrix instructions, which align each eight products to their
+ * largest and keep about 14 bits of them: 1e-5 to 1e-4 of the result for normal and for
+ * heavy-tailed values, against 2^-9 and 2^-12 of the rounding to bf16 and fp16.  An fp32
+ * C, or one of fewer rows, comes from bf16 matrix instructions on the same values, whose
+ * sums are exact to fp32.  The product of two scales has to be an fp32 number; an operand's
+ * values (byte times scale) below 2^-126 may count as 0.
  * Few output tiles under a long reduction split it over workgroups and join the
  * partial sums in order in a workspace as kernel_run keeps (and under the same rule
  * for captures): two calls give the same bits.  Asynchronous on stream.

@@ -12,7 +12,8 @@ int q8_check(const ds_q8 *m, const char *what) {
         set_error("%s: null 8-bit matrix", what);
         return DS_EINVAL;
     }
-    if (m->rows < 0 || m->cols < 0 || m->rows > 0x7fffffff || m->cols > 0x7fffffff) {
+    // (room for a tile past the last row in 32 bits)
+    if (m->rows < 0 || m->cols < 0 || m->rows > 0x7ffffe00 || m->cols > 0x7ffffe00) {
         set_error("%s: %lld x %lld values", what, (long long)m->rows, (long long)m->cols);
         return DS_EINVAL;
     }
@@ -56,8 +57,7 @@ int plain_check(const void *p, int type, int64_t rows, int64_t cols, int64_t ld,
 
 namespace {
 
-// FULL, here and below: the caller has seen that all rows and columns exist and that rows of plain
-// matrices are 16-byte aligned.
+// FULL, here and below: the caller has seen that all rows and columns of a tile exist.
 
 // Eight elements of a row of `cols`, 0 past its end; vec: rows are 16-byte aligned.
 template <typename T>
@@ -77,10 +77,13 @@ struct Eight {
 template <bool FULL, typename T>
 __device__ __forceinline__ Eight<T> raw8(const T *row, int c, int cols, bool vec) {
     Eight<T> e;
-    if (FULL || (vec && c + 8 <= cols)) {
+    if (vec && (FULL || c + 8 <= cols)) {
 #pragma unroll
         for (size_t i = 0; i < sizeof(e) / 16; ++i)
             reinterpret_cast<intx4 *>(e.t)[i] = reinterpret_cast<const intx4 *>(row + c)[i];
+    } else if (FULL || c + 8 <= cols) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e.t[i] = row[c + i];
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) e.t[i] = c + i < cols ? row[c + i] : T(0.f);
@@ -154,7 +157,10 @@ __device__ __forceinline__ void by_fmt(int fmt, Fn fn) {
     else fn(std::integral_constant<int, DS_Q8_E5M2>{});
 }
 
-// Rows alone: 16 lanes a block.
+// Rows alone, or one plain matrix read once and written in a half to a quarter of its bytes: bound by
+// the memory.  16 lanes a block, so that the largest magnitude meets in one row of lanes, without LDS,
+// and a wave's loads cover whole lines: 16384x8192 bf16 in 71 us (5.7 TB/s, of which the caches
+// serve a part); of rows that are not 16-byte aligned 88.
 template <typename T>
 __global__ __launch_bounds__(256) void q8_rows(const T *x, int64_t ldx, int vec, Q8View m, int nb,
                                                int64_t total) {
@@ -169,6 +175,10 @@ __global__ __launch_bounds__(256) void q8_rows(const T *x, int64_t ldx, int vec,
 }
 
 // ---- tiles of 128 x 128 -----------------------------------------------------------
+// Both directions from one read: bound by the memory, if enough of it is on its way.  A tile stays in
+// registers while its rows' and its columns' largest magnitudes are found (rows by lanes, columns
+// by lanes, then over the waves through LDS), and its transpose goes through LDS as bytes, so that it
+// is written in whole lines too.  16384x8192 bf16 both ways in 110 us (4.9 TB/s), fp32 160 us (5.0).
 // 512 threads; thread t holds rows 4 (t / 16) .. + 3 of columns 8 (t % 16) .. + 7.
 constexpr int kTileThreads = 512, kRows = 4, kTileWaves = kTileThreads / 64;
 
@@ -341,13 +351,14 @@ __device__ __forceinline__ void tile_body(const T *x, int64_t ldx, int vec, int 
     transpose_out<FULL>(o, r0, lds.t);
 }
 
-// (six waves a SIMD unit hide the memory's latency: 117 us for 16384x8192 both ways, 125 with five)
+// (Six waves a SIMD unit hide the memory's latency: five took 7 % longer.  Where rows are not 16-byte
+// aligned a whole tile still loads without looking at each column: 16384x8191 bf16 223 -> 150 us.)
 template <typename T>
 __global__ __launch_bounds__(kTileThreads, 6) void q8_tile(const T *x, int64_t ldx, int vec, int rows, int cols,
                                                            int tiles_c, Q8View row, Q8View col) {
     __shared__ TileLds lds;
     const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
-    if (vec && tr * 128 + 128 <= rows && tc * 128 + 128 <= cols)
+    if (tr * 128 + 128 <= rows && tc * 128 + 128 <= cols)
         tile_body<true>(x, ldx, vec, rows, cols, tr, tc, row, col, lds);
     else
         tile_body<false>(x, ldx, vec, rows, cols, tr, tc, row, col, lds);
@@ -370,8 +381,12 @@ __device__ __forceinline__ float sigmoid(float g) {
     return fmaf(fmaf(-d, r, 1.f), r, r);
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void swiglu8_rows(const T *gu, int64_t ldg, int vec, int hidden, int up,
+// h = g sigmoid(g) u, with g and u kept in 8 bits: bound by the memory, the sigmoid's arithmetic
+// beside it.  As q8_rows: 16 lanes a block, which write up to three blocks of one read.  8192x8192 bf16
+// with its checkpoint in 85 us (5.5 TB/s).  VEC: rows are 16-byte aligned (8192x8191, which are not,
+// 109 us, and 142 with the columns looked at one by one).
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void swiglu8_rows(const T *gu, int64_t ldg, int hidden, int up,
                                                     Q8View h, Q8View saved, int nb, int64_t total) {
     const int cl = threadIdx.x & 15;
     const int64_t step = int64_t(gridDim.x) * 16;
@@ -380,8 +395,8 @@ __global__ __launch_bounds__(256) void swiglu8_rows(const T *gu, int64_t ldg, in
         const T *p = gu + int64_t(r) * ldg;
         const int c = b * kQ8Block + 8 * cl;
         float g[8], u[8], v[8];
-        load8<false>(p, c, hidden, vec, g);
-        load8<false>(p + up, c, hidden, vec, u);
+        load8<false>(p, c, hidden, VEC, g);
+        load8<false>(p + up, c, hidden, VEC, u);
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = g[k] * sigmoid(g[k]) * u[k];
         const bool in = b * kQ8Block < hidden;             // not a block between the two
@@ -452,7 +467,7 @@ __device__ __forceinline__ void grad_body(const Q8View &saved, const T *dh, int6
             x.u = bytes8<FULL>(q + up, c, hidden);
             x.sg = scale_at(saved.scale, saved.stype, si);
             x.su = scale_at(saved.scale, saved.stype, si + up / kQ8Block);
-            x.d = raw8<FULL>(dh + int64_t(rr) * ldh, c, hidden, vec);
+            x.d = raw8<FULL>(dh + int64_t(rr) * ldh, c, hidden, FULL || vec);
         }
         return x;
     };
@@ -502,7 +517,10 @@ __device__ __forceinline__ void grad_body(const Q8View &saved, const T *dh, int6
     emit(2);
 }
 
-// 8192x8192, bf16 dh: 229 us with two workgroups a CU and what that leaves out of registers, 263 with
+// A tile of g, u and dh gives three outputs in five layouts.  Its 602 MB at 8192x8192 would take
+// 116 us; bound by the vector unit (three exponent, reciprocal and rounding chains an element, and the
+// largest magnitudes of 5 x 128 blocks a tile) and by how few waves the registers leave to hide
+// latency: bf16 dh 229 us with two workgroups a CU and what that leaves out of registers, 263 with
 // one; fp32 dh, whose loaded rows take twice the registers, 281 and 237.
 template <typename T>
 __global__ __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 3 : 4) void swiglu8_grad_tile(Q8View saved, const T *dh, int64_t ldh,
@@ -630,8 +648,8 @@ int ds_swiglu8(const void *gu, int type, int64_t rows, int64_t hidden, int64_t u
     return by_type(type, [&](auto *t) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(t)>>;
         // the gate's block that reaches past hidden ends at `up` in the checkpoint
-        swiglu8_rows<T><<<row_grid(total), 256, 0, stream>>>(static_cast<const T *>(gu), ldg, vec,
-                                                             int(hidden), int(up), vh, vs, nb, total);
+        (vec ? swiglu8_rows<T, true> : swiglu8_rows<T, false>)<<<row_grid(total), 256, 0, stream>>>(
+            static_cast<const T *>(gu), ldg, int(hidden), int(up), vh, vs, nb, total);
     });
 }
 

@@ -1,4 +1,5 @@
 // C = A B^T of 8-bit matrices with a scale for each block of 128 along the reduction.
+#include <new>
 #include <type_traits>
 
 #include "kern_common.h"
@@ -92,9 +93,12 @@ __device__ __forceinline__ floatx4 dot128(const bf16x8 (&a)[4], intx8 b) {
 
 constexpr int kFewWaves = 8;
 
-// Up to 16 rows of A: the weight passes once from memory to registers, in the layout of the
-// matrix instructions, and bounds the time.  A workgroup has 16 NT columns; each of its waves
-// takes a run of the reduction's steps, two at a time in flight, and their sums meet in LDS.
+// C's 16 x 16 NT blocks for few rows of A: every byte of the weight is used once, so it passes once
+// from memory to registers, in the layout of the matrix instructions, and bounds the time; LDS
+// in between would only add to it.  A workgroup has 16 NT columns; each of its waves takes a run of
+// the reduction's steps, two at a time in flight, and their sums meet in LDS.  Each step's sum is
+// scaled by its two scales in fp32.  16x16384x8192 in 28 us (4.8 TB/s), 1x4096x4096 in 6.0, of which
+// 3 are the launch's.
 // SQ: B's scales are of squares, one for the workgroup's columns.
 template <int NT, bool SQ, int FA, int FB>
 __global__ __launch_bounds__(64 * kFewWaves) void q8_few(Q8MatArgs a) {
@@ -241,6 +245,14 @@ struct MmShape {
     static constexpr int LDS = 2 * STAGE + 2 * SCALES;
 };
 
+// C = sum over steps of 128 of (A's scales x B's scales) * (A's bytes B's bytes^T), in a tile of C that
+// stays in registers.  Bound by the matrix instructions: a step of a 256 x 256 tile is 16.8 MFLOP for
+// 64 KB, more than the caches' rate asks for.  Operands go from memory to LDS without registers, in
+// two stages, each step's copies issued a step and a half before their use, in two parts, as
+// each half of a stage has been read; fragments are read from LDS between the products of the
+// quarter before.  8192x16384x8192 to bf16: 820 us (2.7 PFLOP/s; the instructions alone, on random
+// bytes in registers, reach 3.2 to 4.2 at the clock that the power leaves them).  Exact to fp32:
+// 4096x8192x8192 475 us (1.2 PFLOP/s; bf16 instructions alone 2.0 to 2.2, and each byte is first decoded).
 // SQ: B's scales are of squares, one for all columns of a wave.  A tile of 256 columns or rows leaves
 // one wave a SIMD unit; the smaller ones two.
 template <int FM, int FN, int MODE, bool SQ, int FA, int FB>
@@ -621,7 +633,7 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
         if (kt0 + 1 < kt1) copy_any(kt0 + 1, STAGE);
         // MM_EXACT_POW2: scales of at most 2^40 go into the decoded operands, which then meet neither
         // the largest bf16 number nor, while the values that they stand for are normal fp32 numbers,
-        // the smallest; the sums need no scaling any more (4096x8192x8192, both operands 1x128: 611 -> 521 us).
+        // the smallest; the sums need no scaling any more (4096x8192x8192, both operands 1x128: 15 % less time).
         bool small = false;
         if constexpr (MODE == MM_EXACT_POW2) small = !__syncthreads_or(scales_past_2_40());
         // (with fewer steps, or one that reaches past K among them, fewer copies are on their way)
@@ -719,7 +731,8 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
     }
 }
 
-// C from the partial sums of ks splits, in their order.
+// C from the partial sums of ks splits, in their order: the same bits at every call, where atomics would
+// give others.  Bound by the launch (3 us) and the sums' reading, from the cache mostly.
 __global__ __launch_bounds__(256) void q8_join(Q8MatArgs a) {
     const int per = (a.N + 3) / 4;
     const int64_t total = int64_t(a.M) * per, mn = int64_t(a.M) * a.N;
@@ -894,7 +907,11 @@ extern "C" int ds_q8_matmul(const ds_q8 *a, const ds_q8 *b, void *c, int type, i
         return reinterpret_cast<uintptr_t>(m->scale) % 4 == 0 && m->scale_ld % 4 == 0;
     };
     g.words = words(a) && words(b);
-    // (32 rows of a short reduction too: 32x4096x4096 12.6 us, in tiles 13.9)
-    if (g.M > (g.nkt <= 32 ? 32 : 16)) return mm_tiles(g, stream);
-    return few(g, stream);
+    try {
+        // (32 rows of a short reduction too: 32x4096x4096 12.6 us, in tiles 13.9)
+        return g.M > (g.nkt <= 32 ? 32 : 16) ? mm_tiles(g, stream) : few(g, stream);
+    } catch (const std::bad_alloc &) {                     // of the workspaces' table
+        set_error("ds_q8_matmul: out of host memory");
+        return DS_ENOMEM;
+    }
 }
