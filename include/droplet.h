@@ -5,7 +5,9 @@
  * explore/exploit kernel scheduler of "Explore as a Storm, Exploit as a
  * Raindrop" (Canesche, Verma, Pereira): a schedule-parameterised fp32 kernel family (NCHW conv2d and
  * row-major matmul) written in HIP for gfx950, a hipEvent measurement harness,
- * a seeded exploration sampler and Droplet Search coordinate descent.
+ * a seeded exploration sampler and Droplet Search coordinate descent; and
+ * operators of large language models in 8-bit floating point (quantization in
+ * blocks, the products, the gated unit and its gradient).
  *
  * Conventions for every entry point:
  *   - The return value is a status: DS_OK (0) or a negative DS_E* code.  No

@@ -2,7 +2,8 @@
 combined Ansor + Droplet Search approach: a schedule-parameterised fp32
 conv2d / matmul kernel family in HIP, a hipEvent measurement harness, a seeded
 exploration sampler and Droplet Search coordinate descent, behind the C ABI
-of ``include/droplet.h``.  ``_lib`` is the Python binding of that ABI; it is
+of ``include/droplet.h``; and the 8-bit operators of the same ABI (``Q8``,
+``ds_q8_quantize``, ``ds_q8_matmul``, ``ds_swiglu8``, ``ds_swiglu8_grad``).  ``_lib`` is the Python binding of that ABI; it is
 loaded on first use of any name below, and raises if the library is missing.
 """
 _EXPORTS = ["DS_OP_CONV2D_NCHW", "DS_OP_MATMUL_RM", "Q8", "Space", "ansor_sample", "droplet_tune",

@@ -809,8 +809,8 @@ int mm_square(Q8MatArgs &g, hipStream_t stream) {
 
 // The split of a reduction over tiles of 128 x 128, by what each took on the chip: a step of 128 about
 // `step` us in a workgroup that has its SIMD units to itself, and the join 3 us and the partial sums'
-// writing and reading.  32x4096x4096 20.7 -> 13.9 us by four, 64x16384x8192 49 -> 38; 512x4096x4096
-// would go from 21.8 to 22.8 and stays whole.
+// writing and reading.  33x4096x4096 18.6 -> 13.8 us by four, 64x16384x8192 48 -> 38; 512x4096x4096
+// would go from 18.4 to 22.0 and stays whole.
 int mm_splits(const Q8MatArgs &g, double step) {
     const int64_t tiles = int64_t((g.M + 127) / 128) * ((g.N + 127) / 128);
     const double sums = double(g.M) * g.N * 10 / 4.5e6;
@@ -831,8 +831,8 @@ int mm_tiles(Q8MatArgs &g, hipStream_t stream) {
     auto tiles = [&](int bm, int bn) { return int64_t((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn); };
     if (pow2 && !exact) {
         // Rounds of workgroups over 256 CUs times a round's time: a step of 1.47, 0.95, 1.1 us (two
-        // workgroups a CU, 0.62 for one) and what comes before and after.  2048x4096x8192: 92, 66
-        // and 71 us; 4096x4096x4096: 61, 73 and 69; 1024x4096x4096: 51, 33 and 23.
+        // workgroups a CU, 0.62 for one) and what comes before and after.  2048x4096x8192: 91, 66
+        // and 72 us; 4096x4096x4096: 60, 70 and 66; 1024x4096x4096: 47, 30 and 22.
         const double n = g.nkt;
         const int64_t t = tiles(128, 128);
         const double large = double((tiles(256, 256) + 255) / 256) * (1.47 * n + 14);
