@@ -100,9 +100,17 @@ __device__ __forceinline__ void load8(const T *row, int c, int cols, bool vec, f
 // The bits of the largest magnitude, kInf or more where some value is not finite: the largest as
 // signed numbers is the largest positive one, as unsigned the most negative one if there is any
 // (one instruction for two values each, where taking signs off first would cost one a value).
+// SUMS: results of arithmetic, which have no signalling NaNs; of those a floating-point maximum passes
+// over the NaNs and takes two values an instruction.
 constexpr unsigned kInf = 0x7f800000u;
-template <int N>
+template <bool SUMS, int N>
 __device__ __forceinline__ unsigned max_bits(const float (&v)[N]) {
+    if constexpr (SUMS) {
+        float m = fmaxf(fabsf(v[0]), fabsf(v[1]));
+#pragma unroll
+        for (int i = 2; i < N; i += 2) m = fmaxf(fmaxf(m, fabsf(v[i])), fabsf(v[i + 1]));
+        return __float_as_uint(m);
+    }
     int pos = 0;
     unsigned neg = 0;
 #pragma unroll
@@ -117,7 +125,11 @@ template <int N>
 __device__ __forceinline__ unsigned max_finite(const float (&v)[N]) {
     unsigned m = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) m = max(m, finite_abs(v[i]));
+    for (int i = 0; i < N; ++i) {
+        float x = v[i];
+        __asm__("" : "+v"(x), "+v"(m));                    // one by one, in few registers
+        m = max(m, finite_abs(x));
+    }
     return m;
 }
 
@@ -140,9 +152,9 @@ __device__ __forceinline__ void store_values(uint8_t *row, int c, int cols, cons
 }
 
 // One 1x128 block of row r at columns c0 .. c0+127, held by 16 lanes of eight values each.
-template <int FMT, bool FULL>
+template <int FMT, bool FULL, bool SUMS>
 __device__ __forceinline__ void emit_block(const Q8View &m, int r, int blk, int cl, const float (&v)[8]) {
-    unsigned top = max_bits(v);
+    unsigned top = max_bits<SUMS>(v);
     // what is not finite sets no scale: only a wave that holds some looks at each value
     if (__any(top >= kInf)) top = max_finite(v);
     const BlockScale s = block_scale(max16(top), FMT, m.stype);
@@ -170,7 +182,7 @@ __global__ __launch_bounds__(256) void q8_rows(const T *x, int64_t ldx, int vec,
         const int r = int(i / nb), b = int(i - int64_t(r) * nb);
         float v[8];
         load8<false>(x + int64_t(r) * ldx, b * kQ8Block + 8 * cl, m.cols, vec, v);
-        by_fmt(m.fmt, [&](auto f) { emit_block<f.value, false>(m, r, b, cl, v); });
+        by_fmt(m.fmt, [&](auto f) { emit_block<f.value, false, false>(m, r, b, cl, v); });
     }
 }
 
@@ -190,13 +202,20 @@ struct TileLds {
     intx4 t[128 * 8];
 };
 
-// Largest over the wave's 16 rows of lanes' column, in all four rows of 16 lanes.
-__device__ __forceinline__ unsigned over_rows(unsigned m) {
+// Largest over the wave's four rows of lanes of eight columns: row of lanes q keeps columns 2 q and
+// 2 q + 1.  Each swap brings two columns' values together at once.
+__device__ __forceinline__ void over_rows(unsigned (&m)[8]) {
     typedef unsigned uintx2 __attribute__((ext_vector_type(2)));
-    const uintx2 a = __builtin_amdgcn_permlane16_swap(m, m, false, false);   // rows 0 0 2 2 and 1 1 3 3
-    m = max(a[0], a[1]);
-    const uintx2 b = __builtin_amdgcn_permlane32_swap(m, m, false, false);   // halves 0 0 and 1 1
-    return max(b[0], b[1]);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {                          // lower lanes c, upper lanes c + 4
+        const uintx2 a = __builtin_amdgcn_permlane32_swap(m[c], m[c + 4], false, false);
+        m[c] = max(a[0], a[1]);
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {                          // rows of lanes c, c + 2, c + 4, c + 6
+        const uintx2 a = __builtin_amdgcn_permlane16_swap(m[c], m[c + 2], false, false);
+        m[c] = max(a[0], a[1]);
+    }
 }
 
 // One tile and where it goes: to `row` at (r0, c0) and transposed to `col` at (rc0, r0); either has
@@ -206,26 +225,53 @@ struct TileOut {
     int c0, rc0;
 };
 
-template <bool FULL>
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp(unsigned v) {
+    return unsigned(__builtin_amdgcn_update_dpp(0, int(v), CTRL, 0xF, 0xF, false));
+}
+
+// The thread's four rows: lane l of 16 gathers the largest magnitude of row l % 4, so that one scale a
+// lane is formed and stored, and each group of four lanes has all four.
+template <bool FULL, bool SUMS>
 __device__ __forceinline__ void emit_rows(const float (&v)[kRows][8], const TileOut &o, int r0) {
     const int cl = threadIdx.x & 15, rg = threadIdx.x >> 4;
-    by_fmt(o.row.fmt, [&](auto f) {
+    unsigned m[kRows];
 #pragma unroll
-        for (int r = 0; r < kRows; ++r) {
-            const int rr = r0 + kRows * rg + r;
-            if (FULL || rr < o.row.rows) emit_block<f.value, FULL>(o.row, rr, o.c0 >> 7, cl, v[r]);
-        }
-    });
+    for (int r = 0; r < kRows; ++r) m[r] = max_bits<SUMS>(v[r]);
+    if (__any(max(max(m[0], m[1]), max(m[2], m[3])) >= kInf))
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) m[r] = max_finite(v[r]);
+    const bool odd = cl & 1, high = cl & 2;
+    const unsigned a = max(odd ? m[1] : m[0], dpp<0xB1>(odd ? m[0] : m[1]));   // with lane ^ 1
+    const unsigned b = max(odd ? m[3] : m[2], dpp<0xB1>(odd ? m[2] : m[3]));
+    unsigned top = max(high ? b : a, dpp<0x4E>(high ? a : b));                 // with lane ^ 2
+    top = max(top, dpp<0x124>(top));                                           // lanes turned by 4, by 8
+    top = max(top, dpp<0x128>(top));
+    const BlockScale s = block_scale(top, o.row.fmt, o.row.stype);
+    const int rr = r0 + kRows * rg;
+    if (cl < kRows && (FULL || rr + cl < o.row.rows))
+        store_scale(o.row, int64_t(rr + cl) * o.row.sld + (o.c0 >> 7), s.bits);
+    const unsigned inv = __float_as_uint(s.inv);
+    const float by[kRows] = {__uint_as_float(dpp<0x00>(inv)), __uint_as_float(dpp<0x55>(inv)),
+                             __uint_as_float(dpp<0xAA>(inv)), __uint_as_float(dpp<0xFF>(inv))};
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+        if (FULL || rr + r < o.row.rows)
+            by_fmt(o.row.fmt, [&](auto f) {                // row by row: scaled values of one at a time
+                store_values<f.value, FULL>(o.row.data + int64_t(rr + r) * o.row.ld, o.c0 + 8 * cl, o.row.cols, v[r],
+                                            by[r]);
+            });
 }
 
 // The thread's largest magnitudes of its eight columns, then the wave's to `lds`.
+template <bool SUMS>
 __device__ __forceinline__ void column_max(const float (&v)[kRows][8], unsigned (*lds)[128]) {
     const int tid = threadIdx.x;
     unsigned m[8], any = 0;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
         const float u[kRows] = {v[0][c], v[1][c], v[2][c], v[3][c]};
-        m[c] = max_bits(u);
+        m[c] = max_bits<SUMS>(u);
         any = max(any, m[c]);
     }
     if (__any(any >= kInf))
@@ -234,13 +280,8 @@ __device__ __forceinline__ void column_max(const float (&v)[kRows][8], unsigned 
             const float u[kRows] = {v[0][c], v[1][c], v[2][c], v[3][c]};
             m[c] = max_finite(u);
         }
-#pragma unroll
-    for (int c = 0; c < 8; ++c) m[c] = over_rows(m[c]);
-    if ((tid & 48) == 0) {
-        intx4 *p = reinterpret_cast<intx4 *>(lds[tid >> 6] + 8 * (tid & 15));
-        p[0] = intx4{int(m[0]), int(m[1]), int(m[2]), int(m[3])};
-        p[1] = intx4{int(m[4]), int(m[5]), int(m[6]), int(m[7])};
-    }
+    over_rows(m);
+    *reinterpret_cast<intx2 *>(lds[tid >> 6] + 8 * (tid & 15) + 2 * (tid >> 4 & 3)) = intx2{int(m[0]), int(m[1])};
 }
 
 // The columns' scales, once the waves' column_max are in.
@@ -288,9 +329,9 @@ __device__ __forceinline__ void transpose_out(const TileOut &o, int r0, const in
 }
 
 // Column by column: a tile's transpose.  The LDS is free again after a barrier that follows.
-template <bool FULL>
+template <bool FULL, bool SUMS>
 __device__ __forceinline__ void emit_columns(const float (&v)[kRows][8], const TileOut &o, int r0, TileLds &lds) {
-    column_max(v, lds.colmax);
+    column_max<SUMS>(v, lds.colmax);
     __syncthreads();
     column_scales(o, r0, lds);
     __syncthreads();
@@ -317,13 +358,13 @@ __device__ __forceinline__ void tile_body(const T *x, int64_t ldx, int vec, int 
         }
     }
     if (!(row.data ? row.shift : col.shift)) {
-        if (row.data) emit_rows<FULL>(v, o, r0);
+        if (row.data) emit_rows<FULL, false>(v, o, r0);
         if (!col.data) return;
-        emit_columns<FULL>(v, o, r0, lds);
+        emit_columns<FULL, false>(v, o, r0, lds);
         return;
     }
     // one scale for the square
-    column_max(v, lds.colmax);
+    column_max<false>(v, lds.colmax);
     __syncthreads();
     unsigned all = 0;
 #pragma unroll
@@ -351,14 +392,19 @@ __device__ __forceinline__ void tile_body(const T *x, int64_t ldx, int vec, int 
     transpose_out<FULL>(o, r0, lds.t);
 }
 
-// (Six waves a SIMD unit hide the memory's latency: five took 7 % longer.  Where rows are not 16-byte
-// aligned a whole tile still loads without looking at each column: 16384x8191 bf16 223 -> 150 us.)
-template <typename T>
-__global__ __launch_bounds__(kTileThreads, 6) void q8_tile(const T *x, int64_t ldx, int vec, int rows, int cols,
-                                                           int tiles_c, Q8View row, Q8View col) {
+// WHOLE, here and below: all tiles are whole and rows 16-byte aligned.  That kernel has the one body
+// without divergent branches, and fits the registers of more waves: six a SIMD unit hide the
+// memory's latency here, and five take 7 % longer.  No instance may spill registers: the compiler
+// has been seen to reload one at the end of a divergent branch for a part of the lanes only.
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(kTileThreads, WHOLE ? 6 : 5) void q8_tile(const T *x, int64_t ldx, int vec, int rows,
+                                                                       int cols, int tiles_c, Q8View row,
+                                                                       Q8View col) {
     __shared__ TileLds lds;
     const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
-    if (tr * 128 + 128 <= rows && tc * 128 + 128 <= cols)
+    if (WHOLE)
+        tile_body<true>(x, ldx, true, rows, cols, tr, tc, row, col, lds);
+    else if (tr * 128 + 128 <= rows && tc * 128 + 128 <= cols)
         tile_body<true>(x, ldx, vec, rows, cols, tr, tc, row, col, lds);
     else
         tile_body<false>(x, ldx, vec, rows, cols, tr, tc, row, col, lds);
@@ -366,25 +412,22 @@ __global__ __launch_bounds__(kTileThreads, 6) void q8_tile(const T *x, int64_t l
 
 // ---- gated unit -----------------------------------------------------------------
 
-// 1 / (1 + exp(-g)).  exp(-g) = 2^(hi + lo), hi the rounded product with log2(e) and lo
-// what the rounding and the constant leave out, so the error does not grow with |g|;
-// the quotient by one Newton step on the reciprocal.
+// 1 / (1 + exp(-g)).  exp(-g) = 2^(hi + lo), hi the rounded product with log2(e) and lo what the
+// rounding and the constant leave out, so the error does not grow with |g|.  Beyond +-88.5, where
+// the result is 1 or less than any normal number, g is taken as that, and all steps are finite.
 __device__ __forceinline__ float sigmoid(float g) {
     const float L = 1.44269502f, L2 = 1.92596299e-8f;      // log2(e) in two parts
+    g = __builtin_amdgcn_fmed3f(g, -88.5f, 88.5f);
     const float hi = -g * L;
-    const float lo = fmaf(-g, L, -hi) - g * L2;
-    float e = __builtin_amdgcn_exp2f(hi);
-    // e * 2^lo; where e is 0 or infinite the result is 1 or 0 whatever lo says
-    e = fabsf(hi) < 127.9f ? fmaf(e, lo * 0.693147181f, e) : e;
-    const float d = 1.f + fminf(e, 3e38f);                 // finite, as the step wants it
-    const float r = __builtin_amdgcn_rcpf(d);
-    return fmaf(fmaf(-d, r, 1.f), r, r);
+    const float lo = fmaf(-g, L2, fmaf(-g, L, -hi));
+    const float e = __builtin_amdgcn_exp2f(hi);
+    return __builtin_amdgcn_rcpf(1.f + fmaf(e, lo * 0.693147181f, e));
 }
 
 // h = g sigmoid(g) u, with g and u kept in 8 bits: bound by the memory, the sigmoid's arithmetic
 // beside it.  As q8_rows: 16 lanes a block, which write up to three blocks of one read.  8192x8192 bf16
-// with its checkpoint in 85 us (5.5 TB/s).  VEC: rows are 16-byte aligned (8192x8191, which are not,
-// 109 us, and 142 with the columns looked at one by one).
+// with its checkpoint in 83 us (5.7 TB/s).  VEC: rows are 16-byte aligned (8192x8191, which are not,
+// 107 us, and 142 with the columns looked at one by one).
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void swiglu8_rows(const T *gu, int64_t ldg, int hidden, int up,
                                                     Q8View h, Q8View saved, int nb, int64_t total) {
@@ -400,11 +443,11 @@ __global__ __launch_bounds__(256) void swiglu8_rows(const T *gu, int64_t ldg, in
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = g[k] * sigmoid(g[k]) * u[k];
         const bool in = b * kQ8Block < hidden;             // not a block between the two
-        if (in) by_fmt(h.fmt, [&](auto f) { emit_block<f.value, false>(h, r, b, cl, v); });
+        if (in) by_fmt(h.fmt, [&](auto f) { emit_block<f.value, false, true>(h, r, b, cl, v); });
         if (saved.data)
             by_fmt(saved.fmt, [&](auto f) {
-                emit_block<f.value, false>(saved, r, b, cl, g);
-                if (in) emit_block<f.value, false>(saved, r, b + up / kQ8Block, cl, u);
+                emit_block<f.value, false, false>(saved, r, b, cl, g);
+                if (in) emit_block<f.value, false, false>(saved, r, b + up / kQ8Block, cl, u);
             });
     }
 }
@@ -478,9 +521,9 @@ __device__ __forceinline__ void grad_body(const Q8View &saved, const T *dh, int6
     // the registers of two workgroups a CU.
     float silu[kRows][8], v[kRows][8];
     auto emit = [&](int n) {
-        if (o[n].row.data) emit_rows<FULL>(v, o[n], r0);
+        if (o[n].row.data) emit_rows<FULL, true>(v, o[n], r0);
         // (the tile before is read out of LDS before the first of these barriers and written after)
-        if (o[n].col.data) emit_columns<FULL>(v, o[n], r0, lds);
+        if (o[n].col.data) emit_columns<FULL, true>(v, o[n], r0, lds);
     };
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
@@ -491,7 +534,7 @@ __device__ __forceinline__ void grad_body(const Q8View &saved, const T *dh, int6
         for (int k = 0; k < 8; ++k) {
             const float s = sigmoid(g[k]);
             silu[r][k] = g[k] * s;
-            v[r][k] = float(x[r].d.t[k]) * u[k] * (s * (1.f + g[k] * (1.f - s)));
+            v[r][k] = float(x[r].d.t[k]) * u[k] * fmaf(silu[r][k], 1.f - s, s);
         }
     }
     emit(0);
@@ -518,18 +561,17 @@ __device__ __forceinline__ void grad_body(const Q8View &saved, const T *dh, int6
 }
 
 // A tile of g, u and dh gives three outputs in five layouts.  Its 602 MB at 8192x8192 would take
-// 116 us; bound by the vector unit (three exponent, reciprocal and rounding chains an element, and the
-// largest magnitudes of 5 x 128 blocks a tile) and by how few waves the registers leave to hide
-// latency: bf16 dh 229 us with two workgroups a CU and what that leaves out of registers, 263 with
-// one; fp32 dh, whose loaded rows take twice the registers, 281 and 237.
-template <typename T>
-__global__ __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 3 : 4) void swiglu8_grad_tile(Q8View saved, const T *dh, int64_t ldh,
-                                                                     int vec, int hidden, int up, int tiles_c,
-                                                                     Q8View dgu, Q8View dgu_t, Q8View h_t) {
+// 116 us; bound by the vector unit (about 55 instructions a value: the sigmoid, three products, and five
+// maxima, scalings and roundings) and by how few waves the registers leave to hide latency: bf16 dh
+// 154 us with 16 waves a CU; fp32 dh, whose loaded rows take twice the registers, 201 with 8.
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 3 : 4) void swiglu8_grad_tile(
+    Q8View saved, const T *dh, int64_t ldh, int vec, int hidden, int up, int tiles_c, Q8View dgu, Q8View dgu_t,
+    Q8View h_t) {
     __shared__ TileLds lds;
     const int tr = blockIdx.x / tiles_c, tc = blockIdx.x - tr * tiles_c;
-    if (vec && tr * 128 + 128 <= saved.rows && tc * 128 + 128 <= hidden)
-        grad_body<true>(saved, dh, ldh, vec, hidden, up, tr, tc, dgu, dgu_t, h_t, lds);
+    if (WHOLE || (vec && tr * 128 + 128 <= saved.rows && tc * 128 + 128 <= hidden))
+        grad_body<true>(saved, dh, ldh, true, hidden, up, tr, tc, dgu, dgu_t, h_t, lds);
     else
         grad_body<false>(saved, dh, ldh, vec, hidden, up, tr, tc, dgu, dgu_t, h_t, lds);
 }
@@ -627,8 +669,9 @@ int ds_q8_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t 
     if ((rc = tile_grid(rows, cols, &grid)) != DS_OK) return rc;
     return by_type(type, [&](auto *t) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(t)>>;
-        q8_tile<T><<<grid, kTileThreads, 0, stream>>>(static_cast<const T *>(x), ldx, vec, int(rows), int(cols),
-                                             int(q8_up(cols)), vr, vc);
+        (vec && rows % 128 == 0 && cols % 128 == 0 ? q8_tile<T, true> : q8_tile<T, false>)
+            <<<grid, kTileThreads, 0, stream>>>(static_cast<const T *>(x), ldx, vec, int(rows), int(cols),
+                                                int(q8_up(cols)), vr, vc);
     });
 }
 
@@ -675,8 +718,9 @@ int ds_swiglu8_grad(const ds_q8 *saved, const void *dh, int type, int64_t hidden
     const int vec = rows16(dh, type, ldh);
     return by_type(type, [&](auto *t) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(t)>>;
-        swiglu8_grad_tile<T><<<grid, kTileThreads, 0, stream>>>(vs, static_cast<const T *>(dh), ldh, vec,
-                                                       int(hidden), int(up), int(up / kQ8Block), vd, vt, vh);
+        (vec && rows % 128 == 0 && hidden == up ? swiglu8_grad_tile<T, true> : swiglu8_grad_tile<T, false>)
+            <<<grid, kTileThreads, 0, stream>>>(vs, static_cast<const T *>(dh), ldh, vec, int(hidden), int(up),
+                                                int(up / kQ8Block), vd, vt, vh);
     });
 }
 
