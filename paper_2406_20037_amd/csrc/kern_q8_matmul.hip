@@ -212,16 +212,17 @@ __device__ __forceinline__ intx4 buffer_of(const uint8_t *p, unsigned n) {
 
 // Copies 16 bytes a lane from d at off to LDS at dst + 16 lane.  The compiler does not see
 // an LDS write here that later reads would have to wait for: stage_barrier's wait and the
-// memory clobbers order the two.
+// memory clobbers order the two.  One instruction has to lie between a write of m0, where dst is
+// taken from, and the copy: the compiler, which writes m0 before, puts none in front of a statement.
 __device__ __forceinline__ void copy16(intx4 d, unsigned off, unsigned dst) {
-    __asm__ volatile("s_mov_b32 m0, %2\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
-                     :: "v"(off), "s"(d), "s"(dst) : "memory", "m0");
+    __asm__ volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+                     :: "v"(off), "s"(d), "{m0}"(dst) : "memory");
 }
 
 // The same for four bytes a lane.
 __device__ __forceinline__ void copy4(intx4 d, unsigned off, unsigned dst) {
-    __asm__ volatile("s_mov_b32 m0, %2\n\tbuffer_load_dword %0, %1, 0 offen lds"
-                     :: "v"(off), "s"(d), "s"(dst) : "memory", "m0");
+    __asm__ volatile("s_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds"
+                     :: "v"(off), "s"(d), "{m0}"(dst) : "memory");
 }
 
 // How a tile's products are formed.
