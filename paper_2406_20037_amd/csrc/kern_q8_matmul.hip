@@ -1,4 +1,5 @@
 // C = A B^T of 8-bit matrices with a scale for each block of 128 along the reduction.
+#include <climits>
 #include <new>
 #include <type_traits>
 
@@ -46,15 +47,20 @@ __device__ __forceinline__ void store4(void *c, int type, int64_t at, int col, i
     }
 }
 
+// The first n of 16 bytes.
+__device__ __forceinline__ intx4 mask16(int n) {
+    intx4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = n >= 4 * i + 4 ? -1 : n > 4 * i ? (1 << (8 * (n - 4 * i))) - 1 : 0;
+    return v;
+}
+
 // 16 bytes from a 16-byte aligned p, zeros from the n-th on.  They are loaded whole where one of
 // them exists: an aligned 16 bytes never reach past the page, or the allocation, of any one.
 __device__ __forceinline__ intx4 first16(const uint8_t *p, int n) {
     intx4 v = {0, 0, 0, 0};
     if (n > 0) v = *reinterpret_cast<const intx4 *>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        v[i] &= n >= 4 * i + 4 ? -1 : n > 4 * i ? (1 << (8 * (n - 4 * i))) - 1 : 0;
-    return v;
+    return v & mask16(n);
 }
 __device__ __forceinline__ intx8 whole32(const uint8_t *p) {
     const intx4 x = reinterpret_cast<const intx4 *>(p)[0], y = reinterpret_cast<const intx4 *>(p)[1];
@@ -275,7 +281,7 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
     const int gm = min(a.tiles_m - first, a.group), r = t - g * per, rn = scalar(r / gm);
     const int m0 = (first + r - rn * gm) * BM, n0 = rn * BN;
     const int kt0 = z * a.kps, kt1 = min(a.nkt, kt0 + a.kps);
-    const int last = a.K % kQ8Block ? a.nkt - 1 : a.nkt;   // the step that reaches past K, if any
+    const int last = a.K % kQ8Block ? a.nkt - 1 : INT_MAX; // the step that reaches past K, if any
 
     // A wave's copy j brings rows 32 j + 8 wid .. + 7 of the stage: lane l the 16 bytes at slot
     // l % 8 of row l / 8.  Slot s of row r holds bytes 16 (s ^ (r / 2) % 8) .. + 15 of the step, so that
@@ -288,13 +294,19 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
     const unsigned nb = unsigned(min(BN, a.N - n0) - 1) * unsigned(a.b.ld) + kQ8Block;
     const unsigned lds0 = unsigned(uintptr_t(DS_LOCAL(smem))) + wid * 1024;
 
-    // one of a step's copies, given its operands' descriptors
+    // One of a step's copies, given its operands' descriptors.  MM_EXACT_POW2, whose two bodies leave the
+    // fewest registers, forms an offset where it is used; the compiler would keep one for each copy.
     auto copy1 = [&](intx4 da, intx4 db, unsigned st, int j) {
-        if (j < LA) copy16(da, oa + 32 * j * unsigned(a.a.ld), lds0 + st + j * 4096);
-        else copy16(db, ob + 32 * (j - LA) * unsigned(a.b.ld), lds0 + st + j * 4096);
+        unsigned o = j < LA ? oa : ob, ld = unsigned(j < LA ? a.a.ld : a.b.ld);
+        if constexpr (MODE == MM_EXACT_POW2) __asm__ volatile("" : "+v"(o), "+s"(ld));
+        copy16(j < LA ? da : db, o + 32 * (j < LA ? j : j - LA) * ld, lds0 + st + j * 4096);
     };
-    auto desc_a = [&](int kt) { return buffer_of(pa + int64_t(kt) * kQ8Block, na); };
-    auto desc_b = [&](int kt) { return buffer_of(pb + int64_t(kt) * kQ8Block, nb); };
+    // Of the step that reaches past K, rows end with the 16 bytes that hold their last value; a step past
+    // the run has no bytes, and its copies read nothing.
+    auto desc = [&](const uint8_t *p, unsigned n, int kt) {
+        const unsigned cut = unsigned(kQ8Block - min(kQ8Block, a.K - kt * kQ8Block)) & ~15u;
+        return buffer_of(p + int64_t(kt) * kQ8Block, kt < kt1 ? n - cut : 0u);
+    };
     // A step's copies in two parts: what the waves' first halves of rows and columns need, and the rest.
     constexpr int PART = (LA + LB) / 2;
     static_assert(PART % 2 == 0);
@@ -302,38 +314,22 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
         const int h = r < LA / 2 ? HM / 2 : HN / 2, x = r < LA / 2 ? r : r - LA / 2;
         return (r < LA / 2 ? 0 : LA) + x / h * 2 * h + x % h + hi * h;
     };
-    // a whole step; the one that reaches past K gets zeros from there on
-    auto copy_any = [&](int kt, unsigned st) {
-        if (kt < last) {
-            const intx4 da = desc_a(kt), db = desc_b(kt);
+    auto copy_all = [&](int kt, unsigned st) {
+        const intx4 da = desc(pa, na, kt), db = desc(pb, nb, kt);
 #pragma unroll
-            for (int j = 0; j < 2 * PART; ++j) copy1(da, db, st, part_copy(j % PART, j / PART));
-            return;
-        }
-        const int left = a.K - kt * kQ8Block - ck;         // bytes of this lane's 16 that exist
-        if (left >= 16) {                                  // (rows may be shorter than a step here)
-            const unsigned cut = kQ8Block - unsigned(a.K - kt * kQ8Block);
-            const intx4 da = buffer_of(pa + int64_t(kt) * kQ8Block, na - cut);
-            const intx4 db = buffer_of(pb + int64_t(kt) * kQ8Block, nb - cut);
-#pragma unroll
-            for (int j = 0; j < 2 * PART; ++j) copy1(da, db, st, j);
-            return;
-        }
+        for (int j = 0; j < 2 * PART; ++j) copy1(da, db, st, part_copy(j % PART, j / PART));
+    };
+    // Step kt, copied to stage st, waits for its copies if it reaches past K, and each lane clears what lies
+    // past K in what it copied itself: none waits for another, and no branch divides a wave.
+    auto clear_past = [&](int kt, unsigned st) {
+        if (kt != last) return;
+        __builtin_amdgcn_s_waitcnt(0x0F70);                // vmcnt(0)
+        __asm__ volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        const intx4 keep = mask16(a.K - kt * kQ8Block - ck);
 #pragma unroll 1
-        for (int j = 0; j < 2 * PART; j += 4) {
-            intx4 v[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const bool isa = j + u < LA;
-                const int row = 32 * (isa ? j + u : j + u - LA) + cr;
-                v[u] = first16((isa ? pa + int64_t(min(row, a.M - 1 - m0)) * a.a.ld
-                                    : pb + int64_t(min(row, a.N - 1 - n0)) * a.b.ld) +
-                               int64_t(kt) * kQ8Block + ck, left);
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                *reinterpret_cast<intx4 *>(smem + st + wid * 1024 + (j + u) * 4096 + lane * 16) = v[u];
-        }
+        for (int j = 0; j < 2 * PART; ++j)
+            *reinterpret_cast<intx4 *>(smem + st + wid * 1024 + j * 4096 + lane * 16) &= keep;
     };
 
     // Fragment f of an operand: lane l holds bytes 32 (l / 16) .. + 31 of row 16 f + l % 16, in halves.
@@ -355,27 +351,31 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
     constexpr int ES = WORDS ? 1 : 4;           // bytes of a scale
     auto copy_scales = [&](int kt, int s) {
         if (kt >= a.nkt) return;
+        int ln = lane;
+        __asm__ volatile("" : "+v"(ln));                   // addresses are formed here, not kept through all steps
 #pragma unroll
         for (int i = 0; i < (ROWS / 64 + 3) / 4; ++i) {
             const int r0 = 64 * (4 * i + wid);             // rows of the stage, all of A or all of B
             if (r0 >= ROWS) break;
             const bool isa = r0 < BM;
             const Q8View &v = isa ? a.a : a.b;
-            const int o0 = isa ? m0 : n0, left = (isa ? a.M : a.N) - o0, row = (isa ? r0 : r0 - BM) + lane;
+            const int o0 = isa ? m0 : n0, left = (isa ? a.M : a.N) - o0, row = (isa ? r0 : r0 - BM) + ln;
             const int s0 = o0 >> v.shift;                  // scale rows from here on
             const unsigned sld = unsigned(v.sld) * ES;
             const int64_t at = int64_t(s0) * sld + int64_t(kt) * ES;
             const unsigned end = unsigned(((o0 + min(isa ? BM : BN, left) - 1) >> v.shift) - s0) * sld +
-                                 (WORDS ? (unsigned(a.nkt - kt) + 3u) & ~3u : unsigned(a.nkt - kt) * 4u);
-            const uint8_t *const p = static_cast<const uint8_t *>(v.scale) + at;
+                                 (!WORDS ? unsigned(a.nkt - kt) * 4u
+                                         : a.words ? (unsigned(a.nkt - kt) + 3u) & ~3u : unsigned(a.nkt - kt));
+            uint8_t *const p = static_cast<uint8_t *>(v.scale) + at;
             const unsigned off = unsigned(((o0 + row) >> v.shift) - s0) * sld;
             uint8_t *const dst = sbuf + s * S::SCALES + 4 * r0;
             if (WORDS && !a.words) {             // not in whole words: byte by byte
+                const auto d = __builtin_amdgcn_make_buffer_rsrc(p, 0, int(end), 0x00020000);
                 int w = 0;
 #pragma unroll 1
-                for (int k = 0; k < 4 && kt + k < a.nkt; ++k)
-                    if (row < left) w |= int(unsigned(p[off + k]) << (8 * k));
-                *reinterpret_cast<int *>(dst + 4 * lane) = w;
+                for (int k = 0; k < 4; ++k)
+                    w |= int(__builtin_amdgcn_raw_buffer_load_b8(d, int(off) + k, 0, 0)) << (8 * k);
+                *reinterpret_cast<int *>(dst + 4 * ln) = w;
                 continue;
             }
             const intx4 d = buffer_of(p, end);
@@ -387,8 +387,7 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
 
     // whether an exponent of the thread's row of the stage is over 167, the byte of 2^40
     auto scales_past_2_40 = [&]() {
-        static_assert(ROWS <= 256 || MODE != MM_EXACT_POW2, "a row a thread");
-        if (tid >= ROWS) return 0;
+        static_assert(ROWS == 256 || MODE != MM_EXACT_POW2, "a row a thread");
         const bool isa = tid < BM;
         const Q8View &v = isa ? a.a : a.b;
         const int row = isa ? min(m0 + tid, a.M - 1) : min(n0 + tid - BM, a.N - 1);
@@ -416,7 +415,7 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
     // bytes, xn the words of the step after as read.  Otherwise fp32.
     constexpr int XN = FM + (WORDS ? FN : 0);
     int xs[XN], xn[MODE == MM_POW2 ? XN : 1];
-    floatx4 sb[MODE == MM_POW2 || SQ ? 1 : FN];
+    floatx4 sb[WORDS || SQ ? 1 : FN];
     float sq = 0.f, sqn = 0.f;
     auto scales_of = [&](int u) {
         return reinterpret_cast<const int *>(sbuf + ((u >> 2) & 1) * S::SCALES) + (WORDS ? 0 : (u & 3) * ROWS);
@@ -436,7 +435,9 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
         return __int_as_float(value(sc[BM + 16 * FN * wn], sh));
     };
 
-    // Sums of blocks wait for D more to be issued before they are scaled and added.
+    // FOLD: the scales go into the decoded operands.  LATE: sums of blocks wait for D more to be issued
+    // before they are scaled and added.
+    constexpr bool FOLD = MODE == MM_EXACT_POW2, LATE = !WORDS;
     constexpr int NQ = HM * HN, D = EXACT ? 1 : 2;
     floatx4 wp[D], ws[D];
 #pragma unroll
@@ -451,9 +452,8 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
     bf16x8 da[EXACT ? HM : 1][4], db[EXACT ? FN : 1][4];   // EXACT: decoded fragments, once a step
     // A quarter of the wave's tile, fragments i0 .. of A by j0 .. of B; beside(q) issues what goes
     // between its products q and q + 1.  wi, wj: the quarter before.
-    auto quarter = [&]<bool FOLD, int U4>(std::bool_constant<FOLD>, std::integral_constant<int, U4>,
-                                          const Frag (&fa)[HM], const Frag (&fb)[HN], int i0, int j0, auto beside,
-                                          int wi, int wj) {
+    auto quarter = [&]<int U4>(std::integral_constant<int, U4>, const Frag (&fa)[HM], const Frag (&fb)[HN], int i0,
+                               int j0, auto beside, int wi, int wj) {
         if constexpr (EXACT)
             if (j0 == 0)
 #pragma unroll
@@ -504,11 +504,10 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-    // Step kt, whose first fragments are in alo and b0; COPY: the whole of step kt + 2 is copied.
+    // Step kt, whose first fragments are in alo and b0; step kt + 2 is copied.
     // U4: its place among the four steps of a word of scales, -1 if that is not a constant (MM_POW2:
     // a constant picks the word's byte in the instruction, else words are read and shifted each step).
-    auto step = [&]<bool COPY, bool FOLD, int U4>(std::bool_constant<COPY>, std::bool_constant<FOLD> fold,
-                                                  std::integral_constant<int, U4> u4, int kt) {
+    auto step = [&]<int U4>(std::integral_constant<int, U4> u4, int kt) {
         const int u = kt - kt0;
         const unsigned cur = (u & 1) * STAGE, nxt = STAGE - cur;
         if (U4 < 0 ? (u & 3) == 0 : U4 == 0) copy_scales(kt + 4, ((u >> 2) & 1) ^ 1);
@@ -522,18 +521,14 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
         };
         // A part is copied a step and a half before it is needed: the two parts copied since may be
         // on their way (the scales' copies among them only make a wait longer).
-        constexpr int LEFT = COPY ? 2 * PART : 0;
-        intx4 da, db;
-        if constexpr (COPY) {
-            da = desc_a(kt + 2);
-            db = desc_b(kt + 2);
-        }
+        constexpr int LEFT = 2 * PART;
+        const intx4 da = desc(pa, na, kt + 2), db = desc(pb, nb, kt + 2);
         const int *const sc = scales_of(u), *const scn = scales_of(u + 1);
         const int sh = 8 * (u & 3), shn = 8 * ((u + 1) & 3);
         // Each half of the fragments and scales is replaced once its last product is issued
-        quarter(fold, u4, alo, b0, 0, 0, [&](int q) {
+        quarter(u4, alo, b0, 0, 0, [&](int q) {
             spread(q, 2 * HN, [&](int r) { b1[r >> 1].h[r & 1] = half(cur, fb0, HN + (r >> 1), r & 1); });
-            if constexpr (COPY) spread(q, PART, [&](int r) { copy1(da, db, cur, part_copy(r, 0)); });
+            spread(q, PART, [&](int r) { copy1(da, db, cur, part_copy(r, 0)); });
             if constexpr (U4 == 0) {
                 spread(q, HN, [&](int f) { xs[FM + HN + f] = word_of(sc, FM + HN + f); });
                 spread(q, HM, [&](int f) { xs[HM + f] = word_of(sc, HM + f); });
@@ -547,23 +542,23 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
                 spread(q, HM, [&](int f) { xs[HM + f] = scale_of_a(sc, HM + f, sh); });
             }
         }, HM, HN);
-        quarter(fold, u4, alo, b1, 0, HN, [&](int q) {
+        quarter(u4, alo, b1, 0, HN, [&](int q) {
             spread(q, 2 * HM, [&](int r) { ahi[r >> 1].h[r & 1] = half(cur, fa0, HM + (r >> 1), r & 1); });
             if constexpr (MODE == MM_POW2 && U4 < 0) spread(q, XN, [&](int f) { xn[f] = word_of(scn, f); });
         }, 0, 0);
         // Every wave has read the second part of this step, which is copied over now, and the first
         // part of the next has arrived.
         stage_barrier<LEFT>();
-        quarter(fold, u4, ahi, b0, HM, 0, [&](int q) {
-            if constexpr (COPY) spread(q, PART, [&](int r) { copy1(da, db, cur, part_copy(r, 1)); });
+        quarter(u4, ahi, b0, HM, 0, [&](int q) {
+            spread(q, PART, [&](int r) { copy1(da, db, cur, part_copy(r, 1)); });
             spread(q, 2 * HM, [&](int r) { alo[r >> 1].h[r & 1] = half(nxt, fa0, r >> 1, r & 1); });
             if constexpr (U4 == 3) spread(q, HM, [&](int f) { xs[f] = word_of(scn, f); });
             if constexpr (MODE != MM_POW2) {
                 spread(q, HM, [&](int f) { xs[f] = scale_of_a(scn, f, shn); });
-                if (SQ && !FOLD && q == 0) sqn = scale_of_square(scn, shn);
+                if (SQ && q == 0) sqn = scale_of_square(scn, shn);
             }
         }, 0, HN);
-        quarter(fold, u4, ahi, b1, HM, HN, [&](int q) {
+        quarter(u4, ahi, b1, HM, HN, [&](int q) {
             spread(q, 2 * HN, [&](int r) { b0[r >> 1].h[r & 1] = half(nxt, fb0, r >> 1, r & 1); });
             if constexpr (U4 >= 0) {
                 if constexpr (U4 == 3) spread(q, HN, [&](int f) { xs[FM + f] = word_of(scn, FM + f); });
@@ -576,12 +571,20 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
                 spread(q, HN, [&](int f) { sb[f] = scale_of_b(scn, f, shn); });
             }
         }, HM, 0);
-        if constexpr (SQ && !FOLD) sq = sqn;
+        if constexpr (SQ) sq = sqn;
         // likewise the first part of the next step, and the second has arrived
         stage_barrier<LEFT>();
     };
 
-    auto run = [&]<bool FOLD>(std::bool_constant<FOLD> fold) {
+    auto run = [&] {
+#pragma unroll
+        for (int f = 0; f < HM; ++f)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) alo[f].h[h] = half(0, fa0, f, h);
+#pragma unroll
+        for (int f = 0; f < HN; ++f)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) b0[f].h[h] = half(0, fb0, f, h);
         const int *const sc = scales_of(0);
         if constexpr (MODE == MM_POW2) {
 #pragma unroll
@@ -600,60 +603,82 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
             }
         }
         int kt = kt0;
-        const int whole = min(kt1, last);
         const std::integral_constant<int, -1> any;
         // (in larger tiles four steps in one are more than the register allocator keeps in place)
         if constexpr (MODE == MM_POW2 && FM * FN <= 16) {
 #pragma unroll 1
-            for (; kt + 5 < whole; kt += 4) {
-                step(std::true_type{}, fold, std::integral_constant<int, 0>{}, kt);
-                step(std::true_type{}, fold, std::integral_constant<int, 1>{}, kt + 1);
-                step(std::true_type{}, fold, std::integral_constant<int, 2>{}, kt + 2);
-                step(std::true_type{}, fold, std::integral_constant<int, 3>{}, kt + 3);
+            for (; kt + 4 <= kt1 && kt + 4 < last; kt += 4) {
+                step(std::integral_constant<int, 0>{}, kt);
+                step(std::integral_constant<int, 1>{}, kt + 1);
+                step(std::integral_constant<int, 2>{}, kt + 2);
+                step(std::integral_constant<int, 3>{}, kt + 3);
             }
             const int *const next = scales_of(kt - kt0);
 #pragma unroll
             for (int f = 0; f < XN; ++f) xn[f] = word_of(next, f);
         }
 #pragma unroll 1
-        for (; kt + 2 < whole; ++kt) step(std::true_type{}, fold, any, kt);
-#pragma unroll 1
         for (; kt < kt1; ++kt) {
-            step(std::false_type{}, fold, any, kt);
-            // the step that reaches past K, half a step later than the others
-            if (kt + 2 < kt1) copy_any(kt + 2, ((kt - kt0) & 1) * STAGE);
+            clear_past(kt + 1, ((kt - kt0) & 1 ^ 1) * STAGE);
+            step(any, kt);
         }
-        // the last step read ahead into a stage that nothing was copied to; its values are unused
-        if constexpr (MODE != MM_POW2 && !FOLD)
+        // the last step read ahead into a stage of a step past the run; its values are unused
+        if constexpr (LATE)
 #pragma unroll
             for (int d = 0; d < D; ++d) add_block(HM + qi(NQ - D + d), HN + qj(NQ - D + d), wp[d], ws[d]);
     };
+    // MM_EXACT_POW2 with larger scales than fit the decoded operands, which no layer's values have: each
+    // step's sums are scaled, nothing overlaps, and fragments are read where they are used.
+    auto run_unfolded = [&] {
+#pragma unroll 1
+        for (int kt = kt0; kt < kt1; ++kt) {
+            const int u = kt - kt0, sh = 8 * (u & 3);
+            const unsigned cur = (u & 1) * STAGE;
+            const int *const sc = scales_of(u);
+            if ((u & 3) == 0) copy_scales(kt + 4, ((u >> 2) & 1) ^ 1);
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                bf16x8 ea[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const intx4 v = half(cur, fa0, i, k >> 1);
+                    ea[k] = to_bf16<FA>(v[2 * (k & 1)], v[2 * (k & 1) + 1]);
+                }
+                const float x = __int_as_float(scale_of_a(sc, i, sh));
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    floatx4 p = {0, 0, 0, 0};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const intx4 v = half(cur, fb0, j, k >> 1);
+                        p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16<FB>(v[2 * (k & 1)], v[2 * (k & 1) + 1]),
+                                                                    ea[k], p, 0, 0, 0);
+                    }
+                    const floatx4 w = x * scale_of_b(sc, j, sh);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(p[e], w[e], acc[i][j][e]);
+                    __asm__ volatile("" ::: "memory");     // (kept from one i to the next they would not fit)
+                }
+            }
+            clear_past(kt + 1, STAGE - cur);
+            stage_barrier<0>();                            // step kt is read, step kt + 1 has arrived
+            copy_all(kt + 2, cur);
+        }
+    };
     if (kt0 < kt1) {
         copy_scales(kt0, 0);
-        copy_any(kt0, 0);
-        if (kt0 + 1 < kt1) copy_any(kt0 + 1, STAGE);
+        copy_all(kt0, 0);
+        copy_all(kt0 + 1, STAGE);
         // MM_EXACT_POW2: scales of at most 2^40 go into the decoded operands, which then meet neither
         // the largest bf16 number nor, while the values that they stand for are normal fp32 numbers,
         // the smallest; the sums need no scaling any more (4096x8192x8192, both operands 1x128: 15 % less time).
-        bool small = false;
+        bool small = true;
         if constexpr (MODE == MM_EXACT_POW2) small = !__syncthreads_or(scales_past_2_40());
-        // (with fewer steps, or one that reaches past K among them, fewer copies are on their way)
-        if (kt0 + 1 < min(kt1, last)) stage_barrier<2 * PART>();
-        else stage_barrier<0>();
-#pragma unroll
-        for (int f = 0; f < HM; ++f)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) alo[f].h[h] = half(0, fa0, f, h);
-#pragma unroll
-        for (int f = 0; f < HN; ++f)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) b0[f].h[h] = half(0, fb0, f, h);
-        if constexpr (MODE == MM_EXACT_POW2) {
-            if (small) run(std::true_type{});
-            else run(std::false_type{});
-        } else {
-            run(std::false_type{});
-        }
+        clear_past(kt0, 0);
+        stage_barrier<2 * PART>();
+        if (small) run();
+        else run_unfolded();
+        stage_barrier<0>();                                // of the copies for steps past the run
     }
 
     // Lane l holds columns 4 (l / 16) .. + 3 of row l % 16 of each 16 x 16 block.  Rows of blocks go
@@ -845,7 +870,7 @@ int mm_tiles(Q8MatArgs &g, hipStream_t stream) {
     }
     const int rc = split(g, mm_splits(g, exact ? 1.0 : 0.5), 4, stream);
     if (rc != DS_OK) return rc;
-    if (exact) return pow2 ? mm_square<4, 4, MM_EXACT_POW2>(g, stream) : mm_square<4, 4, MM_EXACT_F32>(g, stream);
+    if (exact) return pow2 ? mm_launch<4, 4, MM_EXACT_POW2, false>(g, stream) : mm_square<4, 4, MM_EXACT_F32>(g, stream);
     return pow2 ? mm_launch<4, 4, MM_POW2, false>(g, stream) : mm_square<4, 4, MM_F32>(g, stream);
 }
 

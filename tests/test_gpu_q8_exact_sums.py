@@ -1,0 +1,63 @@
+"""8-bit products of small whole numbers, whose sums every kernel has to give exactly: values in {-1, 0, 1}
+and scales of 1 and 2 a block, so that no sum passes 2048, up to where fp16 holds every whole number, and no
+group of products needs more bits than the 8-bit instructions keep.  One product left out, or taken twice, shows."""
+import numpy as np
+import pytest
+
+from oracle import q8
+from test_gpu_q8 import env, make  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+ONE = {q8.E4M3: 0x38, q8.E5M2: 0x3C}
+
+
+def whole(torch, L, rng, rows, cols, fmt, kind, block_rows):
+    """A Q8 of such values between NaN-coded edges, and the values."""
+    m = make(torch, L, rows, cols, fmt, kind, block_rows)
+    m.store.fill_(0x7F)
+    v = rng.integers(-1, 2, (rows, cols)).astype(np.int8)
+    codes = np.where(v == 0, 0, ONE[fmt] | np.where(v < 0, 0x80, 0)).astype(np.uint8)
+    m.store[:rows, :cols] = torch.from_numpy(codes).cuda()
+    e = rng.integers(0, 2, tuple(m.scale.shape))
+    if kind == q8.POW2:
+        m.sc.view(torch.uint8)[:] = 255
+        m.scale.view(torch.uint8).copy_(torch.from_numpy((127 + e).astype(np.uint8)))
+    else:
+        m.sc[:] = float("nan")
+        m.scale.copy_(torch.from_numpy((2.0 ** e).astype(np.float32)))
+    return m, (v * q8.spread(2.0 ** e, rows, cols, block_rows)).astype(np.float32)
+
+
+@pytest.mark.parametrize("mkn", [(33, 300, 64), (130, 1003, 260), (70, 5000, 64), (200, 640, 130)])
+@pytest.mark.parametrize("tight", [False, True])
+def test_scales_past_two_to_the_forty(env, mkn, tight):  # noqa: F811
+    """Scales of 2^90 in a few rows of one operand and of 2^-30 in the other; rows of scales that do
+    and do not start at words of four."""
+    torch, L = env
+    M, K, N = mkn
+    rng = np.random.default_rng(M + K + N + tight)
+    a, av = whole(torch, L, rng, M, K, q8.E4M3, q8.POW2, 1)
+    b, bv = whole(torch, L, rng, N, K, q8.E5M2, q8.POW2, 1)
+    rows = rng.integers(0, min(M, 128), 3)
+    a.scale.view(torch.uint8)[rows] += 90
+    av[rows] *= 2.0 ** 90
+    a.scale.view(torch.uint8)[rows[0], 0] -= 90
+    av[rows[0], :128] *= 2.0 ** -90
+    b.scale.view(torch.uint8)[:] -= 30
+    want = av.astype(np.float64) @ (bv.astype(np.float64) * 2.0 ** -30).T
+    if tight:
+        nb = -(-K // 128)
+        for m in (a, b):
+            raw = torch.empty(1 + m.rows * nb, dtype=torch.uint8, device="cuda")
+            view = raw[1:].view(m.rows, nb)
+            view.copy_(m.scale.view(torch.uint8))
+            m.tight = L.Q8.of(m.data, view.view(torch.float8_e8m0fnu))
+        a, b = a.tight, b.tight
+    c = torch.empty(M, N, device="cuda")
+    L.ds_q8_matmul(a, b, c)
+    torch.cuda.synchronize()
+    # rows[0] mixes 2^90 and 1: its sums are rounded to fp32 at most once a block
+    got, lim = c.double().cpu().numpy(), np.zeros((M, N))
+    lim[rows[0]] = (K // 128 + 2) * 2.0 ** -24 * (np.abs(av[rows[0]]).astype(np.float64) @ np.abs(bv).T * 2.0 ** -30)
+    assert (np.abs(got - want) <= lim).all()

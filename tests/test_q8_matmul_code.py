@@ -2,7 +2,10 @@
 
 Copies from memory to LDS are statements of their own, into which the compiler puts no waits.  Such a
 copy takes its LDS address from m0, with one instruction at least between a scalar write of m0 and the
-copy, and its descriptor from scalar registers, five after a vector instruction that wrote one."""
+copy, and its descriptor from scalar registers, five after a vector instruction that wrote one.
+
+No vector register goes to scratch memory: one that is loaded again where a branch has switched lanes off
+leaves those lanes with a wild value, and such loads stand in the counter that the copies' waits use."""
 import os
 import re
 import subprocess
@@ -103,6 +106,13 @@ def test_copies_wait_for_their_scalars(compiled):
         total += copies
         assert not early, early[:3]
     assert total > 0
+
+
+def test_no_kernel_spills(compiled):
+    names = re.findall(r"Function Name: (\S+)", compiled[1])
+    scratch = re.findall(r"ScratchSize \[bytes/lane\]: (\d+)", compiled[1])
+    assert len(names) == len(scratch) >= 45
+    assert not {n: s for n, s in zip(names, scratch) if s != "0"}
 
 
 def test_nothing_else_is_warned_of(compiled):
