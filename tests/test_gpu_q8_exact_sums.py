@@ -29,6 +29,32 @@ def whole(torch, L, rng, rows, cols, fmt, kind, block_rows):
     return m, (v * q8.spread(2.0 ** e, rows, cols, block_rows)).astype(np.float32)
 
 
+# one row to 32, tiles of 128 x 128 (whole, ragged, split), of 256 x 128 and of 256 x 256, and
+# reductions that end inside a step, inside 16 bytes, and after less than one step
+SHAPES = [(1, 4000, 70), (9, 8200, 300), (31, 1001, 8300), (40, 4100, 130), (128, 128, 128), (130, 77, 260),
+          (256, 1111, 384), (1003, 777, 1501), (100, 5000, 200), (2048, 1152, 4096), (2001, 1111, 4000),
+          (4096, 1024, 4096), (3900, 1003, 4001)]
+
+
+@pytest.mark.parametrize("mkn", SHAPES)
+@pytest.mark.parametrize("kind", [q8.POW2, q8.F32])
+def test_sums_are_exact(env, mkn, kind):  # noqa: F811
+    torch, L = env
+    M, K, N = mkn
+    rng = np.random.default_rng(M + 3 * K + N + kind)
+    for fa, fb, ra, rb, name in ((0, 0, 1, 128, "float16"), (1, 0, 1, 1, "float32"), (0, 1, 128, 1, "float16")):
+        print("exact sums", mkn, kind, fa, fb, ra, rb, name, flush=True)
+        a, av = whole(torch, L, rng, M, K, fa, kind, ra)
+        b, bv = whole(torch, L, rng, N, K, fb, kind, rb)
+        want = av @ bv.T                               # whole numbers below 2^24: exact in fp32
+        assert np.max(np.abs(want)) <= 2048
+        c = torch.full((M + 1, (N + 15) // 8 * 8), float("nan"), dtype=getattr(torch, name), device="cuda")
+        L.ds_q8_matmul(a, b, c[:M, :N])
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(c[:M, :N].float().cpu().numpy(), want)
+        assert torch.isnan(c[M:]).all() and torch.isnan(c[:, N:]).all(), "wrote past C"
+
+
 @pytest.mark.parametrize("mkn", [(33, 300, 64), (130, 1003, 260), (70, 5000, 64), (200, 640, 130)])
 @pytest.mark.parametrize("tight", [False, True])
 def test_scales_past_two_to_the_forty(env, mkn, tight):  # noqa: F811
