@@ -651,7 +651,11 @@ class Q8:
     ``block_rows=128``, each 128x128 square): ``data`` [rows, cols] of
     ``torch.float8_e4m3fn`` or ``float8_e5m2`` and ``scale`` [ceil(rows / block_rows),
     ceil(cols / 128)] of ``torch.float8_e8m0fnu`` (powers of two) or ``float32``.
-    Q8(rows, cols) allocates both, uninitialised; Q8.of wraps tensors that exist."""
+    Q8(rows, cols) allocates both, uninitialised; Q8.of wraps tensors that exist.
+
+    The operators below run on the one GPU that holds their operands, on its current
+    stream unless one is given, and raise ValueError for operands in host memory or on
+    several GPUs."""
 
     def __init__(self, rows, cols, dtype=None, *, scale=None, block_rows=1, device="cuda"):
         dtype = dtype or _torch.float8_e4m3fn
@@ -689,6 +693,7 @@ class Q8:
             ld = max(ld, (cols + 15) // 16 * 16)
         self.data, self.scale, self.rows, self.cols = data, scale, rows, cols
         self.block_rows = block_rows
+        self._device = data.get_device()
         self._c = ds_q8(data.data_ptr(), scale.data_ptr(), rows, cols, ld, sld, fmt, kind, block_rows, 0)
         self._p = C.addressof(self._c)
 
@@ -719,24 +724,41 @@ def _plain(t):
     return (t.data_ptr(), _PLAIN[t.dtype], *_plain_rows(t))
 
 
+def _q8_device(first, *rest):
+    """The one GPU of operands with these device indices (-1: host memory, None: no operand)."""
+    one = first >= 0
+    for d in rest:
+        one = one and (d is None or d == first)
+    if not one:
+        raise ValueError("operands on " + ", ".join("the host" if d < 0 else f"GPU {d}" for d in (first, *rest)
+                                                    if d is not None) + ", not on one GPU")
+    return first
+
+
 # the current stream's handle without a Stream object (2.5 us of a call's 7)
 _raw_stream = getattr(getattr(_torch, "_C", None), "_cuda_getCurrentRawStream", None)
 
 
-def _q8_stream(stream):
+def _q8_stream(stream, dev):
     if stream is not None:
+        if getattr(stream, "device_index", dev) != dev:
+            raise ValueError(f"a stream of GPU {stream.device_index}, operands on GPU {dev}")
         return stream_handle(stream)
     if _raw_stream is not None:
-        return _raw_stream(_torch.cuda.current_device())
-    return _torch.cuda.current_stream().cuda_stream
+        return _raw_stream(dev)
+    return _torch.cuda.current_stream(dev).cuda_stream
 
 
 def ds_q8_quantize(x, row=None, col=None, stream=None):
     """x [rows, cols] (fp32, fp16, bf16) in 8 bits: in row (a Q8 of x's shape), transposed in
     col (a Q8 of cols x rows), or both."""
     p, t, rows, cols, ld = _plain(x)
+    dev = _q8_device(x.get_device(), row and row._device, col and col._device)
+    if dev != _torch.cuda.current_device():
+        with _torch.cuda.device(dev):
+            return ds_q8_quantize(x, row, col, stream)
     return check("ds_q8_quantize", lib.ds_q8_quantize(p, t, rows, cols, ld, row and row._p,
-                                                      col and col._p, _q8_stream(stream)))
+                                                      col and col._p, _q8_stream(stream, dev)))
 
 
 def ds_q8_matmul(a, b, c, stream=None):
@@ -744,7 +766,11 @@ def ds_q8_matmul(a, b, c, stream=None):
     p, t, rows, cols, ld = _plain(c)
     if rows != a.rows or cols != b.rows:
         raise ValueError(f"c is {rows} x {cols}, not {a.rows} x {b.rows}")
-    return check("ds_q8_matmul", lib.ds_q8_matmul(a._p, b._p, p, t, ld, _q8_stream(stream)))
+    dev = _q8_device(c.get_device(), a._device, b._device)
+    if dev != _torch.cuda.current_device():
+        with _torch.cuda.device(dev):
+            return ds_q8_matmul(a, b, c, stream)
+    return check("ds_q8_matmul", lib.ds_q8_matmul(a._p, b._p, p, t, ld, _q8_stream(stream, dev)))
 
 
 def ds_swiglu8(gu, h, saved=None, stream=None):
@@ -753,8 +779,12 @@ def ds_swiglu8(gu, h, saved=None, stream=None):
     p, t, rows, cols, ld = _plain(gu)
     if rows != h.rows:
         raise ValueError(f"gu has {rows} rows, h {h.rows}")
+    dev = _q8_device(gu.get_device(), h._device, saved and saved._device)
+    if dev != _torch.cuda.current_device():
+        with _torch.cuda.device(dev):
+            return ds_swiglu8(gu, h, saved, stream)
     return check("ds_swiglu8", lib.ds_swiglu8(p, t, rows, h.cols, cols - h.cols, ld, h._p,
-                                              saved and saved._p, _q8_stream(stream)))
+                                              saved and saved._p, _q8_stream(stream, dev)))
 
 
 def ds_swiglu8_grad(saved, dh, dgu=None, dgu_t=None, h_t=None, stream=None):
@@ -763,9 +793,14 @@ def ds_swiglu8_grad(saved, dh, dgu=None, dgu_t=None, h_t=None, stream=None):
     p, t, rows, cols, ld = _plain(dh)
     if rows != saved.rows:
         raise ValueError(f"dh has {rows} rows, saved {saved.rows}")
+    dev = _q8_device(dh.get_device(), saved._device, dgu and dgu._device, dgu_t and dgu_t._device,
+                     h_t and h_t._device)
+    if dev != _torch.cuda.current_device():
+        with _torch.cuda.device(dev):
+            return ds_swiglu8_grad(saved, dh, dgu, dgu_t, h_t, stream)
     return check("ds_swiglu8_grad",
                  lib.ds_swiglu8_grad(saved._p, p, t, cols, saved.cols - cols, ld, dgu and dgu._p,
-                                     dgu_t and dgu_t._p, h_t and h_t._p, _q8_stream(stream)))
+                                     dgu_t and dgu_t._p, h_t and h_t._p, _q8_stream(stream, dev)))
 
 
 def ds_gen_uniform(seed, n):
