@@ -236,7 +236,9 @@ int sched_space_programs(const ds_space *space, uint64_t *keys, int32_t *instanc
  * Asynchronous on stream; y is overwritten.  An empty output launches nothing.
  * A split reduction (ks > 1) writes its partial outputs to a workspace the
  * library keeps per (device, stream): split launches on different streams do
- * not share partials.  When a stream's workspace is too small it is replaced
+ * not share partials, and host threads may share a stream (a thread has a
+ * workspace of its own for hipStreamPerThread, and ds_measure keeps a stream's
+ * for as long as it measures).  When a stream's workspace is too small it is replaced
  * by a larger one (hipMalloc; the old one is kept until ds_shutdown, since a
  * graph captured earlier may still use it, and the stream is synchronised
  * first).  Under stream capture nothing may be allocated: a split schedule

@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <mutex>
 #include <string>
 #include <vector>
 
@@ -17,8 +18,11 @@ const char *last_error();
 bool hip_ok(hipError_t e, const char *what);
 
 // ---- per-device state (harness.hip) -------------------------------------------
+// Keeps a split workspace for the calling thread: held until the launch that writes the partial sums and
+// the one that joins them are both queued, so that no other thread's come between.
+using SplitHold = std::unique_lock<std::mutex>;
 // The workspace of split reductions on `stream`, at least `elems` floats.
-int split_workspace(int64_t elems, hipStream_t stream, float **out);
+int split_workspace(int64_t elems, hipStream_t stream, float **out, SplitHold &hold);
 // Allows `func` launches with `lds` bytes of dynamic LDS (above 64 KiB).
 int ensure_lds_attr(const void *func, int lds);
 

@@ -8,6 +8,8 @@
 #include <map>
 #include <mutex>
 #include <set>
+#include <thread>
+#include <tuple>
 #include <utility>
 #include <vector>
 
@@ -165,14 +167,16 @@ std::mutex g_mu;
 unsigned *g_parity_buf[kMaxDevices];     // 4 words per device, library-owned
 hipStream_t g_graph_stream[kMaxDevices];  // capture / replay stream per device
 // Partial outputs of split reductions: one buffer per (device, stream), so
-// split launches on different streams never share partials.  A buffer that
+// split launches on different streams never share partials; a thread's own for
+// hipStreamPerThread, one handle that is another stream in each.  A buffer that
 // grows is retired, not freed: a graph the caller captured earlier may still
 // hold its address.  Retired and live buffers are freed by ds_shutdown.
 struct SplitWs {
+    std::mutex mu;
     float *p = nullptr;
     int64_t elems = 0;
 };
-std::map<std::pair<int, hipStream_t>, SplitWs> g_split_ws;
+std::map<std::tuple<int, hipStream_t, std::thread::id>, SplitWs> g_split_ws;
 std::vector<std::pair<int, void *>> g_split_retired;
 std::set<std::pair<int, const void *>> g_lds_attr;
 
@@ -230,12 +234,18 @@ int graph_stream(hipStream_t *out) {
 // while the stream is being captured nothing may be allocated, so a capture
 // needs the buffer to exist already (one uncaptured call of the same schedule
 // on that stream creates it).
-int split_workspace(int64_t elems, hipStream_t stream, float **out) {
+int split_workspace(int64_t elems, hipStream_t stream, float **out, SplitHold &hold) {
     int dev;
     int rc = current_device(dev);
     if (rc != DS_OK) return rc;
-    std::lock_guard<std::mutex> lk(g_mu);
-    SplitWs &ws = g_split_ws[{dev, stream}];
+    const std::thread::id own = stream == hipStreamPerThread ? std::this_thread::get_id() : std::thread::id();
+    SplitWs *found;
+    {
+        std::lock_guard<std::mutex> lk(g_mu);
+        found = &g_split_ws[{dev, stream, own}];
+    }
+    SplitWs &ws = *found;
+    hold = SplitHold(ws.mu);
     if (ws.elems < elems) {
         hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
         if (!hip_ok(hipStreamIsCapturing(stream, &cap), "hipStreamIsCapturing")) return DS_EHIP;
@@ -255,6 +265,7 @@ int split_workspace(int64_t elems, hipStream_t stream, float **out) {
                 (void)hipFree(p);
                 return DS_EHIP;
             }
+            std::lock_guard<std::mutex> lk(g_mu);
             g_split_retired.emplace_back(dev, ws.p);
         }
         ws.p = static_cast<float *>(p);
@@ -701,11 +712,11 @@ void set_workspace(Plan &plan, float *part) {
     else plan.mm.part = part;
 }
 
-int attach_workspace(Plan &plan, hipStream_t stream) {
+int attach_workspace(Plan &plan, hipStream_t stream, SplitHold &hold) {
     const int64_t elems = workspace_elems(plan);
     if (elems == 0) return DS_OK;
     float *part = nullptr;
-    const int rc = split_workspace(elems, stream, &part);
+    const int rc = split_workspace(elems, stream, &part, hold);
     if (rc != DS_OK) return rc;
     set_workspace(plan, part);
     return DS_OK;
@@ -798,7 +809,8 @@ int kernel_run(int op, const ds_sched *s, const float *x, const float *w, float 
         set_error("null buffer");
         return DS_EINVAL;
     }
-    rc = attach_workspace(plan, stream);
+    SplitHold hold;
+    rc = attach_workspace(plan, stream, hold);
     if (rc != DS_OK) return rc;
     return launch_plan(plan, stream);
 }
@@ -925,7 +937,8 @@ int ds_measure(const ds_sched *s, const ds_tune_io *io, const ds_measure_cfg *cf
         set_error("null buffer");
         return DS_EINVAL;
     }
-    rc = attach_workspace(plan, io->stream);
+    SplitHold hold;                          // while it measures
+    rc = attach_workspace(plan, io->stream, hold);
     if (rc != DS_OK) {
         out->status = rc;
         return DS_OK;
@@ -1219,7 +1232,7 @@ void ds_shutdown(void) {
     if (hipGetDevice(&cur) != hipSuccess) return;
     for (int d = 0; d < kMaxDevices; ++d) {
         bool ws = false;
-        for (auto &e : g_split_ws) ws = ws || e.first.first == d;
+        for (auto &e : g_split_ws) ws = ws || std::get<0>(e.first) == d;
         for (auto &e : g_split_retired) ws = ws || e.first == d;
         if (!g_parity_buf[d] && !g_graph_stream[d] && !ws) continue;
         if (hipSetDevice(d) == hipSuccess) {
@@ -1227,7 +1240,7 @@ void ds_shutdown(void) {
             if (g_parity_buf[d]) (void)hipFree(g_parity_buf[d]);
             if (g_graph_stream[d]) (void)hipStreamDestroy(g_graph_stream[d]);
             for (auto &e : g_split_ws)
-                if (e.first.first == d && e.second.p) (void)hipFree(e.second.p);
+                if (std::get<0>(e.first) == d && e.second.p) (void)hipFree(e.second.p);
             for (auto &e : g_split_retired)
                 if (e.first == d) (void)hipFree(e.second);
         }

@@ -791,12 +791,12 @@ int by_formats(int fa, int fb, Fn fn) {
 }
 
 // Splits the reduction into `ks` runs of a multiple of `unit` steps, whose partial products go to
-// the stream's workspace.
-int split(Q8MatArgs &g, int ks, int unit, hipStream_t stream) {
+// the stream's workspace, held until they are joined.
+int split(Q8MatArgs &g, int ks, int unit, hipStream_t stream, SplitHold &hold) {
     if (ks <= 1) return DS_OK;
     g.kps = ((g.nkt + ks - 1) / ks + unit - 1) / unit * unit;
     g.ks = (g.nkt + g.kps - 1) / g.kps;
-    return g.ks > 1 ? split_workspace(int64_t(g.ks) * g.M * g.N, stream, &g.part) : DS_OK;
+    return g.ks > 1 ? split_workspace(int64_t(g.ks) * g.M * g.N, stream, &g.part, hold) : DS_OK;
 }
 
 int join(const Q8MatArgs &g, hipStream_t stream) {
@@ -868,7 +868,8 @@ int mm_tiles(Q8MatArgs &g, hipStream_t stream) {
         if (large <= tall && large <= small) return mm_launch<8, 8, MM_POW2, false>(g, stream);
         if (tall <= small) return mm_launch<8, 4, MM_POW2, false>(g, stream);
     }
-    const int rc = split(g, mm_splits(g, exact ? 1.0 : 0.5), 4, stream);
+    SplitHold hold;
+    const int rc = split(g, mm_splits(g, exact ? 1.0 : 0.5), 4, stream, hold);
     if (rc != DS_OK) return rc;
     if (exact) return pow2 ? mm_launch<4, 4, MM_EXACT_POW2, false>(g, stream) : mm_square<4, 4, MM_EXACT_F32>(g, stream);
     return pow2 ? mm_launch<4, 4, MM_POW2, false>(g, stream) : mm_square<4, 4, MM_F32>(g, stream);
@@ -886,8 +887,9 @@ int few_launch(Q8MatArgs &g, int waves, hipStream_t stream) {
 int few(Q8MatArgs &g, hipStream_t stream) {
     // Few columns under a long reduction leave most CUs idle: it is split over workgroups too
     // (8x512x16384 17.8 -> 10.4 us, 16x2048x8192 12.6 -> 11.5; 16x4096x16384 would go from 25 to 28).
+    SplitHold hold;
     if (g.N <= 2048 && g.nkt >= 64) {
-        const int rc = split(g, std::min(g.nkt / 16, 8), 4, stream);
+        const int rc = split(g, std::min(g.nkt / 16, 8), 4, stream, hold);
         if (rc != DS_OK) return rc;
     }
     // 32 columns a workgroup read A half as often and are enough workgroups in wide layers
