@@ -414,7 +414,9 @@ __global__ __launch_bounds__(kTileThreads, WHOLE ? 6 : 5) void q8_tile(const T *
 
 // 1 / (1 + exp(-g)).  exp(-g) = 2^(hi + lo), hi the rounded product with log2(e) and lo what the
 // rounding and the constant leave out, so the error does not grow with |g|.  Beyond +-88.5, where
-// the result is 1 or less than any normal number, g is taken as that, and all steps are finite.
+// the result is 1 or less than any normal number, g is taken as that, and all steps are finite; the
+// reciprocal instruction gives 0 in place of a subnormal number, so that g sigmoid(g) is 0 there too,
+// however large |g| is (tests/test_gpu_q8_tails.py).
 __device__ __forceinline__ float sigmoid(float g) {
     const float L = 1.44269502f, L2 = 1.92596299e-8f;      // log2(e) in two parts
     g = __builtin_amdgcn_fmed3f(g, -88.5f, 88.5f);
