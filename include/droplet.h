@@ -579,6 +579,7 @@ enum {
 };
 
 #define DS_Q8_BLOCK 128
+#define DS_EXACT_SUMS 256    /* added to the type of ds_q8_matmul's C */
 
 /* An 8-bit matrix in device memory (a plain value; the buffers are the caller's).
  * data: 16-byte aligned, ld >= cols a multiple of 16, below 2^24; bytes past cols
@@ -621,8 +622,9 @@ int ds_q8_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t 
  * comes from the 8-bit matrix instructions, which align each eight products to their
  * largest and keep about 14 bits of them: 1e-5 to 1e-4 of the result for normal and for
  * heavy-tailed values, against 2^-9 and 2^-12 of the rounding to bf16 and fp16.  An fp32
- * C, or one of fewer rows, comes from bf16 matrix instructions on the same values, whose
- * sums are exact to fp32.  The product of two scales has to be an fp32 number; an operand's
+ * C, one of fewer rows, or any C whose type has DS_EXACT_SUMS added, comes from bf16 matrix
+ * instructions on the same values, whose sums are exact to fp32 (in about twice the time of a
+ * large 16-bit C).  The product of two scales has to be an fp32 number; an operand's
  * values (byte times scale) below 2^-126 may count as 0.
  * Few output tiles under a long reduction split it over workgroups and join the
  * partial sums in order in a workspace as kernel_run keeps (and under the same rule

@@ -50,6 +50,7 @@ DS_TYPE_F32, DS_TYPE_F16, DS_TYPE_BF16 = 0, 1, 2
 DS_Q8_E4M3, DS_Q8_E5M2 = 0, 1
 DS_SCALE_POW2, DS_SCALE_F32 = 0, 1
 DS_Q8_BLOCK = 128
+DS_EXACT_SUMS = 256
 
 
 class ds_q8(C.Structure):
@@ -761,15 +762,18 @@ def ds_q8_quantize(x, row=None, col=None, stream=None):
                                                       col and col._p, _q8_stream(stream, dev)))
 
 
-def ds_q8_matmul(a, b, c, stream=None):
-    """c = a b^T of two Q8; c fp32, fp16 or bf16."""
+def ds_q8_matmul(a, b, c, stream=None, exact=False):
+    """c = a b^T of two Q8; c fp32, fp16 or bf16.  exact: sums exact to fp32 for a 16-bit c of any
+    size, as an fp32 c and one of few rows always have them."""
     p, t, rows, cols, ld = _plain(c)
     if rows != a.rows or cols != b.rows:
         raise ValueError(f"c is {rows} x {cols}, not {a.rows} x {b.rows}")
     dev = _q8_device(c.get_device(), a._device, b._device)
     if dev != _torch.cuda.current_device():
         with _torch.cuda.device(dev):
-            return ds_q8_matmul(a, b, c, stream)
+            return ds_q8_matmul(a, b, c, stream, exact)
+    if exact:
+        t += DS_EXACT_SUMS
     return check("ds_q8_matmul", lib.ds_q8_matmul(a._p, b._p, p, t, ld, _q8_stream(stream, dev)))
 
 

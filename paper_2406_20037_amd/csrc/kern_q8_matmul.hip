@@ -852,8 +852,8 @@ int mm_splits(const Q8MatArgs &g, double step) {
     return best;
 }
 
-int mm_tiles(Q8MatArgs &g, hipStream_t stream) {
-    const bool pow2 = g.a.stype == DS_SCALE_POW2, exact = g.type == DS_TYPE_F32;
+int mm_tiles(Q8MatArgs &g, bool exact, hipStream_t stream) {
+    const bool pow2 = g.a.stype == DS_SCALE_POW2;
     auto tiles = [&](int bm, int bn) { return int64_t((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn); };
     if (pow2 && !exact) {
         // Rounds of workgroups over 256 CUs times a round's time: a step of 1.47, 0.95, 1.1 us (two
@@ -915,6 +915,8 @@ extern "C" int ds_q8_matmul(const ds_q8 *a, const ds_q8 *b, void *c, int type, i
                   a->scale_type, (long long)b->cols, b->scale_type);
         return DS_EINVAL;
     }
+    const bool exact = (type & DS_EXACT_SUMS) != 0 || type == DS_TYPE_F32;
+    type &= ~DS_EXACT_SUMS;
     if ((rc = plain_check(c, type, a->rows, b->rows, ldc, "c")) != DS_OK) return rc;
     if (a->rows == 0 || b->rows == 0) return DS_OK;
     Q8MatArgs g{};
@@ -937,7 +939,7 @@ extern "C" int ds_q8_matmul(const ds_q8 *a, const ds_q8 *b, void *c, int type, i
     g.words = words(a) && words(b);
     try {
         // (32 rows of a short reduction too: 32x4096x4096 12.6 us, in tiles 13.9)
-        return g.M > (g.nkt <= 32 ? 32 : 16) ? mm_tiles(g, stream) : few(g, stream);
+        return g.M > (g.nkt <= 32 ? 32 : 16) ? mm_tiles(g, exact, stream) : few(g, stream);
     } catch (const std::bad_alloc &) {                     // of the workspaces' table
         set_error("ds_q8_matmul: out of host memory");
         return DS_ENOMEM;

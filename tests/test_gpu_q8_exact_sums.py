@@ -87,3 +87,33 @@ def test_scales_past_two_to_the_forty(env, mkn, tight):  # noqa: F811
     got, lim = c.double().cpu().numpy(), np.zeros((M, N))
     lim[rows[0]] = (K // 128 + 2) * 2.0 ** -24 * (np.abs(av[rows[0]]).astype(np.float64) @ np.abs(bv).T * 2.0 ** -30)
     assert (np.abs(got - want) <= lim).all()
+
+
+@pytest.mark.parametrize("mkn", [(5, 1000, 70), (24, 4300, 64), (40, 1000, 130), (300, 1003, 260), (1030, 640, 2050)])
+@pytest.mark.parametrize("kind", [q8.POW2, q8.F32])
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_sums_that_cancel(env, mkn, kind, block_rows):  # noqa: F811
+    """Products of +-256 that sum to 0 beside products of +-2^-6: every partial sum is a multiple of 2^-6 below
+    2^18, exact in fp32 in any order, and the sums are exact in 16 bits; 14 bits below the largest product
+    would leave nothing of them."""
+    torch, L = env
+    M, K, N = mkn
+    rng = np.random.default_rng(M + K + N + kind + block_rows)
+    large = np.arange(K) % 4 < 2                       # pairs of them, and of small ones
+    av, bv = rng.integers(-1, 2, (M, K)).astype(np.float64), rng.integers(-1, 2, (N, K)) * 2.0 ** -6
+    sign = np.where(rng.random((N, K)) < 0.5, 1.0, -1.0)
+    sign[:, 1::2] = -sign[:, 0:K - K % 2:2]
+    bv[:, large] = 256.0 * sign[:, large]
+    av[:, large] = 1.0
+    av[:, K - K % 4:] = 0.0                            # no pair there
+    a, b = make(torch, L, M, K, q8.E4M3, kind), make(torch, L, N, K, q8.E4M3, kind, block_rows)
+    for m, v in ((a, av), (b, bv)):
+        m.store[:m.rows, :m.cols] = torch.from_numpy(q8.encode(v, q8.E4M3)).cuda()
+        m.scale.fill_(1.0) if kind == q8.F32 else m.scale.view(torch.uint8).fill_(127)
+    want = av @ bv.T
+    assert np.max(np.abs(want)) <= 2 and np.any(want)
+    for name in ("bfloat16", "float16"):
+        c = torch.empty(M, N, dtype=getattr(torch, name), device="cuda")
+        L.ds_q8_matmul(a, b, c, exact=True)
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(c.double().cpu().numpy(), want)
