@@ -627,8 +627,12 @@ int ds_q8_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t 
  * large 16-bit C).  The product of two scales has to be an fp32 number; an operand's
  * values (byte times scale) below 2^-126 may count as 0.
  * Few output tiles under a long reduction split it over workgroups and join the
- * partial sums in order in a workspace as kernel_run keeps (and under the same rule
- * for captures): two calls give the same bits.  Asynchronous on stream.
+ * partial sums in order, so two calls give the same bits, in the workspace that
+ * kernel_run keeps for the stream.  A capture of such a product (often one of 17 to 500 rows,
+ * or of few rows and up to 2048 columns under K > 8064) therefore needs the same call
+ * once on the capturing stream before, else it returns DS_EUNSUPPORTED with nothing recorded;
+ * and its replays use that stream's workspace: on another stream they are ordered against the
+ * first one's calls by the caller.  Asynchronous on stream.
  * Errors: DS_EINVAL (shapes, strides, types), DS_EHIP, DS_ENOMEM, DS_EUNSUPPORTED.
  */
 int ds_q8_matmul(const ds_q8 *a, const ds_q8 *b, void *c, int type, int64_t ldc,

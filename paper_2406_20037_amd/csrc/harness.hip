@@ -250,9 +250,9 @@ int split_workspace(int64_t elems, hipStream_t stream, float **out, SplitHold &h
         hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
         if (!hip_ok(hipStreamIsCapturing(stream, &cap), "hipStreamIsCapturing")) return DS_EHIP;
         if (cap != hipStreamCaptureStatusNone) {
-            set_error("split reduction needs %lld workspace floats on a stream under capture; run "
-                      "the schedule once on that stream outside capture first, or use "
-                      "kernel_run_noalloc",
+            set_error("split reduction needs %lld workspace floats on a stream under capture; make the "
+                      "same call once on that stream before the capture (kernel_run_noalloc runs a "
+                      "schedule without)",
                       (long long)elems);
             return DS_EUNSUPPORTED;
         }
