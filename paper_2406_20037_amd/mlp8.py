@@ -23,6 +23,7 @@ import torch
 from . import _lib as L
 
 E4M3, E5M2 = torch.float8_e4m3fn, torch.float8_e5m2
+SETS = 4      # sets of buffers kept for training passes, and for others: of the latest token counts
 
 
 def _up(n):
@@ -43,7 +44,7 @@ class Mlp8:
         self.w2 = torch.randn(width, hidden, generator=gen, device=device) / hidden ** 0.5
         self.q1, self.q1_t = self._pair(*self.w1.shape, block_rows=L.DS_Q8_BLOCK)
         self.q2, self.q2_t = self._pair(*self.w2.shape, block_rows=L.DS_Q8_BLOCK)
-        self._buffers = {}
+        self._buffers = {True: {}, False: {}}
         self.requantize()
 
     def _q8(self, rows, cols, dtype=E4M3, block_rows=1):
@@ -58,9 +59,12 @@ class Mlp8:
         L.ds_q8_quantize(self.w2, self.q2, self.q2_t)
 
     def _room(self, tokens, train):
-        """What a pass over so many tokens writes, kept from pass to pass."""
-        key = tokens, train
-        if key not in self._buffers:
+        """What a pass over so many tokens writes, kept from pass to pass for the latest token counts."""
+        sets = self._buffers[train]
+        b = sets.pop(tokens, None)
+        if b is None:
+            if len(sets) == SETS:
+                del sets[next(iter(sets))]                 # the one used longest ago
             wide, new = self.up + self.hidden, lambda r, c: torch.empty(r, c, dtype=torch.bfloat16,
                                                                         device=self.device)
             b = {"x": self._q8(tokens, self.width), "gu": new(tokens, wide),
@@ -73,8 +77,8 @@ class Mlp8:
                 b["h_t"] = self._q8(self.hidden, tokens)
                 b["dh"], b["dx"] = new(tokens, self.hidden), new(tokens, self.width)
                 b["dw1"], b["dw2"] = torch.empty_like(self.w1), torch.empty_like(self.w2)
-            self._buffers[key] = b
-        return self._buffers[key]
+        sets[tokens] = b
+        return b
 
     def forward(self, x, train=False):
         """y [tokens, width] in bf16, in a buffer that the next call of as many tokens uses again;
@@ -87,8 +91,11 @@ class Mlp8:
         return b["y"]
 
     def backward(self, dy):
-        """(dx in bf16, dw1, dw2 in fp32) after forward(x, train=True) of as many tokens."""
-        b = self._room(dy.shape[0], True)
+        """(dx in bf16, dw1, dw2 in fp32) after forward(x, train=True) of as many tokens, among the latest
+        SETS token counts of such calls."""
+        b = self._buffers[True].get(dy.shape[0])
+        if b is None:
+            raise ValueError(f"no forward pass of {dy.shape[0]} tokens is kept")
         L.ds_q8_quantize(dy, b["dy"], b["dy_t"])
         L.ds_q8_matmul(b["dy"], self.q2_t, b["dh"])
         L.ds_swiglu8_grad(b["saved"], b["dh"], b["dgu"], b["dgu_t"], b["h_t"])
