@@ -690,8 +690,10 @@ class Q8:
         if scale.device != data.device:
             raise ValueError(f"values on {data.device}, scales on {scale.device}")
         sld = _plain_rows(scale)[2]
-        if rows == 1:                   # the stride of a single row says nothing
-            ld = max(ld, (cols + 15) // 16 * 16)
+        if rows <= 1:                   # the stride of a single row says nothing
+            ld = max(16, (cols + 15) // 16 * 16)
+        if want[0] <= 1:                # (in whole words where it allows them: products copy scales so)
+            sld = min(sld, (want[1] + 3) // 4 * 4)
         self.data, self.scale, self.rows, self.cols = data, scale, rows, cols
         self.block_rows = block_rows
         self._device = data.get_device()
