@@ -606,7 +606,8 @@ typedef struct {
  * NaN gives NaN, an infinity NaN in e4m3 and infinity in e5m2; other values of
  * its block keep their precision.  Writes the scales of every block and no byte
  * past a row's end.  x needs its type's alignment only (16-byte rows are faster).
- * Asynchronous on stream; allocates nothing.  Errors: DS_EINVAL, DS_EHIP.
+ * Asynchronous on stream; allocates nothing.  Errors: DS_EINVAL, DS_EHIP,
+ * DS_EUNSUPPORTED (2^23 tiles of 128 x 128 or more).
  */
 int ds_q8_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t ldx,
                    const ds_q8 *row, const ds_q8 *col, hipStream_t stream);
@@ -633,7 +634,8 @@ int ds_q8_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t 
  * once on the capturing stream before, else it returns DS_EUNSUPPORTED with nothing recorded;
  * and its replays use that stream's workspace: on another stream they are ordered against the
  * first one's calls by the caller.  Asynchronous on stream.
- * Errors: DS_EINVAL (shapes, strides, types), DS_EHIP, DS_ENOMEM, DS_EUNSUPPORTED.
+ * Errors: DS_EINVAL (shapes, strides, types), DS_EHIP, DS_ENOMEM, DS_EUNSUPPORTED
+ * (captures; 2^32 threads or more).
  */
 int ds_q8_matmul(const ds_q8 *a, const ds_q8 *b, void *c, int type, int64_t ldc,
                  hipStream_t stream);
@@ -658,7 +660,8 @@ int ds_swiglu8(const void *gu, int type, int64_t rows, int64_t hidden, int64_t u
  * + hidden)) and transposed in *dgu_t; and silu(g) * u transposed in *h_t (hidden x rows),
  * with which the next layer's weight gradient is taken.  Each output may be null.
  * dh [rows, hidden]: type DS_TYPE_*, rows ldh elements apart.  block_rows 1 throughout.
- * Asynchronous; allocates nothing.  Errors: DS_EINVAL, DS_EHIP.
+ * Asynchronous; allocates nothing.  Errors: DS_EINVAL, DS_EHIP, DS_EUNSUPPORTED
+ * (as ds_q8_quantize).
  */
 int ds_swiglu8_grad(const ds_q8 *saved, const void *dh, int type, int64_t hidden, int64_t up,
                     int64_t ldh, const ds_q8 *dgu, const ds_q8 *dgu_t, const ds_q8 *h_t,

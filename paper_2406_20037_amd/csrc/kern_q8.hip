@@ -39,6 +39,14 @@ int q8_check(const ds_q8 *m, const char *what) {
     return DS_OK;
 }
 
+int launch_check(int64_t groups, int threads, const char *what) {
+    if (groups > int64_t(0xffffffffu) / threads) {
+        set_error("%s: %lld workgroups of %d threads are more than a launch takes", what, (long long)groups, threads);
+        return DS_EUNSUPPORTED;
+    }
+    return DS_OK;
+}
+
 int plain_check(const void *p, int type, int64_t rows, int64_t cols, int64_t ld, const char *what) {
     if (type != DS_TYPE_F32 && type != DS_TYPE_F16 && type != DS_TYPE_BF16) {
         set_error("%s: type %d", what, type);
@@ -591,15 +599,11 @@ int by_type(int type, Fn fn) {
     return hip_ok(hipGetLastError(), "8-bit kernel launch") ? DS_OK : DS_EHIP;
 }
 
-// One workgroup a tile; DS_EUNSUPPORTED past the grid's limit.
+// One workgroup a tile.
 int tile_grid(int64_t rows, int64_t cols, unsigned *grid) {
     const int64_t n = q8_up(rows) * q8_up(cols);
-    if (n > kGridLimit) {
-        set_error("%lld tiles of 128 x 128 are more than a launch takes", (long long)n);
-        return DS_EUNSUPPORTED;
-    }
     *grid = unsigned(n);
-    return DS_OK;
+    return launch_check(n, kTileThreads, "tiles of 128 x 128");
 }
 
 // Workgroups of 16 blocks each, at most what fills the chip several times over.

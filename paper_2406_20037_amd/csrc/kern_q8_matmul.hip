@@ -813,11 +813,8 @@ int mm_launch(Q8MatArgs &g, hipStream_t stream) {
     g.tiles_n = (g.N + S::BN - 1) / S::BN;
     g.group = 4;
     const int64_t grid = int64_t(g.tiles_m) * g.tiles_n * g.ks;
-    if (grid > kGridLimit) {
-        set_error("ds_q8_matmul: %lld workgroups", (long long)grid);
-        return DS_EUNSUPPORTED;
-    }
-    int rc = DS_OK;
+    int rc = launch_check(grid, 256, "ds_q8_matmul");
+    if (rc != DS_OK) return rc;
     const int done = by_formats(g.a.fmt, g.b.fmt, [&](auto fa, auto fb) {
         auto *k = &q8_mm<FM, FN, MODE, SQ, fa.value, fb.value>;
         rc = ensure_lds_attr(reinterpret_cast<const void *>(k), S::LDS);
@@ -878,7 +875,9 @@ int mm_tiles(Q8MatArgs &g, bool exact, hipStream_t stream) {
 template <int NT, bool SQ>
 int few_launch(Q8MatArgs &g, int waves, hipStream_t stream) {
     const unsigned tn = unsigned((g.N + 16 * NT - 1) / (16 * NT)), tm = unsigned((g.M + 15) / 16);
-    const int rc = by_formats(g.a.fmt, g.b.fmt, [&](auto fa, auto fb) {
+    int rc = launch_check(tn, 64 * waves, "ds_q8_matmul");
+    if (rc != DS_OK) return rc;
+    rc = by_formats(g.a.fmt, g.b.fmt, [&](auto fa, auto fb) {
         q8_few<NT, SQ, fa.value, fb.value><<<dim3(tn, tm, unsigned(g.ks)), 64 * waves, 0, stream>>>(g);
     });
     return rc == DS_OK ? join(g, stream) : rc;

@@ -16,6 +16,10 @@ int q8_check(const ds_q8 *m, const char *what);
 // The same for a plain matrix of DS_TYPE_* elements, ld elements between rows.
 int plain_check(const void *p, int type, int64_t rows, int64_t cols, int64_t ld, const char *what);
 
+// DS_OK, or DS_EUNSUPPORTED with the error set where a launch, whose work-items are counted in 32 bits,
+// does not take so many workgroups.
+int launch_check(int64_t groups, int threads, const char *what);
+
 inline int64_t q8_up(int64_t n) { return (n + kQ8Block - 1) / kQ8Block; }
 inline int type_bytes(int type) { return type == DS_TYPE_F32 ? 4 : 2; }
 

@@ -30,3 +30,11 @@ def test_the_stride_of_a_single_row(rows, apart):
     # the host's checks alone: a second operand without rows launches nothing
     none = L.Q8(0, 200, device="cpu")
     assert L.lib.ds_q8_matmul(m._p, none._p, None, L.DS_TYPE_F32, 0, None) == L.DS_OK
+
+
+def test_more_workgroups_than_a_launch_takes():
+    """A launch counts its threads in 32 bits: shapes within the limits of a matrix that need more."""
+    wide = 0x7ffffe00
+    assert quantize(None, q8(wide, 1, 16, 1), rows=1, cols=wide, ldx=wide) == L.DS_EUNSUPPORTED
+    assert matmul(q8(1, 4096, 4096, 32), q8(wide, 4096, 4096, 32), ldc=wide) == L.DS_EUNSUPPORTED
+    assert b"workgroups" in L.lib.ds_last_error()
