@@ -89,7 +89,7 @@ def test_scales_past_two_to_the_forty(env, mkn, tight):  # noqa: F811
     assert (np.abs(got - want) <= lim).all()
 
 
-@pytest.mark.parametrize("mkn", [(5, 1000, 70), (24, 4300, 64), (40, 1000, 130), (300, 1003, 260), (1030, 640, 2050)])
+@pytest.mark.parametrize("mkn", [(5, 1000, 70), (24, 1000, 70), (24, 4300, 64), (40, 1000, 130), (300, 1003, 260), (1030, 640, 2050)])
 @pytest.mark.parametrize("kind", [q8.POW2, q8.F32])
 @pytest.mark.parametrize("block_rows", [1, 128])
 def test_sums_that_cancel(env, mkn, kind, block_rows):  # noqa: F811
@@ -112,8 +112,11 @@ def test_sums_that_cancel(env, mkn, kind, block_rows):  # noqa: F811
         m.scale.fill_(1.0) if kind == q8.F32 else m.scale.view(torch.uint8).fill_(127)
     want = av @ bv.T
     assert np.max(np.abs(want)) <= 2 and np.any(want)
-    for name in ("bfloat16", "float16"):
+    few = M <= (32 if K <= 4096 else 16)               # exact without asking
+    for name, exact in (("bfloat16", True), ("float16", True), ("bfloat16", False), ("float32", False)):
+        if not exact and name == "bfloat16" and not few:
+            continue
         c = torch.empty(M, N, dtype=getattr(torch, name), device="cuda")
-        L.ds_q8_matmul(a, b, c, exact=True)
+        L.ds_q8_matmul(a, b, c, exact=exact)
         torch.cuda.synchronize()
         np.testing.assert_array_equal(c.double().cpu().numpy(), want)
