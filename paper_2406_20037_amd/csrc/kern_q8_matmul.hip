@@ -853,15 +853,17 @@ int mm_tiles(Q8MatArgs &g, bool exact, hipStream_t stream) {
     const bool pow2 = g.a.stype == DS_SCALE_POW2;
     auto tiles = [&](int bm, int bn) { return int64_t((g.M + bm - 1) / bm) * ((g.N + bn - 1) / bn); };
     if (pow2 && !exact) {
-        // Rounds of workgroups over 256 CUs times a round's time: a step of 1.47, 0.95, 1.1 us (two
-        // workgroups a CU, 0.62 for one) and what comes before and after.  2048x4096x8192: 91, 66
-        // and 72 us; 4096x4096x4096: 60, 70 and 66; 1024x4096x4096: 47, 30 and 22.
+        // Rounds of workgroups over 256 CUs times a round's time: a step of 1.31, 0.86, 0.87 us (two
+        // workgroups a CU, 0.47 for one) and what comes before and after.  In tiles of 256 x 256, 256 x 128
+        // and 128 x 128: 4096x4096x4096 55, 68 and 63 us; 8192x8192x8192 391, 477 and 462; 2048x4096x8192
+        // 85, 61 and 61; 1024x4096x4096 46, 30 and 20; 3000x5000x6000 86, 101 and 114; 4096x4096x700 20, 24
+        // and 22.  Of the two smaller it is 256 x 128 for reductions from 12700 on: 512x16384x16384 131 and 141.
         const double n = g.nkt;
         const int64_t t = tiles(128, 128);
-        const double large = double((tiles(256, 256) + 255) / 256) * (1.47 * n + 14);
-        const double tall = double((tiles(256, 128) + 255) / 256) * (0.95 * n + 6);
-        const double small = double(t / 512) * (1.1 * n + 5) +
-                             (t % 512 > 256 ? 1.1 * n + 5 : t % 512 ? 0.62 * n + 5 : 0);
+        const double large = double((tiles(256, 256) + 255) / 256) * (1.31 * n + 12);
+        const double tall = double((tiles(256, 128) + 255) / 256) * (0.86 * n + 6);
+        const double small = double(t / 512) * (0.87 * n + 5) +
+                             (t % 512 > 256 ? 0.87 * n + 5 : t % 512 ? 0.47 * n + 5 : 0);
         if (large <= tall && large <= small) return mm_launch<8, 8, MM_POW2, false>(g, stream);
         if (tall <= small) return mm_launch<8, 4, MM_POW2, false>(g, stream);
     }

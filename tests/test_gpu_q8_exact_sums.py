@@ -29,11 +29,11 @@ def whole(torch, L, rng, rows, cols, fmt, kind, block_rows):
     return m, (v * q8.spread(2.0 ** e, rows, cols, block_rows)).astype(np.float32)
 
 
-# one row to 32, tiles of 128 x 128 (whole, ragged, split), of 256 x 128 and of 256 x 256, and
-# reductions that end inside a step, inside 16 bytes, and after less than one step
+# one row to 32, tiles of 128 x 128 (whole, ragged, split), of 256 x 256 and of 256 x 128 (long
+# reductions), and reductions that end inside a step, inside 16 bytes, and after less than one step
 SHAPES = [(1, 4000, 70), (9, 8200, 300), (31, 1001, 8300), (40, 4100, 130), (128, 128, 128), (130, 77, 260),
           (256, 1111, 384), (1003, 777, 1501), (100, 5000, 200), (2048, 1152, 4096), (2001, 1111, 4000),
-          (4096, 1024, 4096), (3900, 1003, 4001)]
+          (4096, 1024, 4096), (3900, 1003, 4001), (300, 12901, 11100)]
 
 
 @pytest.mark.parametrize("mkn", SHAPES)
