@@ -624,8 +624,8 @@ int ds_q8_quantize(const void *x, int type, int64_t rows, int64_t cols, int64_t 
  * largest and keep about 14 bits of them: 1e-5 to 1e-4 of the result for normal and for
  * heavy-tailed values, against 2^-9 and 2^-12 of the rounding to bf16 and fp16.  An fp32
  * C, one of fewer rows, or any C whose type has DS_EXACT_SUMS added, comes from bf16 matrix
- * instructions on the same values, whose sums are exact to fp32 (in about twice the time of a
- * large 16-bit C).  The product of two scales has to be an fp32 number; an operand's
+ * instructions on the same values, whose sums are exact to fp32 (a large 16-bit C takes 2.2
+ * times as long so).  The product of two scales has to be an fp32 number; an operand's
  * values (byte times scale) below 2^-126 may count as 0.
  * Few output tiles under a long reduction split it over workgroups and join the
  * partial sums in order, so two calls give the same bits, in the workspace that

@@ -179,8 +179,8 @@ __device__ __forceinline__ void by_fmt(int fmt, Fn fn) {
 
 // Rows alone, or one plain matrix read once and written in a half to a quarter of its bytes: bound by
 // the memory.  16 lanes a block, so that the largest magnitude meets in one row of lanes, without LDS,
-// and a wave's loads cover whole lines: 16384x8192 bf16 in 71 us (5.7 TB/s, of which the caches
-// serve a part); of rows that are not 16-byte aligned 88.
+// and a wave's loads cover whole lines: 16384x8192 bf16 in 74 us (5.4 TB/s, of which the caches
+// serve a part); of rows that are not 16-byte aligned 89.
 template <typename T>
 __global__ __launch_bounds__(256) void q8_rows(const T *x, int64_t ldx, int vec, Q8View m, int nb,
                                                int64_t total) {
@@ -198,7 +198,8 @@ __global__ __launch_bounds__(256) void q8_rows(const T *x, int64_t ldx, int vec,
 // Both directions from one read: bound by the memory, if enough of it is on its way.  A tile stays in
 // registers while its rows' and its columns' largest magnitudes are found (rows by lanes, columns
 // by lanes, then over the waves through LDS), and its transpose goes through LDS as bytes, so that it
-// is written in whole lines too.  16384x8192 bf16 both ways in 110 us (4.9 TB/s), fp32 160 us (5.0).
+// is written in whole lines too.  16384x8192 bf16 both ways in 115 us (4.7 TB/s), fp32 151 us (5.3), and in
+// squares 152; 16384x8191 bf16, whose rows load element by element, 147.
 // 512 threads; thread t holds rows 4 (t / 16) .. + 3 of columns 8 (t % 16) .. + 7.
 constexpr int kTileThreads = 512, kRows = 4, kTileWaves = kTileThreads / 64;
 
@@ -436,8 +437,8 @@ __device__ __forceinline__ float sigmoid(float g) {
 
 // h = g sigmoid(g) u, with g and u kept in 8 bits: bound by the memory, the sigmoid's arithmetic
 // beside it.  As q8_rows: 16 lanes a block, which write up to three blocks of one read.  8192x8192 bf16
-// with its checkpoint in 83 us (5.7 TB/s).  VEC: rows are 16-byte aligned (8192x8191, which are not,
-// 107 us, and 142 with the columns looked at one by one).
+// with its checkpoint in 85 us (5.5 TB/s).  VEC: rows are 16-byte aligned (8192x8191, which are not,
+// 105 us, and 142 with the columns looked at one by one).
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void swiglu8_rows(const T *gu, int64_t ldg, int hidden, int up,
                                                     Q8View h, Q8View saved, int nb, int64_t total) {
@@ -571,9 +572,9 @@ __device__ __forceinline__ void grad_body(const Q8View &saved, const T *dh, int6
 }
 
 // A tile of g, u and dh gives three outputs in five layouts.  Its 602 MB at 8192x8192 would take
-// 116 us; bound by the vector unit (about 55 instructions a value: the sigmoid, three products, and five
+// 116 us; bound by the vector unit (51 instructions a value: the sigmoid, three products, and five
 // maxima, scalings and roundings) and by how few waves the registers leave to hide latency: bf16 dh
-// 154 us with 16 waves a CU; fp32 dh, whose loaded rows take twice the registers, 201 with 8.
+// 150 us with 16 waves a CU; fp32 dh, whose loaded rows take twice the registers, 241 with 8.
 template <typename T, bool WHOLE>
 __global__ __launch_bounds__(kTileThreads, sizeof(T) == 4 ? 3 : 4) void swiglu8_grad_tile(
     Q8View saved, const T *dh, int64_t ldh, int vec, int hidden, int up, int tiles_c, Q8View dgu, Q8View dgu_t,

@@ -257,7 +257,7 @@ struct MmShape {
 // 64 KB, more than the caches' rate asks for.  Operands go from memory to LDS without registers, in
 // two stages, each step's copies issued a step and a half before their use, in two parts, as
 // each half of a stage has been read; fragments are read from LDS between the products of the
-// quarter before.  8192x16384x8192 to bf16: 820 us (2.7 PFLOP/s; the instructions alone, on random
+// quarter before.  8192x16384x8192 to bf16: 810 us (2.7 PFLOP/s; the instructions alone, on random
 // bytes in registers, reach 3.2 to 4.2 at the clock that the power leaves them).  Exact to fp32:
 // 4096x8192x8192 475 us (1.2 PFLOP/s; bf16 instructions alone 2.0 to 2.2, and each byte is first decoded).
 // SQ: B's scales are of squares, one for all columns of a wave.  A tile of 256 columns or rows leaves
@@ -671,7 +671,8 @@ __global__ __launch_bounds__(256, FM * FN > 16 ? 1 : 2) void q8_mm(Q8MatArgs a) 
         copy_all(kt0 + 1, STAGE);
         // MM_EXACT_POW2: scales of at most 2^40 go into the decoded operands, which then meet neither
         // the largest bf16 number nor, while the values that they stand for are normal fp32 numbers,
-        // the smallest; the sums need no scaling any more (4096x8192x8192, both operands 1x128: 15 % less time).
+        // the smallest; the sums need no scaling any more (4096x8192x8192, both operands 1x128: 455 us, and 505
+        // with fp32 scales, whose sums do).
         bool small = true;
         if constexpr (MODE == MM_EXACT_POW2) small = !__syncthreads_or(scales_past_2_40());
         clear_past(kt0, 0);
@@ -832,8 +833,8 @@ int mm_square(Q8MatArgs &g, hipStream_t stream) {
 
 // The split of a reduction over tiles of 128 x 128, by what each took on the chip: a step of 128 about
 // `step` us in a workgroup that has its SIMD units to itself, and the join 3 us and the partial sums'
-// writing and reading.  33x4096x4096 18.6 -> 13.8 us by four, 64x16384x8192 48 -> 38; 512x4096x4096
-// would go from 18.4 to 22.0 and stays whole.
+// writing and reading.  33x4096x4096 17.6 -> 12.6 us by eight, 64x16384x8192 32 -> 30 by four;
+// 512x4096x4096 would go from 16.6 to 20.5 and stays whole.
 int mm_splits(const Q8MatArgs &g, double step) {
     const int64_t tiles = int64_t((g.M + 127) / 128) * ((g.N + 127) / 128);
     const double sums = double(g.M) * g.N * 10 / 4.5e6;
@@ -939,7 +940,7 @@ extern "C" int ds_q8_matmul(const ds_q8 *a, const ds_q8 *b, void *c, int type, i
     };
     g.words = words(a) && words(b);
     try {
-        // (32 rows of a short reduction too: 32x4096x4096 12.6 us, in tiles 13.9)
+        // (32 rows of a short reduction too: 32x4096x4096 10.0 us, 33 rows in tiles 12.4)
         return g.M > (g.nkt <= 32 ? 32 : 16) ? mm_tiles(g, exact, stream) : few(g, stream);
     } catch (const std::bad_alloc &) {                     // of the workspaces' table
         set_error("ds_q8_matmul: out of host memory");
