@@ -2,6 +2,7 @@
 // harness (the "trial" of Section 2.1: observing one schedule's execution).
 #include <algorithm>
 #include <array>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 #include <limits>
@@ -175,6 +176,7 @@ struct SplitWs {
     std::mutex mu;
     float *p = nullptr;
     int64_t elems = 0;
+    uint64_t owner = 0;   // hipStreamPerThread: the thread, by a number that is not used again as its id is
 };
 std::map<std::tuple<int, hipStream_t, std::thread::id>, SplitWs> g_split_ws;
 std::vector<std::pair<int, void *>> g_split_retired;
@@ -238,7 +240,10 @@ int split_workspace(int64_t elems, hipStream_t stream, float **out, SplitHold &h
     int dev;
     int rc = current_device(dev);
     if (rc != DS_OK) return rc;
-    const std::thread::id own = stream == hipStreamPerThread ? std::this_thread::get_id() : std::thread::id();
+    static std::atomic<uint64_t> threads{0};
+    thread_local const uint64_t self = ++threads;
+    const bool per_thread = stream == hipStreamPerThread;
+    const std::thread::id own = per_thread ? std::this_thread::get_id() : std::thread::id();
     SplitWs *found;
     {
         std::lock_guard<std::mutex> lk(g_mu);
@@ -246,7 +251,9 @@ int split_workspace(int64_t elems, hipStream_t stream, float **out, SplitHold &h
     }
     SplitWs &ws = *found;
     hold = SplitHold(ws.mu);
-    if (ws.elems < elems) {
+    // left by a thread that has ended, whose last work may be on its way
+    const bool left = per_thread && ws.p && ws.owner != self;
+    if (ws.elems < elems || left) {
         hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
         if (!hip_ok(hipStreamIsCapturing(stream, &cap), "hipStreamIsCapturing")) return DS_EHIP;
         if (cap != hipStreamCaptureStatusNone) {
@@ -256,6 +263,9 @@ int split_workspace(int64_t elems, hipStream_t stream, float **out, SplitHold &h
                       (long long)elems);
             return DS_EUNSUPPORTED;
         }
+        if (left && !hip_ok(hipDeviceSynchronize(), "hipDeviceSynchronize")) return DS_EHIP;
+    }
+    if (ws.elems < elems) {
         const int64_t grow = std::max<int64_t>(elems, 2 * ws.elems);
         void *p = nullptr;
         if (!hip_ok(hipMalloc(&p, size_t(grow) * sizeof(float)), "hipMalloc(split workspace)"))
@@ -271,6 +281,7 @@ int split_workspace(int64_t elems, hipStream_t stream, float **out, SplitHold &h
         ws.p = static_cast<float *>(p);
         ws.elems = grow;
     }
+    ws.owner = self;
     *out = ws.p;
     return DS_OK;
 }

@@ -58,6 +58,25 @@ def test_products(env, own_streams):  # noqa: F811
         assert all(torch.equal(got[i], want) for i in range(CALLS))
 
 
+def test_threads_one_after_another(env):  # noqa: F811
+    """Threads that end with work on their way, each on its own stream of one handle: a later thread may have an
+    earlier one's id."""
+    torch, L = env
+    rng = np.random.default_rng(59)
+    cases = [product(torch, L, rng, *shape) for shape in ((200, 8192, 900, "float32"), (40, 8192, 64, "float32"))]
+
+    def once(i):
+        a, b, got, _ = cases[i % 2]
+        L.ds_q8_matmul(a, b, got[i], stream=2)
+
+    for i in range(40):
+        t = threading.Thread(target=once, args=(i,))
+        t.start()
+        t.join()
+    torch.cuda.synchronize()
+    assert all(torch.equal(cases[i % 2][2][i], cases[i % 2][3]) for i in range(40))
+
+
 def test_beside_a_split_schedule(env):  # noqa: F811
     """kernel_run's split schedules use the same workspace."""
     torch, L = env
