@@ -667,6 +667,120 @@ int ds_swiglu8_grad(const ds_q8 *saved, const void *dh, int type, int64_t hidden
                     int64_t ldh, const ds_q8 *dgu, const ds_q8 *dgu_t, const ds_q8 *h_t,
                     hipStream_t stream);
 
+/* ---- attention over an 8-bit cache -------------------------------------------- */
+
+/* A tensor [tokens, heads, dim] in device memory (a plain value; the buffer is the
+ * caller's): element (t, h, d) is data[t * ld + h * head_ld + d], aligned to its type
+ * (16-byte rows are faster).  Inputs may have any strides from 0 on (a row of several
+ * tokens' or heads' is read for each); an output's rows must not overlap. */
+typedef struct {
+    void *data;
+    int64_t tokens, heads, dim, ld, head_ld;
+    int32_t type;            /* DS_TYPE_* */
+    int32_t reserved;        /* 0 */
+} ds_heads;
+
+/* Keys and values of sequences in 8 bits, in pages of `page` tokens.  Page p holds the
+ * rows of head h and offset i at k + p * stride + (h * page + i) * dim, dim bytes each
+ * (v alike), and one scale a row at entry p * scale_stride + h * page + i of k_scale (v_scale).
+ * A row's value d is its byte times its scale.  dim: a multiple of 16, up to 256; page: a
+ * multiple of 16, up to 65536; pages: up to 2^31 - 1; stride: a multiple of 16, at least
+ * heads * page * dim, which is below 2^31; scale_stride: at least heads * page.
+ * k and v 16-byte aligned; F32 scales 4-byte aligned. */
+typedef struct {
+    void *k, *v;
+    void *k_scale, *v_scale;
+    int64_t pages, stride, scale_stride;
+    int32_t page, heads, dim;
+    int32_t format;          /* DS_Q8_* */
+    int32_t scale_type;      /* DS_SCALE_* */
+    int32_t reserved;        /* 0 */
+} ds_cache8;
+
+/* What new tokens belong to, in device memory (read by the kernels, so a captured graph
+ * follows its changes).  Sequence b has the tokens starts[b] .. starts[b + 1] - 1 of a call (starts
+ * does not decrease; none, one or many), which are the last of its lengths[b] tokens: token t is at position
+ * lengths[b] - starts[b + 1] + t.  Position p lies in page table[b * table_ld + p / page],
+ * at offset p % page.  A position has no place if it is negative, past the table's table_cols
+ * pages, or in a page whose number is not 0 .. pages - 1; no access follows such a number.
+ * seqs: 0 to 2^24; table_cols * page: below 2^31 - 2^16. */
+typedef struct {
+    const int32_t *starts, *lengths, *table;
+    int64_t seqs, table_cols, table_ld;
+} ds_chunk;
+
+enum {
+    DS_ROTARY_HALVES = 0,    /* pair i is values i and i + turn / 2 */
+    DS_ROTARY_PAIRS = 1,     /* pair i is values 2 i and 2 i + 1 */
+    DS_ROTARY_INVERSE = 2    /* added: the opposite angle, the gradient's turn */
+};
+
+/*
+ * ds_rotary -- rotary positions: y = x with each pair i of the first `turn` values (even,
+ * up to dim) of every head turned by the angle pos[t] * freqs[i] and multiplied by scale:
+ *     y_a = scale * (x_a cos - x_b sin),  y_b = scale * (x_a sin + x_b cos),
+ * the other values copied.  freqs [turn / 2] (fp32) holds any scaling for long texts.  With
+ * DS_ROTARY_INVERSE the angle's sign changes: the gradient of x from the gradient of y.
+ * The angle is formed and reduced in 64 bits, so far positions lose nothing; the rest is fp32, with
+ * one rounding to y's type.  y: x's type and shape; x itself (same data and strides) is fine, other
+ * overlaps are not.  Asynchronous; allocates nothing.  Errors: DS_EINVAL, DS_EHIP, DS_EUNSUPPORTED
+ * (2^32 threads or more).
+ */
+int ds_rotary(const ds_heads *x, const int32_t *pos, const float *freqs, int64_t turn, int mode,
+              float scale, const ds_heads *y, hipStream_t stream);
+
+/*
+ * ds_cache8_write -- the rows of k and v [tokens, cache heads, cache dim] in 8 bits, as
+ * ds_q8_quantize would write a block (one scale a row, whatever dim), to the places of their
+ * tokens.  Tokens of no sequence and positions without a place are not written; no other byte of
+ * the cache changes.  Of tokens that share a place one is kept in each 8 bytes and each scale, any of
+ * them.  Asynchronous; allocates nothing.  Errors: DS_EINVAL, DS_EHIP, DS_EUNSUPPORTED.
+ */
+int ds_cache8_write(const ds_cache8 *cache, const ds_chunk *chunk, const ds_heads *k, const ds_heads *v,
+                    hipStream_t stream);
+
+/*
+ * ds_cache8_read -- the rows of the tokens' places back in k and v (the values, byte times
+ * scale in fp32, rounded to their type): with starts as the running sum of lengths, whole
+ * sequences.  Rows of no sequence stay as they were; positions without a place give zeros.
+ * Asynchronous; allocates nothing.  Errors: as ds_cache8_write.
+ */
+int ds_cache8_read(const ds_cache8 *cache, const ds_chunk *chunk, const ds_heads *k, const ds_heads *v,
+                   hipStream_t stream);
+
+/* Arguments of ds_attn8 beside its tensors. */
+typedef struct {
+    double scale;            /* of the products q.k, finite */
+    int32_t causal;          /* 1: keys up to the token's own position; 0: all of its sequence */
+    int32_t reserved;        /* 0 */
+    int64_t window;          /* > 0, with causal: the latest so many of them; 0: all */
+    int64_t max_len;         /* no sequence is longer (keys past it are not seen); 0: what the table holds */
+} ds_attn8_cfg;
+
+/*
+ * ds_attn8 -- attention of new tokens over their sequences' keys and values in the cache,
+ * where ds_cache8_write has put the new tokens' own: one token a sequence, a chunk of a
+ * prompt, or a whole one.
+ *     out[t, h] = sum_j p_j v_j,   p = softmax over the keys j that t sees of scale * q[t, h].k_j,
+ * k_j and v_j of cache head h / (q heads / cache heads).  lse [tokens, q heads] (fp32, or null):
+ * log sum_j exp(scale * q.k_j), with which parts over several caches are joined.  A row that sees no key (or
+ * only places without a page) gives zeros and -infinity; rows of no sequence stay as they were. What
+ * a key holds that a token does not see, NaN included, does not reach its row.
+ * q, out: fp32, fp16 or bf16 (the same), tokens x q heads x cache dim.  Products of q and k are exact
+ * and summed in fp32, softmax and sums are fp32; the weights p enter the second product in bf16, as one
+ * part of 8 bits for bf16 (half the rounding of out, on average), as two for fp16 and three for fp32, whose
+ * queries are split into three too.
+ * A few tokens over long sequences split the keys over workgroups and join the parts in order, so two
+ * calls give the same bits, in `work` (16-byte aligned, work_bytes of it, as ds_attn8_work
+ * says for the same arguments; 0 bytes need no pointer): the caller's, for this call until it is done.
+ * Asynchronous; allocates nothing.  Errors: DS_EINVAL, DS_EHIP, DS_EUNSUPPORTED (fp32 queries of more
+ * than 128 values; 2^32 threads or more).
+ */
+int ds_attn8(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg,
+             const ds_heads *out, float *lse, void *work, int64_t work_bytes, hipStream_t stream);
+int ds_attn8_work(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk,
+                  const ds_attn8_cfg *cfg, int64_t *bytes);
+
 /* ---- misc ------------------------------------------------------------------ */
 
 const char *ds_last_error(void);

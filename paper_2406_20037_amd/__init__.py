@@ -3,16 +3,18 @@ combined Ansor + Droplet Search approach: a schedule-parameterised fp32
 conv2d / matmul kernel family in HIP, a hipEvent measurement harness, a seeded
 exploration sampler and Droplet Search coordinate descent, behind the C ABI
 of ``include/droplet.h``; and the 8-bit operators of the same ABI (``Q8``,
-``ds_q8_quantize``, ``ds_q8_matmul``, ``ds_swiglu8``, ``ds_swiglu8_grad``).
+``ds_q8_quantize``, ``ds_q8_matmul``, ``ds_swiglu8``, ``ds_swiglu8_grad``; ``Cache8``, ``Chunk``,
+``ds_rotary``, ``ds_cache8_write``, ``ds_cache8_read``, ``ds_attn8``).
 ``_lib`` is the Python binding of that ABI; it is loaded on first use of any
 name below, and raises if the library is missing.
 """
 import sys
 import types
 
-_EXPORTS = ["DS_OP_CONV2D_NCHW", "DS_OP_MATMUL_RM", "Q8", "Space", "ansor_sample", "droplet_tune",
-            "droplet_tune_ex", "ds_empty_kernel_floor", "ds_measure", "ds_q8_matmul",
-            "ds_q8_quantize", "ds_swiglu8", "ds_swiglu8_grad", "ds_tune", "kernel_run",
+_EXPORTS = ["Cache8", "Chunk", "DS_OP_CONV2D_NCHW", "DS_OP_MATMUL_RM", "Q8", "Space", "ansor_sample",
+            "droplet_tune", "droplet_tune_ex", "ds_attn8", "ds_attn8_work", "ds_cache8_read",
+            "ds_cache8_write", "ds_empty_kernel_floor", "ds_measure", "ds_q8_matmul", "ds_q8_quantize",
+            "ds_rotary", "ds_swiglu8", "ds_swiglu8_grad", "ds_tune", "kernel_run",
             "kernel_run_reference", "make_io", "measure_cfg", "tune_cfg"]
 
 __all__ = _EXPORTS + ["_lib"]

@@ -51,6 +51,7 @@ DS_Q8_E4M3, DS_Q8_E5M2 = 0, 1
 DS_SCALE_POW2, DS_SCALE_F32 = 0, 1
 DS_Q8_BLOCK = 128
 DS_EXACT_SUMS = 256
+DS_ROTARY_HALVES, DS_ROTARY_PAIRS, DS_ROTARY_INVERSE = 0, 1, 2
 
 
 class ds_q8(C.Structure):
@@ -58,6 +59,28 @@ class ds_q8(C.Structure):
                 ("cols", C.c_int64), ("ld", C.c_int64), ("scale_ld", C.c_int64),
                 ("format", C.c_int32), ("scale_type", C.c_int32), ("block_rows", C.c_int32),
                 ("reserved", C.c_int32)]
+
+
+class ds_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("tokens", C.c_int64), ("heads", C.c_int64), ("dim", C.c_int64),
+                ("ld", C.c_int64), ("head_ld", C.c_int64), ("type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class ds_cache8(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("pages", C.c_int64), ("stride", C.c_int64), ("scale_stride", C.c_int64),
+                ("page", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32), ("format", C.c_int32),
+                ("scale_type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class ds_chunk(C.Structure):
+    _fields_ = [("starts", C.c_void_p), ("lengths", C.c_void_p), ("table", C.c_void_p),
+                ("seqs", C.c_int64), ("table_cols", C.c_int64), ("table_ld", C.c_int64)]
+
+
+class ds_attn8_cfg(C.Structure):
+    _fields_ = [("scale", C.c_double), ("causal", C.c_int32), ("reserved", C.c_int32),
+                ("window", C.c_int64), ("max_len", C.c_int64)]
 
 
 class ds_sched(C.Structure):
@@ -224,6 +247,12 @@ SIGNATURES = {
                              C.c_void_p, C.c_void_p, C.c_void_p]),
     "ds_swiglu8_grad": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64,
                                   C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ds_rotary": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_float, C.c_void_p,
+                            C.c_void_p]),
+    "ds_cache8_write": (C.c_int, [C.c_void_p] * 5),
+    "ds_cache8_read": (C.c_int, [C.c_void_p] * 5),
+    "ds_attn8": (C.c_int, [C.c_void_p] * 7 + [C.c_int64, C.c_void_p]),
+    "ds_attn8_work": (C.c_int, [C.c_void_p] * 4 + [C.POINTER(C.c_int64)]),
     "ds_last_error": (C.c_char_p, []),
     "ds_gen_uniform": (C.c_int, [C.c_uint64, C.c_int64, C.POINTER(C.c_float)]),
     "ds_device_info": (C.c_int, [C.POINTER(C.c_int), C.POINTER(C.c_int), C.c_char_p, C.c_int]),
@@ -807,6 +836,194 @@ def ds_swiglu8_grad(saved, dh, dgu=None, dgu_t=None, h_t=None, stream=None):
     return check("ds_swiglu8_grad",
                  lib.ds_swiglu8_grad(saved._p, p, t, cols, saved.cols - cols, ld, dgu and dgu._p,
                                      dgu_t and dgu_t._p, h_t and h_t._p, _q8_stream(stream, dev)))
+
+
+class Cache8:
+    """Keys and values of sequences in 8 bits, in pages of ``page`` tokens: ``k`` and ``v`` [pages, heads,
+    page, dim] of ``torch.float8_e4m3fn`` or ``float8_e5m2``, and one scale a row in ``k_scale`` and
+    ``v_scale`` [pages, heads, page] of ``torch.float8_e8m0fnu`` (powers of two) or ``float32``.
+    Cache8(pages, heads, dim) allocates them, uninitialised: what no token was written to is never
+    used.  Cache8.of wraps tensors that exist.
+
+    The operators on it run as those of Q8 do: on the one GPU that holds their operands, on its current
+    stream unless one is given."""
+
+    def __init__(self, pages, heads, dim, page=64, dtype=None, *, scale=None, device="cuda"):
+        def rows():
+            return _torch.empty(pages, heads, page, dim, dtype=_torch.uint8,
+                                device=device).view(dtype or _torch.float8_e4m3fn)
+
+        def scales():
+            return _torch.empty(pages, heads, page, dtype=scale or _torch.float8_e8m0fnu, device=device)
+        self._wrap(rows(), rows(), scales(), scales())
+
+    @classmethod
+    def of(cls, k, v, k_scale, v_scale):
+        """The cache held in these tensors, which it shares.  Pages may lie apart (k and v the halves of one
+        tensor), as far in k as in v; what is inside a page lies in order."""
+        c = cls.__new__(cls)
+        c._wrap(k, v, k_scale, v_scale)
+        return c
+
+    def _wrap(self, k, v, k_scale, v_scale):
+        fmt = {_torch.float8_e4m3fn: DS_Q8_E4M3, _torch.float8_e5m2: DS_Q8_E5M2}.get(k.dtype)
+        kind = {_torch.float8_e8m0fnu: DS_SCALE_POW2, _torch.float32: DS_SCALE_F32}.get(k_scale.dtype)
+        if fmt is None or kind is None or v.dtype != k.dtype or v_scale.dtype != k_scale.dtype:
+            raise TypeError(f"a cache of {k.dtype} and {v.dtype} with scales of {k_scale.dtype} and {v_scale.dtype}")
+        pages, heads, page, dim = k.shape
+        if v.shape != k.shape or tuple(k_scale.shape) != (pages, heads, page) or v_scale.shape != k_scale.shape:
+            raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}, scales {tuple(k_scale.shape)} and "
+                             f"{tuple(v_scale.shape)}")
+        if len({t.get_device() for t in (k, v, k_scale, v_scale)}) != 1:
+            raise ValueError("k, v and their scales are not on one device")
+        stride = [_page_stride(t) for t in (k, v)]
+        sstride = [_page_stride(t) for t in (k_scale, v_scale)]
+        if pages > 1 and (stride[0] != stride[1] or sstride[0] != sstride[1]):
+            raise ValueError(f"pages {stride} bytes and {sstride} scales apart")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pages, self.heads, self.page, self.dim = pages, heads, page, dim
+        self._device = k.get_device()
+        self._c = ds_cache8(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), pages, stride[0],
+                            sstride[0], page, heads, dim, fmt, kind, 0)
+        self._p = C.addressof(self._c)
+
+    def values(self):
+        """The fp32 values of all pages' keys and values (new tensors)."""
+        return tuple(x.to(_torch.float32) * s.to(_torch.float32)[..., None]
+                     for x, s in ((self.k, self.k_scale), (self.v, self.v_scale)))
+
+
+def _page_stride(t):
+    """Elements between pages of a cache's tensor whose pages are whole."""
+    want = 1
+    for n, s in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if n > 1 and s != want:
+            raise ValueError(f"a page's elements do not lie in order: strides {t.stride()} of {tuple(t.shape)}")
+        want *= n
+    return t.stride(0) if t.shape[0] > 1 else (want + 15) // 16 * 16
+
+
+class Chunk:
+    """What a call's new tokens belong to: int32 tensors on the GPU, whose contents may change between calls
+    and replays.  Sequence b has tokens starts[b] .. starts[b + 1] - 1 (``starts`` [seqs + 1]), the last of
+    its ``lengths[b]`` tokens; its token at position p lies in page ``table[b, p // page]``."""
+
+    def __init__(self, starts, lengths, table):
+        for name, t, dims in (("starts", starts, 1), ("lengths", lengths, 1), ("table", table, 2)):
+            if t.dtype != _torch.int32 or t.dim() != dims:
+                raise TypeError(f"{name}: {t.dtype} of {t.dim()} dimensions, not int32 of {dims}")
+            if t.shape[-1] > 1 and t.stride(-1) != 1:
+                raise ValueError(f"{name}: elements {t.stride(-1)} apart, not side by side")
+        seqs = lengths.shape[0]
+        if starts.shape[0] != seqs + 1 or table.shape[0] != seqs:
+            raise ValueError(f"{starts.shape[0]} starts and {table.shape[0]} rows of pages of {seqs} sequences")
+        if not starts.get_device() == lengths.get_device() == table.get_device():
+            raise ValueError("starts, lengths and table are not on one device")
+        self.starts, self.lengths, self.table = starts, lengths, table
+        self._device = starts.get_device()
+        cols = table.shape[1]
+        ld = table.stride(0) if seqs > 1 else max(cols, table.stride(0))
+        self._c = ds_chunk(starts.data_ptr(), lengths.data_ptr(), table.data_ptr(), seqs, cols, ld)
+        self._p = C.addressof(self._c)
+
+
+def _heads(t):
+    """The C form of a tensor [tokens, heads, dim] whose rows' elements are side by side."""
+    if t.dtype not in _PLAIN:
+        raise TypeError(f"fp32, fp16 or bf16, not {t.dtype}")
+    tokens, heads, dim = t.shape
+    ld, hld, one = t.stride()
+    if one != 1 and dim > 1:
+        raise ValueError(f"elements of a row are {one} apart, not side by side")
+    return ds_heads(t.data_ptr(), tokens, heads, dim, ld, hld, _PLAIN[t.dtype], 0)
+
+
+def _list(t, dtype, n, what):
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what}: {t.dtype} of shape {tuple(t.shape)}, not {n} of {dtype} side by side")
+    return t.data_ptr()
+
+
+def ds_rotary(x, pos, freqs, y=None, *, pairs=False, scale=1.0, inverse=False, stream=None):
+    """x [tokens, heads, dim] turned by its tokens' positions (pos [tokens], int32) in y, or in place:
+    pair i of the first 2 * len(freqs) values of each head by pos * freqs[i] (fp32), times scale.
+    pairs: values 2 i and 2 i + 1 in place of i and i + len(freqs).  inverse: by the opposite angle, which
+    takes the gradient of y to the gradient of x."""
+    y = x if y is None else y
+    dev = _q8_device(x.get_device(), pos.get_device(), freqs.get_device(), y.get_device())
+    if dev != _torch.cuda.current_device():
+        with _torch.cuda.device(dev):
+            return ds_rotary(x, pos, freqs, y, pairs=pairs, scale=scale, inverse=inverse, stream=stream)
+    mode = (DS_ROTARY_PAIRS if pairs else DS_ROTARY_HALVES) + (DS_ROTARY_INVERSE if inverse else 0)
+    n = freqs.numel()
+    return check("ds_rotary", lib.ds_rotary(C.byref(_heads(x)), _list(pos, _torch.int32, x.shape[0], "pos"),
+                                            _list(freqs, _torch.float32, n, "freqs"), 2 * n, mode, scale,
+                                            C.byref(_heads(y)), _q8_stream(stream, dev)))
+
+
+def _cache8_rows(name, cache, chunk, k, v, stream):
+    dev = _q8_device(cache._device, chunk._device, k.get_device(), v.get_device())
+    if dev != _torch.cuda.current_device():
+        with _torch.cuda.device(dev):
+            return _cache8_rows(name, cache, chunk, k, v, stream)
+    return check(name, getattr(lib, name)(cache._p, chunk._p, C.byref(_heads(k)), C.byref(_heads(v)),
+                                          _q8_stream(stream, dev)))
+
+
+def ds_cache8_write(cache, chunk, k, v, stream=None):
+    """The rows of k and v [tokens, cache heads, dim] (fp32, fp16, bf16) in 8 bits to the places of their
+    tokens in the cache."""
+    return _cache8_rows("ds_cache8_write", cache, chunk, k, v, stream)
+
+
+def ds_cache8_read(cache, chunk, k, v, stream=None):
+    """The rows of the tokens' places in the cache back in k and v [tokens, cache heads, dim]."""
+    return _cache8_rows("ds_cache8_read", cache, chunk, k, v, stream)
+
+
+def ds_attn8_work(q, cache, chunk, *, scale=None, causal=True, window=0, max_len=0):
+    """Bytes of the workspace of ds_attn8 with these arguments."""
+    n = C.c_int64()
+    cfg = ds_attn8_cfg(q.shape[2] ** -0.5 if scale is None else scale, causal, 0, window, max_len)
+    check("ds_attn8_work", lib.ds_attn8_work(C.byref(_heads(q)), cache._p, chunk._p, C.byref(cfg), C.byref(n)))
+    return n.value
+
+
+def ds_attn8(q, cache, chunk, out, lse=None, *, scale=None, causal=True, window=0, max_len=0, work=None,
+             stream=None):
+    """Attention of q [tokens, heads, dim] over the keys and values of the tokens' sequences in the cache, in
+    out; log of the sums in lse [tokens, heads] (fp32) unless that is None.  scale: dim ** -0.5 unless given.
+    causal: keys up to the token's own position, the latest ``window`` of them if that is not 0.  max_len: no sequence
+    is longer (0: what the table holds); a low one keeps the split of few tokens' work even.
+    work: a uint8 tensor of ds_attn8_work bytes, this call's until it is done; allocated if None."""
+    dev = _q8_device(q.get_device(), cache._device, chunk._device, out.get_device(), lse if lse is None else lse.get_device(),
+                     work if work is None else work.get_device())
+    if dev != _torch.cuda.current_device():
+        with _torch.cuda.device(dev):
+            return ds_attn8(q, cache, chunk, out, lse, scale=scale, causal=causal, window=window, max_len=max_len,
+                            work=work, stream=stream)
+    cfg = C.byref(ds_attn8_cfg(q.shape[2] ** -0.5 if scale is None else scale, causal, 0, window, max_len))
+    qh, oh = C.byref(_heads(q)), C.byref(_heads(out))
+    if lse is not None and (lse.dtype != _torch.float32 or tuple(lse.shape) != tuple(q.shape[:2]) or
+                            not lse.is_contiguous()):
+        raise ValueError(f"lse: {lse.dtype} of shape {tuple(lse.shape)}, not float32 of {tuple(q.shape[:2])}")
+    handle = _q8_stream(stream, dev)
+    if work is None:
+        n = C.c_int64()
+        check("ds_attn8", lib.ds_attn8_work(qh, cache._p, chunk._p, cfg, C.byref(n)))
+        need = n.value
+        if need:
+            if stream is None:
+                work = _torch.empty(need, dtype=_torch.uint8, device=q.device)
+            else:                        # the stream's own memory: it is given back in its order
+                with _torch.cuda.stream(_torch.cuda.ExternalStream(handle or 0, device=q.device)
+                                        if isinstance(stream, int) else stream):
+                    work = _torch.empty(need, dtype=_torch.uint8, device=q.device)
+    else:
+        if work.dtype != _torch.uint8 or not work.is_contiguous():
+            raise ValueError(f"work: {work.dtype}, not uint8 side by side")
+        need = work.numel()
+    return check("ds_attn8", lib.ds_attn8(qh, cache._p, chunk._p, cfg, oh, ptr(lse), ptr(work), need, handle))
 
 
 def ds_gen_uniform(seed, n):

@@ -27,7 +27,8 @@ ARCH = "gfx950"
 
 HOST_SOURCES = ["space.cpp", "tuner.cpp"]
 HIP_SOURCES = ["harness.hip", "kern_reduce.hip", "kern_conv_split.hip", "kern_conv_few.hip",
-               "kern_q8.hip", "kern_q8_matmul.hip"]
+               "kern_q8.hip", "kern_q8_matmul.hip", "kern_cache8.hip", "kern_attn8.hip",
+               "kern_attn8_bf16.hip", "kern_attn8_f16.hip", "kern_attn8_f32.hip"]
 SLICED_SOURCES = ["kern_conv.hip", "kern_matmul.hip"]
 
 HIP_FLAGS = [

@@ -1,0 +1,206 @@
+// Attention over the paged 8-bit cache: the launch, and the join of parts.
+#include <cmath>
+
+#include "attn8.h"
+#include "kern_common.h"
+#include "q8.h"
+
+namespace ds {
+namespace {
+
+// A wave joins the parts of a row, in the order of the splits.
+template <typename T>
+__global__ __launch_bounds__(256) void attn8_join(AttnArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t at = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+    const int64_t rows = int64_t(a.n.tokens) * a.heads;
+    if (at >= rows) return;
+    const int t = int(at / a.heads), hd = int(at - int64_t(t) * a.heads);
+    int b = 0;
+    for (int n = a.n.seqs; n > 1;) {
+        const int by = (n + 63) / 64;
+        const bool ok = lane == 0 || (lane * by < n && a.n.starts[b + lane * by] <= t);
+        const int k = 63 - __clzll(__ballot(ok));
+        b += k * by;
+        n = min(by, n - k * by);
+    }
+    if (a.n.starts[b] > t || t >= a.n.starts[b + 1]) return;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < a.splits) ml = a.ml[lane * rows + at];
+    float top = ml.x;
+#pragma unroll
+    for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
+    const float by = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
+    float l = 0.f;
+    floatx4 sum = {};
+    const int d = 4 * lane;
+    for (int s = 0; s < a.splits; ++s) {
+        const float ls = __shfl(ml.y, s), bs = __shfl(by, s);
+        if (ls == 0.f) continue;
+        l += ls * bs;
+        if (d < a.c.dim) sum += bs * *reinterpret_cast<const floatx4 *>(a.part + (s * rows + at) * a.c.dim + d);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if (a.lse && lane == 0) a.lse[at] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+    if (d >= a.c.dim) return;
+    T *op = static_cast<T *>(a.out) + t * a.ldo + hd * a.hldo + d;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) op[e] = T(sum[e] * inv);
+}
+
+// ---- host ---------------------------------------------------------------------------
+
+struct AttnPlan {
+    int rows;                             // of a tile
+    bool few;
+    int nq;
+    int splits, span;
+    int64_t tiles, groups, bytes, part;   // part: bytes of the sums, a multiple of 16
+};
+
+int attn_check(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg) {
+    int rc;
+    if ((rc = heads_check(q, "q", false)) != DS_OK || (rc = cache8_check(cache)) != DS_OK ||
+        (rc = chunk_check(chunk, cache)) != DS_OK)
+        return rc;
+    if (q->dim != cache->dim || q->heads % cache->heads != 0) {
+        set_error("q has %lld heads of %lld values, the cache %d of %d", (long long)q->heads, (long long)q->dim,
+                  cache->heads, cache->dim);
+        return DS_EINVAL;
+    }
+    if (q->type == DS_TYPE_F32 && cache->dim > 128) {
+        // (three parts of such queries do not fit the registers beside the sums)
+        set_error("fp32 queries of %d values (up to 128; 16-bit ones up to 256)", cache->dim);
+        return DS_EUNSUPPORTED;
+    }
+    if (!cfg || !std::isfinite(cfg->scale) || !std::isfinite(float(cfg->scale * 1.4426950408889634)) ||
+        (cfg->causal != 0 && cfg->causal != 1) || cfg->reserved != 0 ||
+        cfg->window < 0 || (cfg->window > 0 && !cfg->causal) || cfg->max_len < 0) {
+        if (cfg)
+            set_error("scale %g, causal %d, window %lld (only with causal), max_len %lld, reserved %d", cfg->scale,
+                      cfg->causal, (long long)cfg->window, (long long)cfg->max_len, cfg->reserved);
+        else
+            set_error("null cfg");
+        return DS_EINVAL;
+    }
+    return DS_OK;
+}
+
+int most_keys(const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg) {
+    const int64_t held = chunk->table_cols * cache->page;
+    return int(cfg->max_len > 0 ? std::min(cfg->max_len, held) : held);
+}
+
+// Tiles and splits from what the host knows: tokens, sequences, heads and the most keys.
+AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg) {
+    AttnPlan p{};
+    const int64_t group = q->heads / cache->heads, rows = q->tokens * group;
+    p.few = rows <= 64 * chunk->seqs;
+    p.nq = p.few ? 1 : attn8_blocks(q->type == DS_TYPE_F32, attn8_dim_blocks(cache->dim));
+    p.rows = p.few ? 32 : kWaves * 32 * p.nq;
+    p.tiles = rows / p.rows + chunk->seqs;
+    const int64_t base = p.tiles * cache->heads;
+    int64_t keys = most_keys(cache, chunk, cfg);
+    if (cfg->window > 0) keys = std::min(keys, cfg->window + p.rows / group + 1 + kKeys);
+    const int64_t unit = p.few ? kWaves * kKeys : kKeys * 8;
+    const int64_t want = std::max<int64_t>(1, (p.few ? 1024 : 512) / std::max<int64_t>(1, base));
+    int64_t splits = std::min({want, (keys + unit - 1) / unit, int64_t(kMostSplits)});
+    splits = std::max<int64_t>(1, splits);
+    int64_t span = ((keys + splits - 1) / splits + unit - 1) / unit * unit;
+    p.span = int(std::max(span, unit));
+    p.splits = int(std::max<int64_t>(1, (keys + p.span - 1) / p.span));
+    p.groups = p.tiles * cache->heads * p.splits;
+    if (p.splits > 1) {
+        p.part = p.splits * q->tokens * q->heads * cache->dim * 4;
+        p.bytes = p.part + p.splits * q->tokens * q->heads * 8;
+    }
+    return p;
+}
+
+template <typename T>
+int run(const AttnPlan &p, const AttnArgs &a, hipStream_t stream) {
+    AttnArgs args = a;
+    void *argv[] = {&args};
+    if (!hip_ok(hipLaunchKernel(attn8_kernel<T>(a.c.fmt, a.c.dim, p.few), dim3(unsigned(p.groups)), dim3(64 * kWaves), argv, 0,
+                                stream),
+                "ds_attn8"))
+        return DS_EHIP;
+    if (p.splits > 1) {
+        const int64_t rows = int64_t(a.n.tokens) * a.heads;
+        attn8_join<T><<<unsigned((rows + kWaves - 1) / kWaves), 256, 0, stream>>>(a);
+        if (!hip_ok(hipGetLastError(), "ds_attn8")) return DS_EHIP;
+    }
+    return DS_OK;
+}
+
+}  // namespace
+}  // namespace ds
+
+using namespace ds;
+
+extern "C" {
+
+int ds_attn8_work(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg,
+                  int64_t *bytes) {
+    const int rc = attn_check(q, cache, chunk, cfg);
+    if (rc != DS_OK) return rc;
+    if (!bytes) {
+        set_error("null bytes");
+        return DS_EINVAL;
+    }
+    *bytes = q->tokens == 0 || chunk->seqs == 0 ? 0 : attn_plan(q, cache, chunk, cfg).bytes;
+    return DS_OK;
+}
+
+int ds_attn8(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg,
+             const ds_heads *out, float *lse, void *work, int64_t work_bytes, hipStream_t stream) {
+    int rc = attn_check(q, cache, chunk, cfg);
+    if (rc != DS_OK || (rc = heads_check(out, "out", true)) != DS_OK) return rc;
+    if (out->tokens != q->tokens || out->heads != q->heads || out->dim != q->dim || out->type != q->type) {
+        set_error("out is %lld x %lld x %lld of type %d, q %lld x %lld x %lld of type %d", (long long)out->tokens,
+                  (long long)out->heads, (long long)out->dim, out->type, (long long)q->tokens, (long long)q->heads,
+                  (long long)q->dim, q->type);
+        return DS_EINVAL;
+    }
+    if (reinterpret_cast<uintptr_t>(lse) % 4 != 0) {
+        set_error("misaligned lse");
+        return DS_EINVAL;
+    }
+    if (q->tokens == 0 || chunk->seqs == 0) return DS_OK;
+    const AttnPlan p = attn_plan(q, cache, chunk, cfg);
+    if (work_bytes < p.bytes || (p.bytes > 0 && (!work || reinterpret_cast<uintptr_t>(work) % 16 != 0))) {
+        set_error("a workspace of %lld bytes, 16-byte aligned, not %lld at %p", (long long)p.bytes,
+                  (long long)work_bytes, work);
+        return DS_EINVAL;
+    }
+    if ((rc = launch_check(p.groups, 256, "ds_attn8")) != DS_OK ||
+        (rc = launch_check((q->tokens * q->heads + kWaves - 1) / kWaves, 256, "ds_attn8")) != DS_OK)
+        return rc;
+    AttnArgs a{};
+    a.c = cache_view(cache);
+    a.n = chunk_view(chunk, cache, q->tokens);
+    a.q = q->data;
+    a.out = out->data;
+    a.ldq = q->ld;
+    a.hldq = q->head_ld;
+    a.ldo = out->ld;
+    a.hldo = out->head_ld;
+    a.lse = lse;
+    a.part = static_cast<float *>(work);
+    a.ml = reinterpret_cast<float2 *>(static_cast<char *>(work) + p.part);
+    a.scale = float(cfg->scale * 1.4426950408889634);
+    a.heads = int(q->heads);
+    a.group = int(q->heads / cache->heads);
+    a.causal = cfg->causal;
+    a.window = int(std::min<int64_t>(cfg->window, kMaxPlaces));
+    a.len = most_keys(cache, chunk, cfg);
+    a.splits = p.splits;
+    a.span = p.span;
+    a.vec_q = heads16(q);
+    a.vec_o = heads16(out);
+    if (q->type == DS_TYPE_F32) return run<float>(p, a, stream);
+    if (q->type == DS_TYPE_F16) return run<_Float16>(p, a, stream);
+    return run<__bf16>(p, a, stream);
+}
+
+}  // extern "C"
