@@ -774,7 +774,7 @@ typedef struct {
  * calls give the same bits, in `work` (16-byte aligned, work_bytes of it, as ds_attn8_work
  * says for the same arguments; 0 bytes need no pointer): the caller's, for this call until it is done.
  * Asynchronous; allocates nothing.  Errors: DS_EINVAL, DS_EHIP, DS_EUNSUPPORTED (fp32 queries of more
- * than 128 values; 2^32 threads or more).
+ * than 128 values; 2^31 rows or more of tokens and the heads that share a cache head; 2^32 threads or more).
  */
 int ds_attn8(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg,
              const ds_heads *out, float *lse, void *work, int64_t work_bytes, hipStream_t stream);

@@ -5,9 +5,6 @@
 
 namespace ds {
 
-constexpr int kWaves = 4;
-constexpr int kKeys = 32;                 // keys of a tile
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kMostSplits = 64;
 
 struct AttnArgs {
@@ -22,19 +19,31 @@ struct AttnArgs {
     float scale;                          // times log2 e
     int heads, group;                     // query heads, and those of a cache head
     int causal, window, len;              // len: most keys of a sequence that are seen
-    int splits, span;                     // keys of a split, a multiple of 32 (kWaves * 32 if waves share rows)
-    int tiles;                            // of rows
-    int vec_q, vec_o;
-    FastDiv f_group;
+    int splits, span;                     // keys of a split
+    int vec_q, vec_o;                     // rows of 16-byte groups
+    FastDiv f_group, f_kv, f_splits;
 };
 
-// Blocks of 32 values that a row of dim is taken as: 2, 4 or 8.
+// Three forms of the kernel (attn8_kernel.h): waves that share 32 rows and split the keys; waves of 32 rows
+// each that read keys by themselves; waves of 32 rows each that share the keys through LDS.
+enum { kAttnShare, kAttnOwn, kAttnTiles };
+constexpr int attn8_threads(int form) { return form == kAttnTiles ? 512 : 256; }
+constexpr int attn8_rows(int form) { return form == kAttnShare ? 32 : attn8_threads(form) / 2; }
 constexpr int attn8_dim_blocks(int dim) { return dim <= 64 ? 2 : dim <= 128 ? 4 : 8; }
-// Blocks of 32 rows of a wave that has rows of its own.
-constexpr int attn8_blocks(bool f32, int dim_blocks) { return f32 || dim_blocks == 8 ? 1 : 1; }
 
+// Whether the many rows of a type and width take kAttnOwn (else kAttnTiles): where the registers hold no more
+// than one wave a SIMD unit.
+template <typename T>
+constexpr bool attn8_own_form(int dim_blocks) {
+    return sizeof(T) == 4 || dim_blocks == 8;
+}
+
+struct AttnKernel {
+    const void *func;
+    int lds;                              // bytes of dynamic LDS
+};
 // The kernel of a type (float, _Float16, __bf16).
 template <typename T>
-const void *attn8_kernel(int fmt, int dim, bool few);
+AttnKernel attn8_kernel(int form, int fmt, int stype, int dim);
 
 }  // namespace ds

@@ -1,17 +1,23 @@
 // Attention of new tokens over the paged 8-bit cache.
 //
-// For one cache head a row is a pair of a new token and one of the query heads that share it.  A wave takes 32 (or
-// 64) rows and walks over tiles of 32 keys with the running maximum m and sum l of each row's softmax.  It
+// For one cache head a row is a pair of a new token and one of the query heads that share it.  A wave takes 32
+// rows and walks over tiles of 32 or 64 keys with the running maximum m and sum l of each row's softmax.  It
 // computes the products transposed, on 32x32x16 matrix instructions:
-//     S^T = K Q^T:  lane (i, h), i = lane % 32, h = lane / 32, has S of row i and 16 of the tile's keys,
+//     S^T = K Q^T:  lane (i, h), i = lane % 32, h = lane / 32, has S of row i and 16 of 32 keys,
 //     O^T = V^T P^T: and the same lane needs P of row i and 8 keys an instruction as the second operand:
 // those that it holds, if V's keys are taken in the same order.  So weights never leave their lane, and a
-// row's maximum is one of 16 registers and one exchange of halves.  Keys and values come from memory
-// as they lie: a lane's 16 bytes of a key's row are the first operand of two instructions (Q in the same order of
-// values), and its 4 bytes (dims up to 128) of eight keys' rows are those of four, transposed by byte
-// permutes, a value and its neighbour key's in one conversion.  There is no LDS on that way and no barrier.
+// row's maximum is one of its registers and one exchange of halves.
+//
+// Few rows: memory bounds it.  Keys and values come from memory as they lie, without LDS and without a barrier: a lane's 16
+// bytes of a key's row are the first operand of two instructions (Q in the same order of values), and its 4 bytes
+// (dims up to 128) of eight keys' rows are those of four, transposed by byte permutes, a value and its
+// neighbour key's in one conversion.
+//
+// Many rows: the matrix and the vector unit bound it, and decoding is a third of the vector unit's work if each wave does it.
+// So eight waves share decoded tiles of 64 keys in LDS, K by rows and V by columns.
 #pragma once
 
+#include <cmath>
 #include <type_traits>
 
 #include "attn8.h"
@@ -23,6 +29,9 @@ namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kKeys = 32;                 // keys of a matrix instruction's tile
+constexpr float kLn2 = 0.69314718055994530942f;
 
 // How the types compute: Q in QP parts of operand type, P in PP parts of bf16.
 template <typename T>
@@ -50,11 +59,11 @@ __device__ __forceinline__ floatx16 mma(f16x8 a, f16x8 b, floatx16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-// Eight bytes of a key's row as an operand: exact in both types.
+// Eight bytes of a key's row as an operand, times a power of two (1 for fp16): exact in both types.
 template <int FMT, typename Op>
-__device__ __forceinline__ Op decode_k(int lo, int hi) {
+__device__ __forceinline__ Op decode_k(int lo, int hi, float by = 1.f) {
     if constexpr (std::is_same_v<Op, bf16x8>) {
-        return to_bf16<FMT>(lo, hi);
+        return to_bf16<FMT>(lo, hi, by);
     } else {
         const int w[2] = {lo, hi};
         f16x8 r;
@@ -87,6 +96,255 @@ __device__ __forceinline__ unsigned not_finite(unsigned w) {
     else return ((w & 0x7c7c7c7cu) + 0x04040404u) & 0x80808080u;
 }
 
+// Two of a word's bytes as bf16, times a power of two.
+template <int FMT, bool HIGH>
+__device__ __forceinline__ bf16x2 decode2(unsigned w, float by) {
+    if constexpr (FMT == DS_Q8_E4M3) return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(int(w), by, HIGH);
+    else return __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(int(w), by, HIGH);
+}
+
+__device__ __forceinline__ float scale_of(unsigned stored, int stype) {
+    return stype == DS_SCALE_POW2 ? __uint_as_float(max(stored << 23, 0x400000u)) : __uint_as_float(stored);
+}
+__device__ __forceinline__ unsigned load_scale(const void *p, int stype, int64_t at) {
+    return stype == DS_SCALE_POW2 ? static_cast<const uint8_t *>(p)[at] : static_cast<const unsigned *>(p)[at];
+}
+
+// Key of register r among 32: the order in which both products take keys.
+__device__ __forceinline__ int key_of(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+// ---- a workgroup's and a wave's rows ------------------------------------------------------
+
+// Sequence of a tile of rows: the tiles of sequence b begin at starts[b] * group / rows + b, which leaves each at
+// least as many as it needs, without a sum over the sequences before it.
+template <int ROWS>
+__device__ __forceinline__ int first_tile(const AttnArgs &a, int b) {
+    return int(unsigned(min(max(a.n.starts[b], 0), a.n.tokens)) * unsigned(a.group) / ROWS) + b;
+}
+
+struct Work {
+    int b, head, split;                   // sequence, cache head, split (all uniform)
+    int len;                              // keys of the sequence that may be seen
+    int s0, rows;                         // its first token, its rows
+    int row0;                             // the workgroup's first row
+    int64_t shift;                        // token s0 + t is at position shift + t
+
+    __device__ __forceinline__ int token(const AttnArgs &a, int r) const { return fdiv(min(r, rows - 1), a.f_group); }
+    // the rows of token t see keys low .. lim - 1
+    __device__ __forceinline__ int lim(const AttnArgs &a, int t) const {
+        return a.causal ? int(min(max(shift + t + 1, int64_t(0)), int64_t(len))) : len;
+    }
+    __device__ __forceinline__ int low(const AttnArgs &a, int t) const {
+        return a.window > 0 ? int(max(min(shift + t + 1 - a.window, int64_t(len)), int64_t(0))) : 0;
+    }
+    // Keys of the split for the workgroup's rows, [from, until): its first key is the tile's, a multiple of 64.
+    __device__ __forceinline__ void keys(const AttnArgs &a, int last_row, int &from, int &until) const {
+        const int base = low(a, token(a, row0)) & ~63;
+        from = int(min(int64_t(base) + int64_t(split) * a.span, kMaxPlaces)) & ~63;
+        until = int(min(int64_t(lim(a, token(a, last_row))), int64_t(base) + int64_t(split + 1) * a.span));
+    }
+};
+
+template <int ROWS>
+__device__ __forceinline__ bool find_work(const AttnArgs &a, Work &w) {
+    const int lane = threadIdx.x & 63;
+    // heads side by side: workgroups go to the chip's eight parts in turn, so the workgroups of a head
+    // share the caches of as few parts as the number of heads allows
+    const int idx = fdiv(blockIdx.x, a.f_kv);
+    w.head = int(blockIdx.x) - idx * a.c.heads;
+    const int tile = fdiv(idx, a.f_splits);
+    w.split = idx - tile * a.splits;
+    int b = 0;
+    for (int n = a.n.seqs; n > 1;) {       // 64 sequences a step
+        const int by = (n + 63) / 64;
+        const bool ok = lane == 0 || (lane * by < n && first_tile<ROWS>(a, b + lane * by) <= tile);
+        const int k = 63 - __clzll(__ballot(ok));
+        b += k * by;
+        n = min(by, n - k * by);
+    }
+    w.b = __builtin_amdgcn_readfirstlane(b);
+    const int length = a.n.lengths[w.b], end = a.n.starts[w.b + 1];
+    w.s0 = min(max(a.n.starts[w.b], 0), a.n.tokens);
+    const int s1 = min(max(end, w.s0), a.n.tokens);
+    w.rows = (s1 - w.s0) * a.group;
+    const int mine = tile - (int(unsigned(w.s0) * unsigned(a.group) / ROWS) + w.b), all = (w.rows + ROWS - 1) / ROWS;
+    if (mine < 0 || mine >= all) return false;
+    // the last rows, which see most keys, first
+    w.row0 = (a.causal ? all - 1 - mine : mine) * ROWS;
+    w.len = min(max(length, 0), a.len);
+    w.shift = int64_t(length) - (s1 - w.s0);
+    return true;
+}
+
+// A lane's row.
+struct Row {
+    int tok, head;
+    bool is;
+    int low, lim;
+};
+__device__ __forceinline__ Row find_row(const AttnArgs &a, const Work &w, int r) {
+    const int t = w.token(a, r);
+    return {w.s0 + t, w.head * a.group + min(r, w.rows - 1) - t * a.group, r < w.rows, w.low(a, t), w.lim(a, t)};
+}
+
+// The row of Q as operands: operand 2 c + u of a lane has values 32 c + 16 h + 8 u and on.
+template <typename T, int DB>
+__device__ __forceinline__ void load_q(const AttnArgs &a, const Row &row, int h, float by,
+                                       typename Parts<T>::Op (&q)[Parts<T>::QP][2 * DB]) {
+    const T *qp = static_cast<const T *>(a.q) + row.tok * a.ldq + row.head * a.hldq;
+#pragma unroll
+    for (int c = 0; c < 2 * DB; ++c) {
+        const int d = 32 * (c >> 1) + 16 * h + 8 * (c & 1);
+        T x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = T(0.f);
+        if (d < a.c.dim) {
+            if (a.vec_q) {
+#pragma unroll
+                for (size_t e = 0; e < sizeof(x) / 16; ++e)
+                    reinterpret_cast<intx4 *>(x)[e] = reinterpret_cast<const intx4 *>(qp + d)[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = qp[d + e];
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (Parts<T>::QP == 1) {
+                q[0][c][e] = T(float(x[e]) * by);
+            } else {
+                float rest = float(x[e]) * by;
+#pragma unroll
+                for (int p = 0; p < Parts<T>::QP; ++p) {
+                    q[p][c][e] = __bf16(rest);
+                    rest -= float(q[p][c][e]);
+                }
+            }
+        }
+    }
+}
+
+// ---- a row's sums -----------------------------------------------------------------------------
+
+// Register r of block blk is value DB * i + blk of the lane's row, i = key_of(r, h).
+template <int DB>
+struct Sums {
+    floatx16 o[DB];
+    float m, l;                           // l: of the lane's half of the keys until halves() joins them
+
+    __device__ __forceinline__ void clear() {
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int blk = 0; blk < DB; ++blk) o[blk] = floatx16{};
+    }
+    // The running maximum follows `top` only by steps of 2^8 or more: any number near it serves, as weights
+    // of up to 2^8 lose nothing in fp32 or bf16.  Returns what weights are taken from.
+    __device__ __forceinline__ float follow(float top) {
+        if (__any(top > m + 8.f || (m == -INFINITY && top > -INFINITY))) {
+            const float now = fmaxf(m, top);
+            const float by = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
+            m = now;
+            l *= by;
+#pragma unroll
+            for (int blk = 0; blk < DB; ++blk)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[blk][r] *= by;
+        }
+        return m == -INFINITY ? 0.f : m;
+    }
+};
+
+// w in parts of bf16, element e of an operand.
+template <int PP>
+__device__ __forceinline__ void put_weight(bf16x8 (&to)[PP], int e, float w) {
+#pragma unroll
+    for (int part = 0; part < PP; ++part) {
+        const __bf16 top8 = __bf16(w);
+        to[part][e] = top8;
+        w -= float(top8);
+    }
+}
+
+// The second product where V holds infinities or NaNs and some row does not see all keys: 0 times those
+// is no 0.  They are taken out of V, and a second product counts for each row and value how many
+// that it sees are +infinity (units of 1), -infinity (64) and NaN (4096): sums of up to 32, exact.
+template <int PP>
+__device__ __forceinline__ void add_poisoned(floatx16 &o, const bf16x8 (&v)[2], const bf16x8 (&p)[2][PP],
+                                             const bf16x8 (&seen)[2]) {
+    floatx16 count = {};
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+        bf16x8 fin, kind;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float f = v[st][e];
+            const bool fine = fabsf(f) < INFINITY;
+            fin[e] = __bf16(fine ? f : 0.f);
+            kind[e] = __bf16(fine ? 0.f : f > 0.f ? 1.f : f < 0.f ? 64.f : 4096.f);
+        }
+#pragma unroll
+        for (int part = PP - 1; part >= 0; --part) o = mma(fin, p[st][part], o);
+        count = mma(kind, seen[st], count);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const float c = count[r];
+        const bool nan = c >= 4096.f, minus = c >= 64.f, plus = c - (minus ? 64.f * floorf(c / 64.f) : 0.f) > 0.f;
+        const float add = nan || (minus && plus) ? NAN : minus ? -INFINITY : INFINITY;
+        o[r] = c > 0.f ? o[r] + add : o[r];
+    }
+}
+
+// What a wave's rows come to: written, or left as a part of them.
+template <typename T, int DB>
+__device__ __forceinline__ void finish(const AttnArgs &a, const Work &w, const Row &row, const Sums<DB> &s, int h) {
+    if (!row.is) return;
+    const int64_t at = int64_t(row.tok) * a.heads + row.head;
+    if (a.splits > 1) {
+        const int64_t p = int64_t(w.split) * a.n.tokens * a.heads + at;
+        if (h == 0) a.ml[p] = make_float2(s.m, s.l);
+        if (s.l == 0.f) return;
+        float *to = a.part + p * a.c.dim;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int d = DB * key_of(r, h);
+            if (d < a.c.dim) {
+#pragma unroll
+                for (int blk = 0; blk < DB; blk += 2) {
+                    typedef float floatx2 __attribute__((ext_vector_type(2)));
+                    *reinterpret_cast<floatx2 *>(to + d + blk) = floatx2{s.o[blk][r], s.o[blk + 1][r]};
+                }
+            }
+        }
+        return;
+    }
+    const float by = s.l == 0.f ? 0.f : 1.f / s.l;
+    if (a.lse && h == 0) a.lse[at] = s.l == 0.f ? -INFINITY : (s.m + log2f(s.l)) * kLn2;
+    T *to = static_cast<T *>(a.out) + row.tok * a.ldo + row.head * a.hldo;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+        const int d = DB * key_of(r, h);
+        if (d >= a.c.dim) continue;
+        T x[DB];
+#pragma unroll
+        for (int blk = 0; blk < DB; ++blk) x[blk] = T(s.l == 0.f ? 0.f : s.o[blk][r] * by);
+        if (a.vec_o) {
+            // (DB values of a 16-byte row: 4 bytes at least, aligned to their size up to 16)
+            constexpr int kBytes = sizeof(x) < 16 ? sizeof(x) : 16;
+            typedef int intv __attribute__((ext_vector_type(kBytes / 4)));
+#pragma unroll
+            for (size_t e = 0; e < sizeof(x) / kBytes; ++e)
+                reinterpret_cast<intv *>(to + d)[e] = reinterpret_cast<const intv *>(x)[e];
+        } else {
+#pragma unroll
+            for (int blk = 0; blk < DB; ++blk) to[d + blk] = x[blk];
+        }
+    }
+}
+
+// ---- keys and values straight from memory -----------------------------------------------------------
+
 // The tile's bytes of a lane.  DB: blocks of 32 values that a row is taken as (2, 4 or 8), also the
 // bytes of a lane of each key of V.
 template <int DB>
@@ -98,25 +356,38 @@ struct Tile {
     int valid;                            // keys of each 16 that exist: low and high half word
 };
 
-template <typename T, int FMT, int DB, int NQ, bool SHARE>
-struct Attn {
+// The lane's DB bytes of a row of V, 0 past its end.
+template <int DB>
+__device__ __forceinline__ void load_v(const uint8_t *p, unsigned at, bool is, unsigned (&w)[DB == 8 ? 2 : 1]) {
+    if constexpr (DB == 2) {
+        w[0] = is ? *reinterpret_cast<const uint16_t *>(p + at) : 0;
+    } else if constexpr (DB == 4) {
+        w[0] = is ? *reinterpret_cast<const unsigned *>(p + at) : 0;
+    } else {
+        intx2 x = {};
+        if (is) x = *reinterpret_cast<const intx2 *>(p + at);
+        w[0] = x[0];
+        w[1] = x[1];
+    }
+}
+
+template <typename T, int FMT, int DB>
+struct Direct {
     using P = Parts<T>;
     using Op = typename P::Op;
-    static constexpr int kRows = 32 * NQ;                          // of a wave
-    static constexpr int kTileRows = SHARE ? kRows : kWaves * kRows;
 
     const AttnArgs &a;
+    const Work &w;
+    const Row &row;
+    const Op (&q)[P::QP][2 * DB];
+    Sums<DB> &s;
     const int lane, i, h;
-    int b, head;                                                   // sequence, cache head (uniform)
-    int len;                                                       // its keys that may be seen
-    const uint8_t *kbase, *vbase;
-    unsigned koff, voff;                                                // of the lane in a 16-key part of a page
-    Op q[P::QP][NQ][2 * DB];
-    floatx16 o[NQ][DB];
-    float m[NQ], l[NQ];
-    int lim[NQ], low[NQ];                                          // the row sees keys low .. lim - 1
+    const unsigned koff, voff;            // of the lane in a 16-key part of a page
 
-    __device__ __forceinline__ Attn(const AttnArgs &args) : a(args), lane(threadIdx.x & 63), i(lane & 31), h(lane >> 5) {}
+    __device__ __forceinline__ Direct(const AttnArgs &a_, const Work &w_, const Row &r_, const Op (&q_)[P::QP][2 * DB],
+                                      Sums<DB> &s_)
+        : a(a_), w(w_), row(r_), q(q_), s(s_), lane(threadIdx.x & 63), i(lane & 31), h(lane >> 5),
+          koff((i & 15) * a_.c.dim + 16 * h), voff(4 * h * a_.c.dim + DB * i) {}
 
     // The two pages of a tile: numbers (kNoPlace if there is none) and offsets.
     struct Pages {
@@ -125,11 +396,11 @@ struct Attn {
     __device__ __forceinline__ Pages pages(int key0) const {
         Pages p;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int key = key0 + 16 * s;
-            const Place at = key < len ? place_at(a.c, a.n, b, key) : Place{kNoPlace, 0};
-            p.id[s] = at.page;
-            p.off[s] = at.off;
+        for (int st = 0; st < 2; ++st) {
+            const int key = key0 + 16 * st;
+            const Place at = key < w.len ? place_at(a.c, a.n, w.b, key) : Place{kNoPlace, 0};
+            p.id[st] = at.page;
+            p.off[st] = at.off;
         }
         return p;
     }
@@ -139,16 +410,16 @@ struct Attn {
     __device__ __forceinline__ void load(Tile<DB> &t, const Pages &p, int key0) const {
         const int dim = a.c.dim;
         int valid[2];
-        int64_t row[2];
+        int64_t page[2];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int id = __builtin_amdgcn_readfirstlane(p.id[s]);
-            valid[s] = id >= 0 ? min(16, len - key0 - 16 * s) : 0;
-            row[s] = max(id, 0);
+        for (int st = 0; st < 2; ++st) {
+            const int id = __builtin_amdgcn_readfirstlane(p.id[st]);
+            valid[st] = id >= 0 ? min(16, w.len - key0 - 16 * st) : 0;
+            page[st] = max(id, 0);
         }
         t.valid = valid[0] | valid[1] << 16;
-        const int at[2] = {head * a.c.page + p.off[0], head * a.c.page + p.off[1]};
-        const int64_t byte[2] = {row[0] * a.c.stride + int64_t(at[0]) * dim, row[1] * a.c.stride + int64_t(at[1]) * dim};
+        const int at[2] = {w.head * a.c.page + p.off[0], w.head * a.c.page + p.off[1]};
+        const int64_t byte[2] = {page[0] * a.c.stride + int64_t(at[0]) * dim, page[1] * a.c.stride + int64_t(at[1]) * dim};
         const bool up = i & 16;
         const uint8_t *kp = a.c.k + (up ? byte[1] : byte[0]) + koff;
 #pragma unroll
@@ -157,465 +428,544 @@ struct Attn {
             if (32 * c + 16 * h < dim) t.k[c] = *reinterpret_cast<const intx4 *>(kp + 32 * c);
         }
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int st = 0; st < 2; ++st)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint8_t *vp = a.c.v + byte[s] + (e < 4 ? e : e + 4) * dim;
-                if constexpr (DB == 2) t.v[s][e][0] = DB * i < dim ? *reinterpret_cast<const uint16_t *>(vp + voff) : 0;
-                else if constexpr (DB == 4) t.v[s][e][0] = DB * i < dim ? *reinterpret_cast<const unsigned *>(vp + voff) : 0;
-                else {
-                    intx2 w = {};
-                    if (DB * i < dim) w = *reinterpret_cast<const intx2 *>(vp + voff);
-                    t.v[s][e][0] = w[0];
-                    t.v[s][e][1] = w[1];
-                }
-            }
-        const int64_t se = (up ? row[1] : row[0]) * a.c.sstride + (up ? at[1] : at[0]) + (i & 15);
-        const void *sp = h ? a.c.vs : a.c.ks;
-        t.s = a.c.stype == DS_SCALE_POW2 ? static_cast<const uint8_t *>(sp)[se] : static_cast<const unsigned *>(sp)[se];
+            for (int e = 0; e < 8; ++e)
+                load_v<DB>(a.c.v + byte[st] + (e < 4 ? e : e + 4) * dim, voff, DB * i < dim, t.v[st][e]);
+        const int64_t se = (up ? page[1] : page[0]) * a.c.sstride + (up ? at[1] : at[0]) + (i & 15);
+        t.s = load_scale(h ? a.c.vs : a.c.ks, a.c.stype, se);
     }
 
-    // The operand of block blk and keys of step s: row i of it is value DB i + blk.
-    __device__ __forceinline__ bf16x8 decode_v(const Tile<DB> &t, int s, int blk) const {
-        const int w = blk >> 2, j = blk & 3;
+    // The operand of block blk and 16 keys: row i of it is value DB i + blk.
+    __device__ __forceinline__ bf16x8 decode_v(const Tile<DB> &t, int st, int blk) const {
+        const int word = blk >> 2, j = blk & 3;
         bf16x8 r;
-        int pair[4];
+        unsigned pair[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            pair[e] = int(__builtin_amdgcn_perm(t.v[s][2 * e + 1][w], t.v[s][2 * e][w], j & 2 ? 0x07030602u : 0x05010400u));
+            pair[e] = __builtin_amdgcn_perm(t.v[st][2 * e + 1][word], t.v[st][2 * e][word], j & 2 ? 0x07030602u : 0x05010400u);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            bf16x2 x;
-            if constexpr (FMT == DS_Q8_E4M3)
-                x = j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(pair[e], 1.f, true)
-                          : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(pair[e], 1.f, false);
-            else
-                x = j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(pair[e], 1.f, true)
-                          : __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(pair[e], 1.f, false);
+            const bf16x2 x = j & 1 ? decode2<FMT, true>(pair[e], 1.f) : decode2<FMT, false>(pair[e], 1.f);
             r[2 * e] = x[0];
             r[2 * e + 1] = x[1];
         }
         return r;
     }
 
-    // Key of register r in the tile: the order in which both products take keys.
-    __device__ __forceinline__ int key_of(int r) const { return 8 * (r >> 2) + 4 * h + (r & 3); }
-
-    // One tile; edge: some row does not see some key of it, or some key does not exist.  POISON: see poisoned();
-    // without it, false where that is needed.
+    // One tile; edge: some row does not see some key of it, or some key does not exist.  POISON: with
+    // add_poisoned; without it, false where that is needed.
     template <bool POISON>
     __device__ __forceinline__ bool step(Tile<DB> &t, int key0, bool edge, float *lds) {
         // the scales of all 32 keys to every lane that needs them; 0 of keys that do not exist
         const int valid[2] = {t.valid & 0xffff, t.valid >> 16};
-        float sc = a.c.stype == DS_SCALE_POW2 ? __uint_as_float(max(t.s << 23, 0x400000u)) : __uint_as_float(t.s);
-        if (edge) sc = (i & 15) < (i & 16 ? valid[1] : valid[0]) ? sc : 0.f;
+        float sc = scale_of(t.s, a.c.stype);
+        if (POISON || edge) sc = (i & 15) < (i & 16 ? valid[1] : valid[0]) ? sc : 0.f;
         lds[lane] = h ? sc : sc * a.scale;
         __builtin_amdgcn_wave_barrier();
-        floatx16 s[NQ] = {};
+        floatx16 sum = {};
 #pragma unroll
         for (int c = 0; c < DB; ++c)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const Op k = decode_k<FMT, Op>(t.k[c][2 * u], t.k[c][2 * u + 1]);
 #pragma unroll
-                for (int p = P::QP - 1; p >= 0; --p)
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) s[n] = mma(k, q[p][n][2 * c + u], s[n]);
+                for (int p = P::QP - 1; p >= 0; --p) sum = mma(k, q[p][2 * c + u], sum);
             }
         __builtin_amdgcn_sched_barrier(0);
-        bf16x8 pt[NQ][P::PP][2], seen[NQ][2];
-        unsigned bad = 0;
+        bf16x8 pt[2][P::PP], seen[2];
         if (POISON || edge) {
+            unsigned bad = 0;
 #pragma unroll
             for (int st = 0; st < 2; ++st)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
 #pragma unroll
-                    for (int w = 0; w < Tile<DB>::W; ++w) {
-                        unsigned &x = t.v[st][e][w];
+                    for (int word = 0; word < Tile<DB>::W; ++word) {
+                        unsigned &x = t.v[st][e][word];
                         if (4 * h + (e < 4 ? e : e + 4) >= valid[st]) x = 0;
                         bad |= not_finite<FMT>(x);
                     }
             if (!POISON && __any(bad != 0)) return false;
         }
+        float x[16];
 #pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            float x[16];
+        for (int j = 0; j < 4; ++j) {
+            const floatx4 sk = *reinterpret_cast<const floatx4 *>(lds + 8 * j + 4 * h);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const floatx4 sk = *reinterpret_cast<const floatx4 *>(lds + 8 * j + 4 * h);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[4 * j + e] = s[n][4 * j + e] * sk[e];
-            }
-            if (POISON || edge)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int k = key_of(r);
-                    const bool sees = key0 + k >= low[n] && key0 + k < lim[n] && (k & 15) < valid[r >> 3];
-                    x[r] = sees ? x[r] : -INFINITY;
-                    if constexpr (POISON) seen[n][r >> 3][r & 7] = __bf16(sees ? 1.f : 0.f);
-                }
-            float top = fmaxf(x[0], x[1]);
-#pragma unroll
-            for (int r = 2; r < 16; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
-            top = fmaxf(top, other_half(top));
-            // the running maximum follows only by steps of 2^8 or more: any number near it serves, as weights
-            // of up to 2^8 lose nothing in fp32 or bf16
-            if (__any(top > m[n] + 8.f || (m[n] == -INFINITY && top > -INFINITY))) {
-                const float now = fmaxf(m[n], top);
-                const float by = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[n] - now);
-                m[n] = now;
-                l[n] *= by;
-#pragma unroll
-                for (int blk = 0; blk < DB; ++blk)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[n][blk][r] *= by;
-            }
-            const float off = m[n] == -INFINITY ? 0.f : m[n];
+            for (int e = 0; e < 4; ++e) x[4 * j + e] = sum[4 * j + e] * sk[e];
+        }
+        if (POISON || edge)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                x[r] = __builtin_amdgcn_exp2f(x[r] - off);
-                l[n] += x[r];
+                const int k = key_of(r, h);
+                const bool sees = key0 + k >= row.low && key0 + k < row.lim && (k & 15) < valid[r >> 3];
+                x[r] = sees ? x[r] : -INFINITY;
+                if constexpr (POISON) seen[r >> 3][r & 7] = __bf16(sees ? 1.f : 0.f);
             }
+        float top = fmaxf(x[0], x[1]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const floatx4 sv = *reinterpret_cast<const floatx4 *>(lds + 32 + 8 * j + 4 * h);
+        for (int r = 2; r < 16; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
+        const float off = s.follow(fmaxf(top, other_half(top)));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float w = x[4 * j + e] * sv[e];
+        for (int r = 0; r < 16; ++r) {
+            x[r] = __builtin_amdgcn_exp2f(x[r] - off);
+            s.l += x[r];
+        }
 #pragma unroll
-                    for (int part = 0; part < P::PP; ++part) {
-                        const __bf16 top8 = __bf16(w);
-                        pt[n][part][j >> 1][4 * (j & 1) + e] = top8;
-                        w -= float(top8);
-                    }
-                }
-            }
+        for (int j = 0; j < 4; ++j) {
+            const floatx4 sv = *reinterpret_cast<const floatx4 *>(lds + 32 + 8 * j + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) put_weight<P::PP>(pt[j >> 1], 4 * (j & 1) + e, x[4 * j + e] * sv[e]);
         }
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (POISON) {
-            poisoned(t, pt, seen);
-            return true;
-        }
 #pragma unroll
-        for (int blk = 0; blk < DB; ++blk)
+        for (int blk = 0; blk < DB; ++blk) {
+            const bf16x8 v[2] = {decode_v(t, 0, blk), decode_v(t, 1, blk)};
+            if constexpr (POISON) {
+                add_poisoned<P::PP>(s.o[blk], v, pt, seen);
+            } else {
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                const bf16x8 v = decode_v(t, st, blk);
+                for (int st = 0; st < 2; ++st)
 #pragma unroll
-                for (int part = P::PP - 1; part >= 0; --part)
-#pragma unroll
-                    for (int n = 0; n < NQ; ++n) o[n][blk] = mma(v, pt[n][part][st], o[n][blk]);
+                    for (int part = P::PP - 1; part >= 0; --part) s.o[blk] = mma(v[st], pt[st][part], s.o[blk]);
             }
+        }
         return true;
     }
 
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-            m[n] = -INFINITY;
-            l[n] = 0.f;
-#pragma unroll
-            for (int blk = 0; blk < DB; ++blk) o[n][blk] = floatx16{};
-        }
-    }
-
-    // The second product where V holds infinities or NaNs and some row does not see all keys: 0 times those
-    // is no 0. They are taken out of V, and a second product counts for each row and value how many
-    // that it sees are +infinity (units of 1), -infinity (64) and NaN (4096): sums of up to 32, exact.
-    __device__ __forceinline__ void poisoned(const Tile<DB> &t, const bf16x8 (&pt)[NQ][P::PP][2],
-                                             const bf16x8 (&seen)[NQ][2]) {
-#pragma unroll
-        for (int blk = 0; blk < DB; ++blk) {
-            floatx16 count[NQ] = {};
-#pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                bf16x8 v = decode_v(t, st, blk), kind;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float f = v[e];
-                    const bool fine = fabsf(f) < INFINITY;
-                    v[e] = __bf16(fine ? f : 0.f);
-                    kind[e] = __bf16(fine ? 0.f : f > 0.f ? 1.f : f < 0.f ? 64.f : 4096.f);
-                }
-#pragma unroll
-                for (int n = 0; n < NQ; ++n) {
-#pragma unroll
-                    for (int part = P::PP - 1; part >= 0; --part) o[n][blk] = mma(v, pt[n][part][st], o[n][blk]);
-                    count[n] = mma(kind, seen[n][st], count[n]);
-                }
+    // The keys from `key` on in steps of STEP, until `until`; every, since: keys that all rows of the wave see.
+    template <int STEP>
+    __device__ __forceinline__ void walk(int key, int until, int every, int since, float *lds) {
+        bool fine = true;
+        const int begin = key;
+        const auto edge = [&](const Tile<DB> &t) {
+            return key + kKeys > every || key < since || t.valid != (16 | 16 << 16);
+        };
+        s.clear();
+        if constexpr (DB == 8) {
+            // (the registers hold one tile of 256 values a row)
+            for (; key < until && fine; key += STEP) {
+                Tile<DB> t;
+                load(t, pages(key), key);
+                fine = step<false>(t, key, edge(t), lds);
             }
-#pragma unroll
-            for (int n = 0; n < NQ; ++n)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float c = count[n][r];
-                    const bool nan = c >= 4096.f, minus = c >= 64.f, plus = c - (minus ? 64.f * floorf(c / 64.f) : 0.f) > 0.f;
-                    if (nan || (minus && plus)) o[n][blk][r] = NAN;
-                    else if (c > 0.f) o[n][blk][r] += minus ? -INFINITY : INFINITY;
-                }
+        } else if (key < until) {
+            Tile<DB> t[2];
+            load(t[0], pages(key), key);
+            Pages next = pages(key + STEP);
+            const auto one = [&](Tile<DB> &now, Tile<DB> &then) {
+                const Pages after = pages(key + 2 * STEP);
+                if (key + STEP < until) load(then, next, key + STEP);
+                next = after;
+                fine = step<false>(now, key, edge(now), lds);
+                key += STEP;
+            };
+            while (true) {
+                one(t[0], t[1]);
+                if (key >= until || !fine) break;
+                one(t[1], t[0]);
+                if (key >= until || !fine) break;
+            }
+        }
+        if (!fine) slow<STEP>(begin, until, lds);
+    }
+    template <int STEP>
+    __device__ __forceinline__ void slow(int key, int until, float *lds) {
+        s.clear();
+#pragma unroll 1
+        for (; key < until; key += STEP) {
+            Tile<DB> t;
+            load(t, pages(key), key);
+            step<true>(t, key, true, lds);
         }
     }
 };
-
-// Sequence of a tile of rows: the tiles of sequence b begin at starts[b] * group / rows + b, which leaves each at
-// least as many as it needs, without a sum over the sequences before it.
-__device__ __forceinline__ int64_t first_tile(const AttnArgs &a, int b, int rows) {
-    const int s = min(max(a.n.starts[b], 0), a.n.tokens);
-    return int64_t(s) * a.group / rows + b;
-}
-
-template <typename T, int FMT, int DB, int NQ, bool SHARE>
-__device__ __forceinline__ void attn8_body(const AttnArgs &a, float *scales, float *join) {
-    using A = Attn<T, FMT, DB, NQ, SHARE>;
-    using P = typename A::P;
-    A w(a);
-    const int lane = w.lane, i = w.i, h = w.h;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kv = a.c.heads;
-    // heads side by side: workgroups go to the chip's eight parts in turn, so the workgroups of a head
-    // share the caches of as few parts as the number of heads allows
-    int idx = blockIdx.x;
-    w.head = idx % kv;
-    idx /= kv;
-    const int split = idx % a.splits;
-    const int tile = idx / a.splits;
-
-    int b = 0;
-    for (int n = a.n.seqs; n > 1;) {       // 64 sequences a step
-        const int by = (n + 63) / 64;
-        const bool ok = lane == 0 || (lane * by < n && first_tile(a, b + lane * by, A::kTileRows) <= tile);
-        const int k = 63 - __clzll(__ballot(ok));
-        b += k * by;
-        n = min(by, n - k * by);
-    }
-    b = __builtin_amdgcn_readfirstlane(b);
-    w.b = b;
-    const int s0 = min(max(a.n.starts[b], 0), a.n.tokens), s1 = min(max(a.n.starts[b + 1], s0), a.n.tokens);
-    const int64_t rows = int64_t(s1 - s0) * a.group;
-    const int64_t mine = tile - first_tile(a, b, A::kTileRows);
-    if (mine < 0 || mine * A::kTileRows >= rows) return;
-    // the last rows, which see most keys, first
-    const int64_t all = (rows + A::kTileRows - 1) / A::kTileRows;
-    const int64_t row0 = (a.causal ? all - 1 - mine : mine) * A::kTileRows + (SHARE ? 0 : wave * A::kRows);
-    const int length = a.n.lengths[b];
-    w.len = min(max(length, 0), a.len);
-    // row r is token s0 + r / group at position length - (s1 - s0) + r / group
-    const int64_t shift = int64_t(length) - (s1 - s0);
-    const auto token = [&](int64_t r) { return int(min(r, rows - 1) / a.group); };
-    const auto limit = [&](int t) { return a.causal ? int(min(max(shift + t + 1, int64_t(0)), int64_t(w.len))) : w.len; };
-    const auto lowest = [&](int t) { return a.window > 0 ? int(max(min(shift + t + 1 - a.window, int64_t(w.len)), int64_t(0))) : 0; };
-
-    int tok[NQ], hd[NQ];
-    bool is[NQ];
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        const int64_t r = row0 + 32 * n + i;
-        is[n] = r < rows;
-        const int t = token(r);
-        tok[n] = s0 + t;
-        hd[n] = w.head * a.group + int(min(r, rows - 1) - int64_t(t) * a.group);
-        w.lim[n] = limit(t);
-        w.low[n] = lowest(t);
-        const T *qp = static_cast<const T *>(a.q) + tok[n] * a.ldq + hd[n] * a.hldq;
-#pragma unroll
-        for (int c = 0; c < 2 * DB; ++c) {
-            const int d = 32 * (c >> 1) + 16 * h + 8 * (c & 1);
-            T x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = T(0.f);
-            if (d < a.c.dim) {
-                if (a.vec_q) {
-#pragma unroll
-                    for (size_t e = 0; e < sizeof(x) / 16; ++e)
-                        reinterpret_cast<intx4 *>(x)[e] = reinterpret_cast<const intx4 *>(qp + d)[e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = qp[d + e];
-                }
-            }
-            if constexpr (P::QP == 1) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) w.q[0][n][c][e] = x[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float rest = x[e];
-#pragma unroll
-                    for (int p = 0; p < P::QP; ++p) {
-                        w.q[p][n][c][e] = __bf16(rest);
-                        rest -= float(w.q[p][n][c][e]);
-                    }
-                }
-            }
-        }
-    }
-    w.koff = (i & 15) * a.c.dim + 16 * h;
-    w.voff = 4 * h * a.c.dim + DB * i;
-
-    // the wave's keys: those that its rows see, from the tile's first
-    const int64_t first = SHARE ? row0 : row0 - wave * A::kRows;
-    const int base = lowest(token(first)) & ~(kKeys - 1);
-    const int from = max(lowest(token(row0)) & ~(kKeys - 1), int(min(int64_t(base) + int64_t(split) * a.span, kMaxPlaces)) & ~(kKeys - 1));
-    const int until = int(min(int64_t(row0 < rows ? limit(token(row0 + A::kRows - 1)) : 0),
-                              int64_t(base) + int64_t(split + 1) * a.span));
-    // keys that all its rows see
-    const int every = limit(token(row0)), since = lowest(token(row0 + A::kRows - 1));
-    constexpr int kStep = SHARE ? kWaves * kKeys : kKeys;
-    const int begin = from + (SHARE ? wave * kKeys : 0);
-    float *lds = scales + wave * 64;
-    w.clear();
-    bool fine = true;
-    const auto edge = [&](int key, const Tile<DB> &t) {
-        return key + kKeys > every || key < since || t.valid != (16 | 16 << 16);
-    };
-    if constexpr (DB == 8) {
-        // (the registers hold one tile of 256 values a row)
-        for (int key = begin; key < until && fine; key += kStep) {
-            Tile<DB> t;
-            w.load(t, w.pages(key), key);
-            fine = w.template step<false>(t, key, edge(key, t), lds);
-        }
-    } else if (begin < until) {
-        int key = begin;
-        Tile<DB> t[2];
-        w.load(t[0], w.pages(key), key);
-        typename A::Pages next = w.pages(key + kStep);
-        const auto one = [&](Tile<DB> &now, Tile<DB> &then) {
-            const typename A::Pages after = w.pages(key + 2 * kStep);
-            if (key + kStep < until) w.load(then, next, key + kStep);
-            next = after;
-            fine = w.template step<false>(now, key, edge(key, now), lds);
-            key += kStep;
-        };
-        while (true) {
-            one(t[0], t[1]);
-            if (key >= until || !fine) break;
-            one(t[1], t[0]);
-            if (key >= until || !fine) break;
-        }
-    }
-    if (!fine) {
-        w.clear();
-#pragma unroll 1
-        for (int key = begin; key < until; key += kStep) {
-            Tile<DB> t;
-            w.load(t, w.pages(key), key);
-            w.template step<true>(t, key, true, lds);
-        }
-    }
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) w.l[n] += other_half(w.l[n]);
-
-    if constexpr (SHARE) {
-        // four waves' sums of the same rows: two halves of the waves, then two waves
-#pragma unroll
-        for (int half = kWaves / 2; half > 0; half /= 2) {
-            constexpr int kSlot = 64 + 64 * 16 * DB;
-            __syncthreads();
-            if (wave >= half && wave < 2 * half) {
-                float *to = join + (wave - half) * kSlot;
-                if (h == 0) {
-                    to[i] = w.m[0];
-                    to[32 + i] = w.l[0];
-                }
-#pragma unroll
-                for (int blk = 0; blk < DB; ++blk)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) to[64 + (blk * 16 + r) * 64 + lane] = w.o[0][blk][r];
-            }
-            __syncthreads();
-            if (wave < half) {
-                const float *of = join + wave * kSlot;
-                const float om = of[i], ol = of[32 + i], now = fmaxf(w.m[0], om);
-                const float by = w.m[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m[0] - now);
-                const float bo = om == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(om - now);
-                w.m[0] = now;
-                w.l[0] = w.l[0] * by + ol * bo;
-#pragma unroll
-                for (int blk = 0; blk < DB; ++blk)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        w.o[0][blk][r] = w.o[0][blk][r] * by + of[64 + (blk * 16 + r) * 64 + lane] * bo;
-            }
-        }
-        if (wave != 0) return;
-    }
-
-    // register r of block blk is value DB * row + blk, row = 8 (r / 4) + 4 h + r % 4
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-        if (!is[n]) continue;
-        const int64_t at = int64_t(tok[n]) * a.heads + hd[n];
-        if (a.splits > 1) {
-            const int64_t p = int64_t(split) * a.n.tokens * a.heads + at;
-            if (h == 0) a.ml[p] = make_float2(w.m[n], w.l[n]);
-            if (w.l[n] == 0.f) continue;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int d = DB * (8 * (r >> 2) + 4 * h + (r & 3));
-                if (d < a.c.dim)
-#pragma unroll
-                    for (int blk = 0; blk < DB; ++blk) a.part[p * a.c.dim + d + blk] = w.o[n][blk][r];
-            }
-            continue;
-        }
-        const float by = w.l[n] == 0.f ? 0.f : 1.f / w.l[n];
-        if (a.lse && h == 0) a.lse[at] = w.l[n] == 0.f ? -INFINITY : (w.m[n] + log2f(w.l[n])) * kLn2;
-        T *op = static_cast<T *>(a.out) + tok[n] * a.ldo + hd[n] * a.hldo;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int d = DB * (8 * (r >> 2) + 4 * h + (r & 3));
-            if (d < a.c.dim)
-#pragma unroll
-                for (int blk = 0; blk < DB; ++blk) op[d + blk] = T(w.l[n] == 0.f ? 0.f : w.o[n][blk][r] * by);
-        }
-    }
-}
 
 // Waves of a SIMD unit: two where their registers allow it.
 template <typename T, int DB>
 constexpr int waves_of = DB <= 4 && !std::is_same_v<T, float> ? 2 : 1;
 
-// Waves that share rows take tiles of keys in turn.
+// Four waves share 32 rows and take tiles of keys in turn.
 template <typename T, int FMT, int DB>
-__global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_few(AttnArgs a) {
-    __shared__ __attribute__((aligned(16))) float scales[kWaves * 64];
-    __shared__ float join[2 * (64 + 64 * 16 * DB)];
-    attn8_body<T, FMT, DB, 1, true>(a, scales, join);
-}
-// Each wave has rows of its own.
-template <typename T, int FMT, int DB, int NQ>
-__global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_many(AttnArgs a) {
-    __shared__ __attribute__((aligned(16))) float scales[kWaves * 64];
-    attn8_body<T, FMT, DB, NQ, false>(a, scales, nullptr);
+__global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a) {
+    constexpr int kSlot = 64 + 64 * 16 * DB;
+    __shared__ __attribute__((aligned(16))) float scales[4 * 64];
+    __shared__ float join[2 * kSlot];
+    Work w;
+    if (!find_work<32>(a, w)) return;
+    const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Row row = find_row(a, w, w.row0 + i);
+    typename Parts<T>::Op q[Parts<T>::QP][2 * DB];
+    load_q<T, DB>(a, row, h, 1.f, q);
+    int from, until;
+    w.keys(a, w.row0 + 31, from, until);
+    Sums<DB> s;
+    Direct<T, FMT, DB>(a, w, row, q, s)
+        .template walk<4 * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
+                                  w.low(a, w.token(a, w.row0 + 31)), scales + wave * 64);
+    s.l += other_half(s.l);
+    // four waves' sums of the same rows: two waves take another's each, then one
+#pragma unroll
+    for (int half = 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (wave >= half && wave < 2 * half) {
+            float *to = join + (wave - half) * kSlot;
+            if (h == 0) {
+                to[i] = s.m;
+                to[32 + i] = s.l;
+            }
+#pragma unroll
+            for (int blk = 0; blk < DB; ++blk)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) to[64 + (blk * 16 + r) * 64 + lane] = s.o[blk][r];
+        }
+        __syncthreads();
+        if (wave < half) {
+            const float *of = join + wave * kSlot;
+            const float om = of[i], ol = of[32 + i], now = fmaxf(s.m, om);
+            const float by = s.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.m - now);
+            const float bo = om == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(om - now);
+            s.m = now;
+            s.l = s.l * by + ol * bo;
+#pragma unroll
+            for (int blk = 0; blk < DB; ++blk)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s.o[blk][r] = s.o[blk][r] * by + of[64 + (blk * 16 + r) * 64 + lane] * bo;
+        }
+    }
+    if (wave == 0) finish<T, DB>(a, w, row, s, h);
 }
 
+// Each wave has rows of its own and reads keys by itself.
+template <typename T, int FMT, int DB>
+__global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_own(AttnArgs a) {
+    __shared__ __attribute__((aligned(16))) float scales[4 * 64];
+    Work w;
+    if (!find_work<128>(a, w)) return;
+    const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = w.row0 + 32 * wave;
+    if (row0 >= w.rows) return;
+    const Row row = find_row(a, w, row0 + i);
+    typename Parts<T>::Op q[Parts<T>::QP][2 * DB];
+    load_q<T, DB>(a, row, h, 1.f, q);
+    int from, until;
+    w.keys(a, row0 + 31, from, until);
+    Sums<DB> s;
+    Direct<T, FMT, DB>(a, w, row, q, s)
+        .template walk<kKeys>(max(from, w.low(a, w.token(a, row0)) & ~(kKeys - 1)), until, w.lim(a, w.token(a, row0)),
+                              w.low(a, w.token(a, row0 + 31)), scales + wave * 64);
+    s.l += other_half(s.l);
+    finish<T, DB>(a, w, row, s, h);
+}
+
+// ---- keys and values decoded in LDS ---------------------------------------------------------------------
+
+constexpr int kTileKeys = 64;
+
+// A tile as operands of 16 bytes.  K: chunk c (values 8 c and on) of key r at r * 4 DB + (c ^ r % 8); V: the keys of
+// step st and half h, in key_of's order, of row blk * 32 + i at row * 8 + (2 st + h ^ i % 8): so that eight lanes
+// side by side read from all banks.
+template <int DB>
+struct TileLds {
+    intx4 k[kTileKeys * 4 * DB];
+    intx4 v[32 * DB * 8];
+    float sk[kTileKeys], sv[kTileKeys];   // fp32 scales, K's times a.scale
+    int note[4];                          // of each 16 keys: those that exist, and 1 << 16 if V holds no number
+};
+
+// Powers of two go into the operands: into V's (bf16), and into K's if those are bf16 too.
+template <typename T, int FMT, bool POW2, int DB>
+struct Tiles {
+    using P = Parts<T>;
+    using Op = typename P::Op;
+    static constexpr bool kFoldK = POW2 && std::is_same_v<Op, bf16x8>, kFoldV = POW2;
+    static constexpr int W = DB == 8 ? 2 : 1;
+    static constexpr int kPieces = 2 * DB;                         // 16-byte pieces of a row of K
+    static constexpr int kLoads = DB / 2;                          // of a thread
+    static_assert(kLoads <= 2, "a thread holds two scales");
+
+    const AttnArgs &a;
+    const Work &w;
+    const int lane, i, h, wave;
+
+    // What a thread of waves 0 to 3 holds of K, or one of waves 4 to 7 of V (wave 4 + st: keys 16 st and on).
+    struct Stage {
+        unsigned raw[8 * W];
+        unsigned sc0, sc1;                // scales as stored: of a K thread's loads, of a V thread's keys
+        int valid;
+    };
+
+    __device__ __forceinline__ Place place(int key) const {
+        Place p = key < w.len ? place_at(a.c, a.n, w.b, key) : Place{kNoPlace, 0};
+        p.page = __builtin_amdgcn_readfirstlane(p.page);
+        p.off = __builtin_amdgcn_readfirstlane(p.off);
+        return p;
+    }
+
+    __device__ __forceinline__ void load(Stage &st, int key0) const {
+        const int dim = a.c.dim;
+        if (wave < 4) {
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int r0 = j * (256 / kPieces) + wave * (64 / kPieces);   // the wave's first row: all in one part
+                const Place p = place(key0 + (r0 & ~15));
+                const int64_t page = max(p.page, 0);
+                const int r = (r0 & 15) + lane / kPieces, piece = lane % kPieces;
+                const int64_t at = w.head * a.c.page + p.off;
+                intx4 x = {};
+                if (16 * piece < dim)
+                    x = *reinterpret_cast<const intx4 *>(a.c.k + page * a.c.stride + at * dim + unsigned(r * dim + 16 * piece));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) st.raw[4 * j + e] = x[e];
+                const unsigned sc = load_scale(a.c.ks, POW2 ? DS_SCALE_POW2 : DS_SCALE_F32, page * a.c.sstride + at + r);
+                if (j == 0) st.sc0 = sc;
+                else st.sc1 = sc;
+            }
+        } else {
+            const int part = wave - 4, key = key0 + 16 * part;
+            const Place p = place(key);
+            const int64_t page = max(p.page, 0);
+            st.valid = p.page >= 0 ? min(16, w.len - key) : 0;
+            const int64_t at = w.head * a.c.page + p.off;
+            const uint8_t *vp = a.c.v + page * a.c.stride + at * dim;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                unsigned x[W];
+                load_v<DB>(vp + (e < 4 ? e : e + 4) * dim, unsigned(4 * h * dim + DB * i), DB * i < dim, x);
+#pragma unroll
+                for (int word = 0; word < W; ++word) st.raw[e * W + word] = x[word];
+            }
+            const int64_t se = page * a.c.sstride + at;
+            if constexpr (kFoldV) {
+                const uint8_t *sp = static_cast<const uint8_t *>(a.c.vs) + se + 4 * h;
+                __builtin_memcpy(&st.sc0, sp, 4);
+                __builtin_memcpy(&st.sc1, sp + 8, 4);
+            } else {
+                st.sc0 = static_cast<const unsigned *>(a.c.vs)[se + (lane & 15)];
+            }
+        }
+    }
+
+    __device__ __forceinline__ void store(Stage &st, TileLds<DB> &t) const {
+        if (wave < 4) {
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j) {
+                const int r = j * (256 / kPieces) + wave * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
+                const float by = scale_of(j == 0 ? st.sc0 : st.sc1, POW2 ? DS_SCALE_POW2 : DS_SCALE_F32);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const Op k = decode_k<FMT, Op>(st.raw[4 * j + 2 * u], st.raw[4 * j + 2 * u + 1], kFoldK ? by : 1.f);
+                    t.k[r * 4 * DB + ((2 * piece + u) ^ (r & 7))] = __builtin_bit_cast(intx4, k);
+                }
+                if (!kFoldK && piece == 0) t.sk[r] = by * a.scale;
+            }
+        } else {
+            const int part = wave - 4;
+            float by[8];
+            if constexpr (kFoldV) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) by[e] = scale_of((e < 4 ? st.sc0 : st.sc1) >> (8 * (e & 3)) & 0xff, DS_SCALE_POW2);
+            }
+            if (st.valid < 16) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (4 * h + (e < 4 ? e : e + 4) >= st.valid) {
+                        by[e] = 1.f;
+#pragma unroll
+                        for (int word = 0; word < W; ++word) st.raw[e * W + word] = 0;
+                    }
+            }
+            unsigned bad = 0;
+#pragma unroll
+            for (int e = 0; e < 8 * W; ++e) bad |= not_finite<FMT>(st.raw[e]);
+#pragma unroll
+            for (int word = 0; word < W; ++word)
+#pragma unroll
+                for (int pair = 0; pair < (DB == 2 ? 1 : 2); ++pair) {
+                    unsigned x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const unsigned raw = st.raw[e * W + word];
+                        const float s = kFoldV ? by[e] : 1.f;
+                        x[e] = __builtin_bit_cast(unsigned, pair ? decode2<FMT, true>(raw, s) : decode2<FMT, false>(raw, s));
+                    }
+#pragma unroll
+                    for (int odd = 0; odd < 2; ++odd) {
+                        intx4 y;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            y[e] = int(__builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], odd ? 0x07060302u : 0x05040100u));
+                        const int blk = 4 * word + 2 * pair + odd;
+                        t.v[(blk * 32 + i) * 8 + ((2 * part + h) ^ (i & 7))] = y;
+                    }
+                }
+            if (!kFoldV && lane < 16) t.sv[16 * part + lane] = lane < st.valid ? __uint_as_float(st.sc0) : 0.f;
+            const int note = max(st.valid, 0) | (__any(bad != 0) ? 1 << 16 : 0);
+            if (lane == 0) t.note[part] = note;
+        }
+    }
+
+    // 32 of the tile's keys; c: what sums are multiplied with (powers of two in K's operands).
+    __device__ __forceinline__ void step(const TileLds<DB> &t, int sub, int key0, bool edge, const intx4 &note, float c,
+                                         const Row &row, const Op (&q)[P::QP][2 * DB], Sums<DB> &s) const {
+        floatx16 sum = {};
+        const intx4 *kp = t.k + (32 * sub + i) * 4 * DB;
+#pragma unroll
+        for (int x = 0; x < 2 * DB; ++x) {
+            const Op k = __builtin_bit_cast(Op, kp[(4 * (x >> 1) + 2 * h + (x & 1)) ^ (i & 7)]);
+#pragma unroll
+            for (int p = P::QP - 1; p >= 0; --p) sum = mma(k, q[p][x], sum);
+        }
+        float x[16];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            floatx4 sk;
+            if constexpr (!kFoldK) sk = *reinterpret_cast<const floatx4 *>(t.sk + 32 * sub + 8 * j + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[4 * j + e] = kFoldK ? sum[4 * j + e] : sum[4 * j + e] * sk[e];
+        }
+        if (edge)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int k = 32 * sub + key_of(r, h);
+                const bool sees = key0 + k >= row.low && key0 + k < row.lim && (k & 15) < (note[2 * sub + (r >> 3)] & 0xffff);
+                x[r] = sees ? x[r] : -INFINITY;
+            }
+        float top = fmaxf(x[0], x[1]);
+#pragma unroll
+        for (int r = 2; r < 16; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
+        top = fmaxf(top, other_half(top));
+        const float off = s.follow(kFoldK ? top * c : top);
+        bf16x8 pt[2][P::PP];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            floatx4 sv;
+            if constexpr (!kFoldV) sv = *reinterpret_cast<const floatx4 *>(t.sv + 32 * sub + 8 * j + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float y = x[4 * j + e];
+                const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(y, c, -off) : y - off);
+                s.l += p;
+                put_weight<P::PP>(pt[j >> 1], 4 * (j & 1) + e, kFoldV ? p : p * sv[e]);
+            }
+        }
+#pragma unroll
+        for (int blk = 0; blk < DB; ++blk)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const bf16x8 v = __builtin_bit_cast(bf16x8, t.v[(blk * 32 + i) * 8 + ((4 * sub + 2 * st + h) ^ (i & 7))]);
+#pragma unroll
+                for (int part = P::PP - 1; part >= 0; --part) s.o[blk] = mma(v, pt[st][part], s.o[blk]);
+            }
+    }
+};
+
+// Waits for the waves' LDS accesses, and not for loads from memory that are on their way.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Eight waves of 32 rows each.  While a tile is used, the next is written to the other half of LDS and the one
+// after is on its way from memory: one barrier a tile.
+template <typename T, int FMT, bool POW2, int DB>
+__global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds_bytes[];
+    TileLds<DB> *lds = reinterpret_cast<TileLds<DB> *>(lds_bytes);
+    using Tl = Tiles<T, FMT, POW2, DB>;
+    Work w;
+    if (!find_work<256>(a, w)) return;
+    const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = w.row0 + 32 * wave;
+    const Row row = find_row(a, w, row0 + i);
+    int from, until;
+    w.keys(a, w.row0 + 255, from, until);
+    // what all rows of the workgroup see, and of the wave; what any row of the wave sees
+    const int wg_every = w.lim(a, w.token(a, w.row0)), wg_since = w.low(a, w.token(a, w.row0 + 255));
+    const int every = w.lim(a, w.token(a, row0)), since = w.low(a, w.token(a, row0 + 31));
+    const int last = row0 < w.rows ? w.lim(a, w.token(a, row0 + 31)) : 0, first = w.low(a, w.token(a, row0));
+    typename Parts<T>::Op q[Parts<T>::QP][2 * DB];
+    // powers of two in K's operands leave one factor for all sums; its sign goes into Q, so that the
+    // largest sum is the largest score
+    const float sign = a.scale < 0.f ? -1.f : a.scale > 0.f ? 1.f : 0.f, c = a.scale == 0.f ? 1.f : fabsf(a.scale);
+    load_q<T, DB>(a, row, h, Tl::kFoldK ? sign : 1.f, q);
+    Sums<DB> s;
+    s.clear();
+    const Tl tl{a, w, lane, i, h, wave};
+    bool fine = true;
+    if (from < until) {
+        typename Tl::Stage st;
+        tl.load(st, from);
+        tl.store(st, lds[0]);
+        if (from + kTileKeys < until) tl.load(st, from + kTileKeys);
+        int at = 0;
+        for (int key = from; key < until; key += kTileKeys, at ^= 1) {
+            lds_barrier();
+            const TileLds<DB> &t = lds[at];
+            if (key + kTileKeys < until) {
+                tl.store(st, lds[at ^ 1]);
+                if (key + 2 * kTileKeys < until) tl.load(st, key + 2 * kTileKeys);
+            }
+            intx4 note = *reinterpret_cast<const intx4 *>(t.note);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) note[e] = __builtin_amdgcn_readfirstlane(note[e]);
+            if (((note[0] | note[1] | note[2] | note[3]) >> 16) && (key + kTileKeys > wg_every || key < wg_since)) {
+                fine = false;
+                break;
+            }
+            const bool whole = (note[0] & note[1] & note[2] & note[3] & 0xffff) == 16;
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub) {
+                const int k0 = key + 32 * sub;
+                if (k0 < last && k0 + 32 > first)
+                    tl.step(t, sub, key, k0 + 32 > every || k0 < since || !whole, note, c, row, q, s);
+            }
+        }
+    }
+    if (!fine) {
+        // (the tile's buffers hold the waves' scales now)
+        __syncthreads();
+        if (Tl::kFoldK) load_q<T, DB>(a, row, h, 1.f, q);
+        Direct<T, FMT, DB>(a, w, row, q, s)
+            .template slow<kKeys>(max(from, first & ~(kKeys - 1)), min(until, last),
+                                  reinterpret_cast<float *>(lds_bytes) + wave * 64);
+    }
+    s.l += other_half(s.l);
+    finish<T, DB>(a, w, row, s, h);
+}
 
 }  // namespace
 
 template <typename T>
-const void *attn8_kernel(int fmt, int dim, bool few) {
-    constexpr int NQ = attn8_blocks(std::is_same_v<T, float>, 4);
-    constexpr int N8 = attn8_blocks(std::is_same_v<T, float>, 8);
-    const int db = attn8_dim_blocks(dim);
-    constexpr bool kWide = !std::is_same_v<T, float>;        // more than 128 values a row
-#define DS_ATTN8(FMT)                                                                                       \
-    if (fmt == FMT && db == 2)                                                                              \
-        return few ? reinterpret_cast<const void *>(&attn8_few<T, FMT, 2>)                                  \
-                   : reinterpret_cast<const void *>(&attn8_many<T, FMT, 2, NQ>);                            \
-    if (fmt == FMT && db == 4)                                                                              \
-        return few ? reinterpret_cast<const void *>(&attn8_few<T, FMT, 4>)                                  \
-                   : reinterpret_cast<const void *>(&attn8_many<T, FMT, 4, NQ>);                            \
-    if constexpr (kWide)                                                                                    \
-        if (fmt == FMT && db == 8)                                                                          \
-            return few ? reinterpret_cast<const void *>(&attn8_few<T, FMT, 8>)                              \
-                       : reinterpret_cast<const void *>(&attn8_many<T, FMT, 8, N8>);
-    DS_ATTN8(DS_Q8_E4M3)
-    DS_ATTN8(DS_Q8_E5M2)
-#undef DS_ATTN8
-    return nullptr;
+AttnKernel attn8_kernel(int form, int fmt, int stype, int dim) {
+    AttnKernel k{nullptr, 0};
+    const auto of_dim = [&](auto f, auto db) {
+        constexpr int FMT = f.value, DB = db.value;
+        if (form == kAttnShare) {
+            k.func = reinterpret_cast<const void *>(&attn8_share<T, FMT, DB>);
+        } else if (form == kAttnOwn) {
+            if constexpr (attn8_own_form<T>(DB)) k.func = reinterpret_cast<const void *>(&attn8_own<T, FMT, DB>);
+        } else {
+            if constexpr (!attn8_own_form<T>(DB)) {
+                k.func = stype == DS_SCALE_POW2 ? reinterpret_cast<const void *>(&attn8_tiles<T, FMT, true, DB>)
+                                                : reinterpret_cast<const void *>(&attn8_tiles<T, FMT, false, DB>);
+                k.lds = 2 * int(sizeof(TileLds<DB>));
+            }
+        }
+    };
+    const auto of_fmt = [&](auto f) {
+        const int db = attn8_dim_blocks(dim);
+        if (db == 2) of_dim(f, std::integral_constant<int, 2>{});
+        else if (db == 4) of_dim(f, std::integral_constant<int, 4>{});
+        else if constexpr (!std::is_same_v<T, float>) of_dim(f, std::integral_constant<int, 8>{});
+    };
+    if (fmt == DS_Q8_E4M3) of_fmt(std::integral_constant<int, DS_Q8_E4M3>{});
+    else of_fmt(std::integral_constant<int, DS_Q8_E5M2>{});
+    return k;
 }
 
 }  // namespace ds

@@ -8,14 +8,20 @@
 namespace ds {
 namespace {
 
-// A wave joins the parts of a row, in the order of the splits.
-template <typename T>
-__global__ __launch_bounds__(256) void attn8_join(AttnArgs a) {
+constexpr int kJoinWaves = 4;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// A wave joins the parts of a row: LPR lanes take four values each of every 64 / LPR-th split, four at a
+// time (their loads together), and the groups of lanes are added up in order.
+template <typename T, int LPR>
+__global__ __launch_bounds__(64 * kJoinWaves) void attn8_join(AttnArgs a) {
     const int lane = threadIdx.x & 63;
-    const int64_t at = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
+    const int64_t at = int64_t(blockIdx.x) * kJoinWaves + (threadIdx.x >> 6);
     const int64_t rows = int64_t(a.n.tokens) * a.heads;
     if (at >= rows) return;
     const int t = int(at / a.heads), hd = int(at - int64_t(t) * a.heads);
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (lane < a.splits) ml = a.ml[lane * rows + at];
     int b = 0;
     for (int n = a.n.seqs; n > 1;) {
         const int by = (n + 63) / 64;
@@ -25,24 +31,39 @@ __global__ __launch_bounds__(256) void attn8_join(AttnArgs a) {
         n = min(by, n - k * by);
     }
     if (a.n.starts[b] > t || t >= a.n.starts[b + 1]) return;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    if (lane < a.splits) ml = a.ml[lane * rows + at];
     float top = ml.x;
 #pragma unroll
     for (int x = 32; x > 0; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
     const float by = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top);
-    float l = 0.f;
+    float l = ml.y * by;
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) l += __shfl_xor(l, x);
+    constexpr int kGroups = 64 / LPR;
+    const int group = lane / LPR, d = 4 * (lane % LPR);
     floatx4 sum = {};
-    const int d = 4 * lane;
-    for (int s = 0; s < a.splits; ++s) {
-        const float ls = __shfl(ml.y, s), bs = __shfl(by, s);
-        if (ls == 0.f) continue;
-        l += ls * bs;
-        if (d < a.c.dim) sum += bs * *reinterpret_cast<const floatx4 *>(a.part + (s * rows + at) * a.c.dim + d);
+    for (int s0 = 0; s0 < a.splits; s0 += 4 * kGroups) {
+        floatx4 x[4];
+        float w[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int s = min(s0 + u * kGroups + group, 63);
+            w[u] = __shfl(by, s);
+            // a split without a key has left nothing but that
+            const bool is = s < a.splits && __shfl(ml.y, s) != 0.f && d < a.c.dim;
+            x[u] = floatx4{};
+            if (is) x[u] = *reinterpret_cast<const floatx4 *>(a.part + (s * rows + at) * a.c.dim + d);
+            w[u] = is ? w[u] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) sum += w[u] * x[u];
     }
+#pragma unroll
+    for (int x = LPR; x < 64; x *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += __shfl_xor(sum[e], x);
     const float inv = l == 0.f ? 0.f : 1.f / l;
     if (a.lse && lane == 0) a.lse[at] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
-    if (d >= a.c.dim) return;
+    if (group != 0 || d >= a.c.dim) return;
     T *op = static_cast<T *>(a.out) + t * a.ldo + hd * a.hldo + d;
 #pragma unroll
     for (int e = 0; e < 4; ++e) op[e] = T(sum[e] * inv);
@@ -51,11 +72,8 @@ __global__ __launch_bounds__(256) void attn8_join(AttnArgs a) {
 // ---- host ---------------------------------------------------------------------------
 
 struct AttnPlan {
-    int rows;                             // of a tile
-    bool few;
-    int nq;
-    int splits, span;
-    int64_t tiles, groups, bytes, part;   // part: bytes of the sums, a multiple of 16
+    int form, splits, span;
+    int64_t groups, bytes, part;          // part: bytes of the sums, a multiple of 16
 };
 
 int attn_check(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg) {
@@ -91,25 +109,24 @@ int most_keys(const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg 
     return int(cfg->max_len > 0 ? std::min(cfg->max_len, held) : held);
 }
 
-// Tiles and splits from what the host knows: tokens, sequences, heads and the most keys.
+// The form and the splits, from what the host knows: tokens, sequences, heads and the most keys.
 AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg) {
     AttnPlan p{};
     const int64_t group = q->heads / cache->heads, rows = q->tokens * group;
-    p.few = rows <= 64 * chunk->seqs;
-    p.nq = p.few ? 1 : attn8_blocks(q->type == DS_TYPE_F32, attn8_dim_blocks(cache->dim));
-    p.rows = p.few ? 32 : kWaves * 32 * p.nq;
-    p.tiles = rows / p.rows + chunk->seqs;
-    const int64_t base = p.tiles * cache->heads;
+    const int db = attn8_dim_blocks(cache->dim);
+    const bool own = q->type == DS_TYPE_F32 ? attn8_own_form<float>(db) : attn8_own_form<__bf16>(db);
+    p.form = rows <= 64 * chunk->seqs ? kAttnShare : own ? kAttnOwn : kAttnTiles;
+    const int tile = attn8_rows(p.form);
+    const int64_t base = (rows / tile + chunk->seqs) * cache->heads;
     int64_t keys = most_keys(cache, chunk, cfg);
-    if (cfg->window > 0) keys = std::min(keys, cfg->window + p.rows / group + 1 + kKeys);
-    const int64_t unit = p.few ? kWaves * kKeys : kKeys * 8;
-    const int64_t want = std::max<int64_t>(1, (p.few ? 1024 : 512) / std::max<int64_t>(1, base));
-    int64_t splits = std::min({want, (keys + unit - 1) / unit, int64_t(kMostSplits)});
-    splits = std::max<int64_t>(1, splits);
-    int64_t span = ((keys + splits - 1) / splits + unit - 1) / unit * unit;
-    p.span = int(std::max(span, unit));
+    if (cfg->window > 0) keys = std::min(keys, cfg->window + tile / group + 1 + 64);
+    const int64_t unit = p.form == kAttnShare ? 128 : 256;
+    const int64_t want = std::max<int64_t>(1, (p.form == kAttnTiles ? 256 : 1024) / std::max<int64_t>(1, base));
+    int64_t splits = std::max<int64_t>(1, std::min({want, (keys + unit - 1) / unit, int64_t(kMostSplits)}));
+    const int64_t span = std::max(unit, ((keys + splits - 1) / splits + unit - 1) / unit * unit);
+    p.span = int(std::min<int64_t>(span, kMaxPlaces));
     p.splits = int(std::max<int64_t>(1, (keys + p.span - 1) / p.span));
-    p.groups = p.tiles * cache->heads * p.splits;
+    p.groups = base * p.splits;
     if (p.splits > 1) {
         p.part = p.splits * q->tokens * q->heads * cache->dim * 4;
         p.bytes = p.part + p.splits * q->tokens * q->heads * 8;
@@ -118,16 +135,19 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
 }
 
 template <typename T>
-int run(const AttnPlan &p, const AttnArgs &a, hipStream_t stream) {
-    AttnArgs args = a;
-    void *argv[] = {&args};
-    if (!hip_ok(hipLaunchKernel(attn8_kernel<T>(a.c.fmt, a.c.dim, p.few), dim3(unsigned(p.groups)), dim3(64 * kWaves), argv, 0,
-                                stream),
-                "ds_attn8"))
+int run(const AttnPlan &p, AttnArgs a, hipStream_t stream) {
+    const AttnKernel k = attn8_kernel<T>(p.form, a.c.fmt, a.c.stype, a.c.dim);
+    if (k.lds) {
+        const int rc = ensure_lds_attr(k.func, k.lds);
+        if (rc != DS_OK) return rc;
+    }
+    void *argv[] = {&a};
+    if (!hip_ok(hipLaunchKernel(k.func, dim3(unsigned(p.groups)), dim3(attn8_threads(p.form)), argv, k.lds, stream), "ds_attn8"))
         return DS_EHIP;
     if (p.splits > 1) {
         const int64_t rows = int64_t(a.n.tokens) * a.heads;
-        attn8_join<T><<<unsigned((rows + kWaves - 1) / kWaves), 256, 0, stream>>>(a);
+        (a.c.dim <= 64 ? attn8_join<T, 16> : a.c.dim <= 128 ? attn8_join<T, 32> : attn8_join<T, 64>)
+            <<<unsigned((rows + kJoinWaves - 1) / kJoinWaves), 64 * kJoinWaves, 0, stream>>>(a);
         if (!hip_ok(hipGetLastError(), "ds_attn8")) return DS_EHIP;
     }
     return DS_OK;
@@ -173,8 +193,12 @@ int ds_attn8(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, c
                   (long long)work_bytes, work);
         return DS_EINVAL;
     }
-    if ((rc = launch_check(p.groups, 256, "ds_attn8")) != DS_OK ||
-        (rc = launch_check((q->tokens * q->heads + kWaves - 1) / kWaves, 256, "ds_attn8")) != DS_OK)
+    if (q->tokens * (q->heads / cache->heads) > 0x7ffffe00) {
+        set_error("%lld tokens of %lld heads a cache head", (long long)q->tokens, (long long)(q->heads / cache->heads));
+        return DS_EUNSUPPORTED;
+    }
+    if ((rc = launch_check(p.groups, attn8_threads(p.form), "ds_attn8")) != DS_OK ||
+        (rc = launch_check((q->tokens * q->heads + kJoinWaves - 1) / kJoinWaves, 256, "ds_attn8")) != DS_OK)
         return rc;
     AttnArgs a{};
     a.c = cache_view(cache);
@@ -196,6 +220,9 @@ int ds_attn8(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, c
     a.len = most_keys(cache, chunk, cfg);
     a.splits = p.splits;
     a.span = p.span;
+    a.f_group = make_fastdiv(a.group);
+    a.f_kv = make_fastdiv(cache->heads);
+    a.f_splits = make_fastdiv(a.splits);
     a.vec_q = heads16(q);
     a.vec_o = heads16(out);
     if (q->type == DS_TYPE_F32) return run<float>(p, a, stream);
