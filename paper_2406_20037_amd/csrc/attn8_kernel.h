@@ -110,6 +110,21 @@ __device__ __forceinline__ unsigned load_scale(const void *p, int stype, int64_t
     return stype == DS_SCALE_POW2 ? static_cast<const uint8_t *>(p)[at] : static_cast<const unsigned *>(p)[at];
 }
 
+// The kernel's argument once more, read again here: what a long loop does not use needs no scalar registers
+// through it.
+__device__ __forceinline__ AttnArgs late_args() {
+    typedef const __attribute__((address_space(4))) AttnArgs *Ptr;
+    uint64_t at = reinterpret_cast<uint64_t>(__builtin_amdgcn_kernarg_segment_ptr());
+    __asm__ volatile("" : "+s"(at));
+    AttnArgs a;
+    typedef const __attribute__((address_space(4))) int *Word;
+    const Word from = reinterpret_cast<Word>(at);
+    int *to = reinterpret_cast<int *>(&a);
+#pragma unroll
+    for (size_t i = 0; i < sizeof(AttnArgs) / 4; ++i) to[i] = from[i];
+    return a;
+}
+
 // Key of register r among 32: the order in which both products take keys.
 __device__ __forceinline__ int key_of(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
@@ -266,33 +281,65 @@ __device__ __forceinline__ void put_weight(bf16x8 (&to)[PP], int e, float w) {
     }
 }
 
-// The second product where V holds infinities or NaNs and some row does not see all keys: 0 times those
-// is no 0.  They are taken out of V, and a second product counts for each row and value how many
-// that it sees are +infinity (units of 1), -infinity (64) and NaN (4096): sums of up to 32, exact.
-template <int PP>
-__device__ __forceinline__ void add_poisoned(floatx16 &o, const bf16x8 (&v)[2], const bf16x8 (&p)[2][PP],
-                                             const bf16x8 (&seen)[2]) {
-    floatx16 count = {};
+// The rows' sums once more, key by key in plain fp32, [key, until): for tiles whose values hold infinities or NaNs
+// where some row does not see all keys, as 0 times those is no 0.  Slow, small and met by broken numbers only.
+template <typename T, int FMT, int DB>
+__device__ __forceinline__ void slow_sums(const AttnArgs &a, const Work &w, const Row &row,
+                                          const typename Parts<T>::Op (&q)[Parts<T>::QP][2 * DB], int h, int key, int until,
+                                          Sums<DB> &s) {
+    const auto bytes = [](const uint8_t *p, int n) {
+        unsigned x = 0;
+        for (int e = 0; e < n; ++e) x |= unsigned(p[e]) << (8 * e);
+        return x;
+    };
+    s.clear();
+#pragma unroll 1
+    for (; key < until; ++key) {
+        const Place at = key < w.len ? place_at(a.c, a.n, w.b, key) : Place{kNoPlace, 0};
+        if (at.page < 0) continue;
+        const int64_t rows = int64_t(w.head) * a.c.page + at.off, scales = at.page * a.c.sstride + rows;
+        const uint8_t *k = a.c.k + at.page * a.c.stride + rows * a.c.dim, *v = a.c.v + at.page * a.c.stride + rows * a.c.dim;
+        const float sk = scale_of(load_scale(a.c.ks, a.c.stype, scales), a.c.stype) * a.scale;
+        const float sv = scale_of(load_scale(a.c.vs, a.c.stype, scales), a.c.stype);
+        float x = 0.f;
 #pragma unroll
-    for (int st = 0; st < 2; ++st) {
-        bf16x8 fin, kind;
+        for (int c = 0; c < 2 * DB; ++c) {
+            const int d = 32 * (c >> 1) + 16 * h + 8 * (c & 1);
+            if (d >= a.c.dim) continue;
+            const bf16x8 kd = decode_k<FMT, bf16x8>(int(bytes(k + d, 4)), int(bytes(k + d + 4, 4)));
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float f = v[st][e];
-            const bool fine = fabsf(f) < INFINITY;
-            fin[e] = __bf16(fine ? f : 0.f);
-            kind[e] = __bf16(fine ? 0.f : f > 0.f ? 1.f : f < 0.f ? 64.f : 4096.f);
+            for (int p = 0; p < Parts<T>::QP; ++p) {
+                intx4 held = __builtin_bit_cast(intx4, q[p][c]);
+                __asm__ volatile("" : "+v"(held));         // (its fp32 values are no registers of the loop's)
+                const auto qd = __builtin_bit_cast(typename Parts<T>::Op, held);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x += float(kd[e]) * float(qd[e]);
+            }
         }
+        x = (x + other_half(x)) * sk;
+        if (key < row.low || key >= row.lim) continue;
+        if (x > s.m) {
+            const float by = __builtin_amdgcn_exp2f(s.m - x);
+            s.m = x;
+            s.l *= by;
 #pragma unroll
-        for (int part = PP - 1; part >= 0; --part) o = mma(fin, p[st][part], o);
-        count = mma(kind, seen[st], count);
-    }
+            for (int blk = 0; blk < DB; ++blk)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const float c = count[r];
-        const bool nan = c >= 4096.f, minus = c >= 64.f, plus = c - (minus ? 64.f * floorf(c / 64.f) : 0.f) > 0.f;
-        const float add = nan || (minus && plus) ? NAN : minus ? -INFINITY : INFINITY;
-        o[r] = c > 0.f ? o[r] + add : o[r];
+                for (int r = 0; r < 16; ++r) s.o[blk][r] *= by;
+        }
+        const float p = __builtin_amdgcn_exp2f(x - (s.m == -INFINITY ? 0.f : s.m));
+        s.l += h == 0 ? p : 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int d = DB * key_of(r, h);
+            if (d >= a.c.dim) continue;
+#pragma unroll
+            for (int blk = 0; blk < DB; blk += 2) {
+                const bf16x2 x2 = decode2<FMT, false>(bytes(v + d + blk, 2), 1.f);
+                s.o[blk][r] += p * (float(x2[0]) * sv);
+                s.o[blk + 1][r] += p * (float(x2[1]) * sv);
+            }
+        }
     }
 }
 
@@ -453,14 +500,13 @@ struct Direct {
         return r;
     }
 
-    // One tile; edge: some row does not see some key of it, or some key does not exist.  POISON: with
-    // add_poisoned; without it, false where that is needed.
-    template <bool POISON>
+    // One tile; edge: some row does not see some key of it, or some key does not exist.  False where that needs
+    // slow_sums.
     __device__ __forceinline__ bool step(Tile<DB> &t, int key0, bool edge, float *lds) {
         // the scales of all 32 keys to every lane that needs them; 0 of keys that do not exist
         const int valid[2] = {t.valid & 0xffff, t.valid >> 16};
         float sc = scale_of(t.s, a.c.stype);
-        if (POISON || edge) sc = (i & 15) < (i & 16 ? valid[1] : valid[0]) ? sc : 0.f;
+        if (edge) sc = (i & 15) < (i & 16 ? valid[1] : valid[0]) ? sc : 0.f;
         lds[lane] = h ? sc : sc * a.scale;
         __builtin_amdgcn_wave_barrier();
         floatx16 sum = {};
@@ -473,9 +519,11 @@ struct Direct {
                 for (int p = P::QP - 1; p >= 0; --p) sum = mma(k, q[p][2 * c + u], sum);
             }
         __builtin_amdgcn_sched_barrier(0);
-        bf16x8 pt[2][P::PP], seen[2];
-        if (POISON || edge) {
+        bf16x8 pt[2][P::PP];
+        if (edge) {
             unsigned bad = 0;
+            int has[2] = {valid[0] - 4 * h, valid[1] - 4 * h};
+            __asm__ volatile("" : "+v"(has[0]), "+v"(has[1]));
 #pragma unroll
             for (int st = 0; st < 2; ++st)
 #pragma unroll
@@ -483,10 +531,10 @@ struct Direct {
 #pragma unroll
                     for (int word = 0; word < Tile<DB>::W; ++word) {
                         unsigned &x = t.v[st][e][word];
-                        if (4 * h + (e < 4 ? e : e + 4) >= valid[st]) x = 0;
+                        if ((e < 4 ? e : e + 4) >= has[st]) x = 0;
                         bad |= not_finite<FMT>(x);
                     }
-            if (!POISON && __any(bad != 0)) return false;
+            if (__any(bad != 0)) return false;
         }
         float x[16];
 #pragma unroll
@@ -495,14 +543,17 @@ struct Direct {
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[4 * j + e] = sum[4 * j + e] * sk[e];
         }
-        if (POISON || edge)
+        if (edge) {
+            // (known here alone, so that this stays a branch: tiles that all rows see spend nothing on it)
+            int low = row.low - key0 - 4 * h, lim = row.lim - key0 - 4 * h, has[2] = {valid[0] - 4 * h, valid[1] - 4 * h};
+            __asm__ volatile("" : "+v"(low), "+v"(lim), "+v"(has[0]), "+v"(has[1]));
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int k = key_of(r, h);
-                const bool sees = key0 + k >= row.low && key0 + k < row.lim && (k & 15) < valid[r >> 3];
+                const int k = key_of(r, 0);
+                const bool sees = k >= low && k < lim && (k & 15) < has[r >> 3];
                 x[r] = sees ? x[r] : -INFINITY;
-                if constexpr (POISON) seen[r >> 3][r & 7] = __bf16(sees ? 1.f : 0.f);
             }
+        }
         float top = fmaxf(x[0], x[1]);
 #pragma unroll
         for (int r = 2; r < 16; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
@@ -522,24 +573,21 @@ struct Direct {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int blk = 0; blk < DB; ++blk) {
-            const bf16x8 v[2] = {decode_v(t, 0, blk), decode_v(t, 1, blk)};
-            if constexpr (POISON) {
-                add_poisoned<P::PP>(s.o[blk], v, pt, seen);
-            } else {
 #pragma unroll
-                for (int st = 0; st < 2; ++st)
+            for (int st = 0; st < 2; ++st) {
+                const bf16x8 v = decode_v(t, st, blk);
 #pragma unroll
-                    for (int part = P::PP - 1; part >= 0; --part) s.o[blk] = mma(v[st], pt[st][part], s.o[blk]);
+                for (int part = P::PP - 1; part >= 0; --part) s.o[blk] = mma(v, pt[st][part], s.o[blk]);
             }
         }
         return true;
     }
 
     // The keys from `key` on in steps of STEP, until `until`; every, since: keys that all rows of the wave see.
+    // False where a tile needs slow_sums.
     template <int STEP>
-    __device__ __forceinline__ void walk(int key, int until, int every, int since, float *lds) {
+    __device__ __forceinline__ bool walk(int key, int until, int every, int since, float *lds) {
         bool fine = true;
-        const int begin = key;
         const auto edge = [&](const Tile<DB> &t) {
             return key + kKeys > every || key < since || t.valid != (16 | 16 << 16);
         };
@@ -549,7 +597,7 @@ struct Direct {
             for (; key < until && fine; key += STEP) {
                 Tile<DB> t;
                 load(t, pages(key), key);
-                fine = step<false>(t, key, edge(t), lds);
+                fine = step(t, key, edge(t), lds);
             }
         } else if (key < until) {
             Tile<DB> t[2];
@@ -559,7 +607,7 @@ struct Direct {
                 const Pages after = pages(key + 2 * STEP);
                 if (key + STEP < until) load(then, next, key + STEP);
                 next = after;
-                fine = step<false>(now, key, edge(now), lds);
+                fine = step(now, key, edge(now), lds);
                 key += STEP;
             };
             while (true) {
@@ -569,17 +617,7 @@ struct Direct {
                 if (key >= until || !fine) break;
             }
         }
-        if (!fine) slow<STEP>(begin, until, lds);
-    }
-    template <int STEP>
-    __device__ __forceinline__ void slow(int key, int until, float *lds) {
-        s.clear();
-#pragma unroll 1
-        for (; key < until; key += STEP) {
-            Tile<DB> t;
-            load(t, pages(key), key);
-            step<true>(t, key, true, lds);
-        }
+        return fine;
     }
 };
 
@@ -603,9 +641,13 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a
     int from, until;
     w.keys(a, w.row0 + 31, from, until);
     Sums<DB> s;
-    Direct<T, FMT, DB>(a, w, row, q, s)
-        .template walk<4 * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
-                                  w.low(a, w.token(a, w.row0 + 31)), scales + wave * 64);
+    const bool fine = Direct<T, FMT, DB>(a, w, row, q, s)
+                          .template walk<4 * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
+                                                    w.low(a, w.token(a, w.row0 + 31)), scales + wave * 64);
+    if (__syncthreads_or(!fine)) {        // then the first wave takes all keys
+        s.clear();
+        if (wave == 0) slow_sums<T, FMT, DB>(late_args(), w, row, q, h, from, until, s);
+    }
     s.l += other_half(s.l);
     // four waves' sums of the same rows: two waves take another's each, then one
 #pragma unroll
@@ -636,7 +678,7 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a
                 for (int r = 0; r < 16; ++r) s.o[blk][r] = s.o[blk][r] * by + of[64 + (blk * 16 + r) * 64 + lane] * bo;
         }
     }
-    if (wave == 0) finish<T, DB>(a, w, row, s, h);
+    if (wave == 0) finish<T, DB>(late_args(), w, row, s, h);
 }
 
 // Each wave has rows of its own and reads keys by itself.
@@ -654,11 +696,13 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_own(AttnArgs a) 
     int from, until;
     w.keys(a, row0 + 31, from, until);
     Sums<DB> s;
-    Direct<T, FMT, DB>(a, w, row, q, s)
-        .template walk<kKeys>(max(from, w.low(a, w.token(a, row0)) & ~(kKeys - 1)), until, w.lim(a, w.token(a, row0)),
-                              w.low(a, w.token(a, row0 + 31)), scales + wave * 64);
+    from = max(from, w.low(a, w.token(a, row0)) & ~(kKeys - 1));
+    const bool fine = Direct<T, FMT, DB>(a, w, row, q, s)
+                          .template walk<kKeys>(from, until, w.lim(a, w.token(a, row0)), w.low(a, w.token(a, row0 + 31)),
+                                                scales + wave * 64);
+    if (!fine) slow_sums<T, FMT, DB>(late_args(), w, row, q, h, from, until, s);
     s.l += other_half(s.l);
-    finish<T, DB>(a, w, row, s, h);
+    finish<T, DB>(late_args(), w, row, s, h);
 }
 
 // ---- keys and values decoded in LDS ---------------------------------------------------------------------
@@ -770,9 +814,11 @@ struct Tiles {
                 for (int e = 0; e < 8; ++e) by[e] = scale_of((e < 4 ? st.sc0 : st.sc1) >> (8 * (e & 3)) & 0xff, DS_SCALE_POW2);
             }
             if (st.valid < 16) {
+                int has = st.valid - 4 * h;
+                __asm__ volatile("" : "+v"(has));
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (4 * h + (e < 4 ? e : e + 4) >= st.valid) {
+                    if ((e < 4 ? e : e + 4) >= has) {
                         by[e] = 1.f;
 #pragma unroll
                         for (int word = 0; word < W; ++word) st.raw[e * W + word] = 0;
@@ -808,58 +854,73 @@ struct Tiles {
         }
     }
 
-    // 32 of the tile's keys; c: what sums are multiplied with (powers of two in K's operands).
-    __device__ __forceinline__ void step(const TileLds<DB> &t, int sub, int key0, bool edge, const intx4 &note, float c,
-                                         const Row &row, const Op (&q)[P::QP][2 * DB], Sums<DB> &s) const {
-        floatx16 sum = {};
+    // K's operands of 32 keys.
+    __device__ __forceinline__ void read_k(const TileLds<DB> &t, int sub, Op (&k)[2 * DB]) const {
         const intx4 *kp = t.k + (32 * sub + i) * 4 * DB;
 #pragma unroll
-        for (int x = 0; x < 2 * DB; ++x) {
-            const Op k = __builtin_bit_cast(Op, kp[(4 * (x >> 1) + 2 * h + (x & 1)) ^ (i & 7)]);
+        for (int x = 0; x < 2 * DB; ++x) k[x] = __builtin_bit_cast(Op, kp[(4 * (x >> 1) + 2 * h + (x & 1)) ^ (i & 7)]);
+    }
+
+    // 32 of the tile's keys; c: what sums are multiplied with (powers of two in K's operands).  then: between the
+    // weights and their product, reads ahead.
+    template <typename Then>
+    __device__ __forceinline__ void step(const TileLds<DB> &t, int sub, int key0, bool edge, const intx4 &note, float c,
+                                         const Row &row, const Op (&q)[P::QP][2 * DB], const Op (&k)[2 * DB], Sums<DB> &s,
+                                         Then then) const {
+        floatx16 sum = {};
 #pragma unroll
-            for (int p = P::QP - 1; p >= 0; --p) sum = mma(k, q[p][x], sum);
-        }
+        for (int x = 0; x < 2 * DB; ++x)
+#pragma unroll
+            for (int p = P::QP - 1; p >= 0; --p) sum = mma(k[x], q[p][x], sum);
+        bf16x8 v[DB][2];
+#pragma unroll
+        for (int blk = 0; blk < DB; ++blk)
+#pragma unroll
+            for (int st = 0; st < 2; ++st)
+                v[blk][st] = __builtin_bit_cast(bf16x8, t.v[(blk * 32 + i) * 8 + ((4 * sub + 2 * st + h) ^ (i & 7))]);
+        floatx4 sk[4], sv[4];
+        if constexpr (!kFoldK)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sk[j] = *reinterpret_cast<const floatx4 *>(t.sk + 32 * sub + 8 * j + 4 * h);
+        __builtin_amdgcn_sched_barrier(0);
         float x[16];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            floatx4 sk;
-            if constexpr (!kFoldK) sk = *reinterpret_cast<const floatx4 *>(t.sk + 32 * sub + 8 * j + 4 * h);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * j + e] = kFoldK ? sum[4 * j + e] : sum[4 * j + e] * sk[e];
-        }
-        if (edge)
+        for (int r = 0; r < 16; ++r) x[r] = kFoldK ? sum[r] : sum[r] * sk[r >> 2][r & 3];
+        if (edge) {
+            // (known here alone, so that this stays a branch: tiles that all rows see spend nothing on it)
+            const int at = key0 + 32 * sub + 4 * h;
+            int low = row.low - at, lim = row.lim - at, has = (note[2 * sub] & 0xffff) - 4 * h, has1 = (note[2 * sub + 1] & 0xffff) - 4 * h;
+            __asm__ volatile("" : "+v"(low), "+v"(lim), "+v"(has), "+v"(has1));
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int k = 32 * sub + key_of(r, h);
-                const bool sees = key0 + k >= row.low && key0 + k < row.lim && (k & 15) < (note[2 * sub + (r >> 3)] & 0xffff);
+                const int k1 = key_of(r, 0);
+                const bool sees = k1 >= low && k1 < lim && (k1 & 15) < (r < 8 ? has : has1);
                 x[r] = sees ? x[r] : -INFINITY;
             }
+        }
         float top = fmaxf(x[0], x[1]);
 #pragma unroll
         for (int r = 2; r < 16; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
         top = fmaxf(top, other_half(top));
         const float off = s.follow(kFoldK ? top * c : top);
+        if constexpr (!kFoldV)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sv[j] = *reinterpret_cast<const floatx4 *>(t.sv + 32 * sub + 8 * j + 4 * h);
         bf16x8 pt[2][P::PP];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            floatx4 sv;
-            if constexpr (!kFoldV) sv = *reinterpret_cast<const floatx4 *>(t.sv + 32 * sub + 8 * j + 4 * h);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float y = x[4 * j + e];
-                const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(y, c, -off) : y - off);
-                s.l += p;
-                put_weight<P::PP>(pt[j >> 1], 4 * (j & 1) + e, kFoldV ? p : p * sv[e]);
-            }
+        for (int r = 0; r < 16; ++r) {
+            const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[r], c, -off) : x[r] - off);
+            s.l += p;
+            put_weight<P::PP>(pt[r >> 3], r & 7, kFoldV ? p : p * sv[r >> 2][r & 3]);
         }
+        then();
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int blk = 0; blk < DB; ++blk)
+        for (int st = 0; st < 2; ++st)
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                const bf16x8 v = __builtin_bit_cast(bf16x8, t.v[(blk * 32 + i) * 8 + ((4 * sub + 2 * st + h) ^ (i & 7))]);
+            for (int part = P::PP - 1; part >= 0; --part)
 #pragma unroll
-                for (int part = P::PP - 1; part >= 0; --part) s.o[blk] = mma(v, pt[st][part], s.o[blk]);
-            }
+                for (int blk = 0; blk < DB; ++blk) s.o[blk] = mma(v[blk][st], pt[st][part], s.o[blk]);
     }
 };
 
@@ -918,24 +979,24 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
                 break;
             }
             const bool whole = (note[0] & note[1] & note[2] & note[3] & 0xffff) == 16;
-#pragma unroll
-            for (int sub = 0; sub < 2; ++sub) {
-                const int k0 = key + 32 * sub;
-                if (k0 < last && k0 + 32 > first)
-                    tl.step(t, sub, key, k0 + 32 > every || k0 < since || !whole, note, c, row, q, s);
+            // (a wave that sees one half of the tile takes both: the other's weights are 0)
+            if (key < last && key + kTileKeys > first) {
+                const bool edge = key + kTileKeys > every || key < since || !whole;
+                typename Tl::Op k0[2 * DB], k1[2 * DB];
+                tl.read_k(t, 0, k0);
+                tl.step(t, 0, key, edge, note, c, row, q, k0, s, [&] {});
+                tl.read_k(t, 1, k1);
+                tl.step(t, 1, key, edge, note, c, row, q, k1, s, [] {});
             }
         }
     }
+    const AttnArgs al = late_args();
     if (!fine) {
-        // (the tile's buffers hold the waves' scales now)
-        __syncthreads();
-        if (Tl::kFoldK) load_q<T, DB>(a, row, h, 1.f, q);
-        Direct<T, FMT, DB>(a, w, row, q, s)
-            .template slow<kKeys>(max(from, first & ~(kKeys - 1)), min(until, last),
-                                  reinterpret_cast<float *>(lds_bytes) + wave * 64);
+        if (Tl::kFoldK) load_q<T, DB>(al, row, h, 1.f, q);
+        slow_sums<T, FMT, DB>(al, w, row, q, h, max(from, first), min(until, last), s);
     }
     s.l += other_half(s.l);
-    finish<T, DB>(a, w, row, s, h);
+    finish<T, DB>(al, w, row, s, h);
 }
 
 }  // namespace

@@ -48,8 +48,9 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attn8_join(AttnArgs a) {
         for (int u = 0; u < 4; ++u) {
             const int s = min(s0 + u * kGroups + group, 63);
             w[u] = __shfl(by, s);
+            const float ls = __shfl(ml.y, s);              // (of all lanes: none may stay away from a shuffle)
             // a split without a key has left nothing but that
-            const bool is = s < a.splits && __shfl(ml.y, s) != 0.f && d < a.c.dim;
+            const bool is = s < a.splits && ls != 0.f && d < a.c.dim;
             x[u] = floatx4{};
             if (is) x[u] = *reinterpret_cast<const floatx4 *>(a.part + (s * rows + at) * a.c.dim + d);
             w[u] = is ? w[u] : 0.f;
@@ -120,12 +121,22 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
     const int64_t base = (rows / tile + chunk->seqs) * cache->heads;
     int64_t keys = most_keys(cache, chunk, cfg);
     if (cfg->window > 0) keys = std::min(keys, cfg->window + tile / group + 1 + 64);
-    const int64_t unit = p.form == kAttnShare ? 128 : 256;
-    const int64_t want = std::max<int64_t>(1, (p.form == kAttnTiles ? 256 : 1024) / std::max<int64_t>(1, base));
-    int64_t splits = std::max<int64_t>(1, std::min({want, (keys + unit - 1) / unit, int64_t(kMostSplits)}));
-    const int64_t span = std::max(unit, ((keys + splits - 1) / splits + unit - 1) / unit * unit);
-    p.span = int(std::min<int64_t>(span, kMaxPlaces));
-    p.splits = int(std::max<int64_t>(1, (keys + p.span - 1) / p.span));
+    // The split that ends first: rounds of workgroups that the chip holds, each as long as its keys and what a
+    // workgroup needs beside them.
+    const int64_t unit = p.form == kAttnShare ? 128 : 64, slots = p.form == kAttnTiles ? 256 : 512, beside = 4 * unit;
+    const int64_t work = std::max<int64_t>(1, rows / tile + (rows % tile > 0)) * cache->heads;
+    int64_t best = INT64_MAX;
+    for (int64_t splits = 1; splits <= kMostSplits; ++splits) {
+        const int64_t span = std::max(unit, ((keys + splits - 1) / splits + unit - 1) / unit * unit);
+        const int64_t n = std::max<int64_t>(1, (keys + span - 1) / span);
+        const int64_t time = (work * n + slots - 1) / slots * (span + beside) + (n > 1 ? beside : 0);
+        if (time < best) {
+            best = time;
+            p.span = int(std::min<int64_t>(span, kMaxPlaces));
+            p.splits = int(n);
+        }
+        if (span == unit) break;
+    }
     p.groups = base * p.splits;
     if (p.splits > 1) {
         p.part = p.splits * q->tokens * q->heads * cache->dim * 4;
