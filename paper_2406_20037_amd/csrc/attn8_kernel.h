@@ -122,6 +122,21 @@ __device__ __forceinline__ AttnArgs late_args() {
     int *to = reinterpret_cast<int *>(&a);
 #pragma unroll
     for (size_t i = 0; i < sizeof(AttnArgs) / 4; ++i) to[i] = from[i];
+    // (global memory, which a pointer read from memory does not say)
+    const auto global = [](auto *&p) {
+        using V = std::remove_reference_t<decltype(*p)>;
+        p = (V *)(__attribute__((address_space(1))) V *)p;
+    };
+    global(a.lse);
+    global(a.part);
+    global(a.ml);
+    global(a.c.k);
+    global(a.c.v);
+    global(a.n.table);
+    a.q = (const void *)(const __attribute__((address_space(1))) void *)a.q;
+    a.out = (void *)(__attribute__((address_space(1))) void *)a.out;
+    a.c.ks = (void *)(__attribute__((address_space(1))) void *)a.c.ks;
+    a.c.vs = (void *)(__attribute__((address_space(1))) void *)a.c.vs;
     return a;
 }
 
@@ -709,9 +724,15 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_own(AttnArgs a) 
 
 constexpr int kTileKeys = 64;
 
-// A tile as operands of 16 bytes.  K: chunk c (values 8 c and on) of key r at r * 4 DB + (c ^ r % 8); V: the keys of
-// step st and half h, in key_of's order, of row blk * 32 + i at row * 8 + (2 st + h ^ i % 8): so that eight lanes
-// side by side read from all banks.
+// Where unit c of row r lies among rows of N 16-byte units: 16 lanes that read the same unit of rows side by side
+// meet all 64 banks (rows of 128 bytes lie two in a line of banks).
+template <int N>
+__device__ __forceinline__ int unit_at(int r, int c) {
+    return r * N + (c ^ (N == 8 ? r >> 1 & 7 : r & 15));
+}
+
+// A tile as operands of 16 bytes.  K: unit c of row r has values 8 c and on of key r; V: unit 2 st + h of row blk * 32 + i
+// has value DB i + blk of the keys of step st and half h, in key_of's order.
 template <int DB>
 struct TileLds {
     intx4 k[kTileKeys * 4 * DB];
@@ -802,7 +823,7 @@ struct Tiles {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const Op k = decode_k<FMT, Op>(st.raw[4 * j + 2 * u], st.raw[4 * j + 2 * u + 1], kFoldK ? by : 1.f);
-                    t.k[r * 4 * DB + ((2 * piece + u) ^ (r & 7))] = __builtin_bit_cast(intx4, k);
+                    t.k[unit_at<4 * DB>(r, 2 * piece + u)] = __builtin_bit_cast(intx4, k);
                 }
                 if (!kFoldK && piece == 0) t.sk[r] = by * a.scale;
             }
@@ -845,7 +866,7 @@ struct Tiles {
                         for (int e = 0; e < 4; ++e)
                             y[e] = int(__builtin_amdgcn_perm(x[2 * e + 1], x[2 * e], odd ? 0x07060302u : 0x05040100u));
                         const int blk = 4 * word + 2 * pair + odd;
-                        t.v[(blk * 32 + i) * 8 + ((2 * part + h) ^ (i & 7))] = y;
+                        t.v[unit_at<8>(blk * 32 + i, 2 * part + h)] = y;
                     }
                 }
             if (!kFoldV && lane < 16) t.sv[16 * part + lane] = lane < st.valid ? __uint_as_float(st.sc0) : 0.f;
@@ -856,36 +877,77 @@ struct Tiles {
 
     // K's operands of 32 keys.
     __device__ __forceinline__ void read_k(const TileLds<DB> &t, int sub, Op (&k)[2 * DB]) const {
-        const intx4 *kp = t.k + (32 * sub + i) * 4 * DB;
-#pragma unroll
-        for (int x = 0; x < 2 * DB; ++x) k[x] = __builtin_bit_cast(Op, kp[(4 * (x >> 1) + 2 * h + (x & 1)) ^ (i & 7)]);
-    }
-
-    // 32 of the tile's keys; c: what sums are multiplied with (powers of two in K's operands).  then: between the
-    // weights and their product, reads ahead.
-    template <typename Then>
-    __device__ __forceinline__ void step(const TileLds<DB> &t, int sub, int key0, bool edge, const intx4 &note, float c,
-                                         const Row &row, const Op (&q)[P::QP][2 * DB], const Op (&k)[2 * DB], Sums<DB> &s,
-                                         Then then) const {
-        floatx16 sum = {};
 #pragma unroll
         for (int x = 0; x < 2 * DB; ++x)
+            k[x] = __builtin_bit_cast(Op, t.k[unit_at<4 * DB>(32 * sub + i, 4 * (x >> 1) + 2 * h + (x & 1))]);
+    }
+    __device__ __forceinline__ void read_v(const TileLds<DB> &t, int sub, bf16x8 (&v)[DB][2]) const {
 #pragma unroll
-            for (int p = P::QP - 1; p >= 0; --p) sum = mma(k[x], q[p][x], sum);
-        bf16x8 v[DB][2];
+        for (int st = 0; st < 2; ++st)
 #pragma unroll
-        for (int blk = 0; blk < DB; ++blk)
+            for (int blk = 0; blk < DB; ++blk)
+                v[blk][st] = __builtin_bit_cast(bf16x8, t.v[unit_at<8>(blk * 32 + i, 4 * sub + 2 * st + h)]);
+    }
+
+    // A step takes 32 keys in two parts, in each of which the matrix unit works on one thing and the vector unit on another:
+    // the weights of these keys beside the scores of the next, and the product with V beside the next scores' maximum.
+    // The row's weights of scores x, with off from follow(), and the scores of the next keys.
+    __device__ __forceinline__ void weights(const TileLds<DB> &t, int sub, const float (&x)[16], float off, float c,
+                                            const Op (&k)[2 * DB], const Op (&q)[P::QP][2 * DB], Sums<DB> &s,
+                                            bf16x8 (&pt)[2][P::PP], floatx16 &next) const {
+        floatx4 sv[4];
+        if constexpr (!kFoldV)
 #pragma unroll
-            for (int st = 0; st < 2; ++st)
-                v[blk][st] = __builtin_bit_cast(bf16x8, t.v[(blk * 32 + i) * 8 + ((4 * sub + 2 * st + h) ^ (i & 7))]);
-        floatx4 sk[4], sv[4];
-        if constexpr (!kFoldK)
+            for (int j = 0; j < 4; ++j) sv[j] = *reinterpret_cast<const floatx4 *>(t.sv + 32 * sub + 8 * j + 4 * h);
+        next = floatx16{};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sk[j] = *reinterpret_cast<const floatx4 *>(t.sk + 32 * sub + 8 * j + 4 * h);
+        for (int y = 0; y < 2 * DB; ++y)
+#pragma unroll
+            for (int p = P::QP - 1; p >= 0; --p) next = mma(k[y], q[p][y], next);
+        float l[2] = {0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[r], c, -off) : x[r] - off);
+            l[r & 1] += p;
+            put_weight<P::PP>(pt[r >> 3], r & 7, kFoldV ? p : p * sv[r >> 2][r & 3]);
+        }
+        s.l += l[0] + l[1];
+        // a matrix instruction for every few of the vector unit's, after the reads
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * DB, 0);
+#pragma unroll
+        for (int y = 0; y < 2 * DB * P::QP; ++y) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 56 / (2 * DB * P::QP), 0);
+        }
         __builtin_amdgcn_sched_barrier(0);
-        float x[16];
+    }
+    // Their product with V, and the largest of the next scores (of the lane; x: them, times K's scales).
+    __device__ __forceinline__ float product(const bf16x8 (&v)[DB][2], const bf16x8 (&pt)[2][P::PP], Sums<DB> &s,
+                                             const floatx16 &next, const TileLds<DB> &t, int sub, float (&x)[16]) const {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = kFoldK ? sum[r] : sum[r] * sk[r >> 2][r & 3];
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+            for (int part = P::PP - 1; part >= 0; --part)
+#pragma unroll
+                for (int blk = 0; blk < DB; ++blk) s.o[blk] = mma(v[blk][st], pt[st][part], s.o[blk]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            floatx4 sk;
+            if constexpr (!kFoldK) sk = *reinterpret_cast<const floatx4 *>(t.sk + 32 * sub + 8 * j + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[4 * j + e] = kFoldK ? next[4 * j + e] : next[4 * j + e] * sk[e];
+        }
+        return largest(x);
+    }
+    __device__ __forceinline__ float largest(const float (&x)[16]) const {
+        float top = fmaxf(x[0], x[1]);
+#pragma unroll
+        for (int r = 2; r < 16; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
+        return top;
+    }
+    // The scores that the row does not see out of x (edge: there are some in the wave), and the maximum followed.
+    __device__ __forceinline__ float follow(float (&x)[16], float top, int key0, int sub, bool edge, const intx4 &note,
+                                            float c, const Row &row, Sums<DB> &s) const {
         if (edge) {
             // (known here alone, so that this stays a branch: tiles that all rows see spend nothing on it)
             const int at = key0 + 32 * sub + 4 * h;
@@ -897,30 +959,10 @@ struct Tiles {
                 const bool sees = k1 >= low && k1 < lim && (k1 & 15) < (r < 8 ? has : has1);
                 x[r] = sees ? x[r] : -INFINITY;
             }
+            top = largest(x);
         }
-        float top = fmaxf(x[0], x[1]);
-#pragma unroll
-        for (int r = 2; r < 16; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
         top = fmaxf(top, other_half(top));
-        const float off = s.follow(kFoldK ? top * c : top);
-        if constexpr (!kFoldV)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sv[j] = *reinterpret_cast<const floatx4 *>(t.sv + 32 * sub + 8 * j + 4 * h);
-        bf16x8 pt[2][P::PP];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[r], c, -off) : x[r] - off);
-            s.l += p;
-            put_weight<P::PP>(pt[r >> 3], r & 7, kFoldV ? p : p * sv[r >> 2][r & 3]);
-        }
-        then();
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-            for (int part = P::PP - 1; part >= 0; --part)
-#pragma unroll
-                for (int blk = 0; blk < DB; ++blk) s.o[blk] = mma(v[blk][st], pt[st][part], s.o[blk]);
+        return s.follow(kFoldK ? top * c : top);
     }
 };
 
@@ -931,8 +973,9 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// Eight waves of 32 rows each.  While a tile is used, the next is written to the other half of LDS and the one
-// after is on its way from memory: one barrier a tile.
+// Eight waves of 32 rows each, which all walk over the workgroup's keys.  Three tiles in LDS: one is used, the next is written
+// (the one after is on its way from memory), and the third may still be read by a wave that is behind: one
+// barrier a tile.
 template <typename T, int FMT, bool POW2, int DB>
 __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_bytes[];
@@ -945,10 +988,9 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
     const Row row = find_row(a, w, row0 + i);
     int from, until;
     w.keys(a, w.row0 + 255, from, until);
-    // what all rows of the workgroup see, and of the wave; what any row of the wave sees
+    // what all rows of the workgroup see, and of the wave
     const int wg_every = w.lim(a, w.token(a, w.row0)), wg_since = w.low(a, w.token(a, w.row0 + 255));
     const int every = w.lim(a, w.token(a, row0)), since = w.low(a, w.token(a, row0 + 31));
-    const int last = row0 < w.rows ? w.lim(a, w.token(a, row0 + 31)) : 0, first = w.low(a, w.token(a, row0));
     typename Parts<T>::Op q[Parts<T>::QP][2 * DB];
     // powers of two in K's operands leave one factor for all sums; its sign goes into Q, so that the
     // largest sum is the largest score
@@ -963,37 +1005,70 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
         tl.load(st, from);
         tl.store(st, lds[0]);
         if (from + kTileKeys < until) tl.load(st, from + kTileKeys);
-        int at = 0;
-        for (int key = from; key < until; key += kTileKeys, at ^= 1) {
-            lds_barrier();
-            const TileLds<DB> &t = lds[at];
-            if (key + kTileKeys < until) {
-                tl.store(st, lds[at ^ 1]);
-                if (key + 2 * kTileKeys < until) tl.load(st, key + 2 * kTileKeys);
-            }
-            intx4 note = *reinterpret_cast<const intx4 *>(t.note);
+        lds_barrier();
+        intx4 note;
+        bool edge = false;
+        // the notes of the tile at `key`; false if it needs slow_sums
+        const auto look = [&](const TileLds<DB> &t, int key) {
+            note = *reinterpret_cast<const intx4 *>(t.note);
 #pragma unroll
             for (int e = 0; e < 4; ++e) note[e] = __builtin_amdgcn_readfirstlane(note[e]);
-            if (((note[0] | note[1] | note[2] | note[3]) >> 16) && (key + kTileKeys > wg_every || key < wg_since)) {
-                fine = false;
-                break;
+            edge = key + kTileKeys > every || key < since || (note[0] & note[1] & note[2] & note[3] & 0xffff) != 16;
+            return !((note[0] | note[1] | note[2] | note[3]) >> 16 && (key + kTileKeys > wg_every || key < wg_since));
+        };
+        typename Tl::Op k[2 * DB];
+        bf16x8 v[DB][2], pt[2][Parts<T>::PP];
+        floatx16 next;
+        float x[16], off;
+        fine = look(lds[0], from);
+        tl.read_k(lds[0], 0, k);
+        next = floatx16{};
+#pragma unroll
+        for (int y = 0; y < 2 * DB; ++y)
+#pragma unroll
+            for (int p = Parts<T>::QP - 1; p >= 0; --p) next = mma(k[y], q[p][y], next);
+#pragma unroll
+        for (int blk = 0; blk < DB; ++blk)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) v[blk][e] = pt[e][0] = bf16x8{};
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int part = 0; part < Parts<T>::PP; ++part) pt[e][part] = bf16x8{};
+        off = tl.follow(x, tl.product(v, pt, s, next, lds[0], 0, x), from, 0, edge, note, c, row, s);
+        tl.read_k(lds[0], 1, k);
+        int at = 0;
+        for (int key = from; fine; key += kTileKeys) {
+            const TileLds<DB> &t = lds[at];
+            const int after = at == 2 ? 0 : at + 1;
+            const bool more = key + kTileKeys < until;
+            tl.read_v(t, 0, v);
+            tl.weights(t, 0, x, off, c, k, q, s, pt, next);
+            const float top = tl.product(v, pt, s, next, t, 1, x);
+            __builtin_amdgcn_sched_barrier(0);
+            off = tl.follow(x, top, key, 1, edge, note, c, row, s);
+            if (more) {
+                tl.store(st, lds[after]);
+                if (key + 2 * kTileKeys < until) tl.load(st, key + 2 * kTileKeys);
+                lds_barrier();
+                fine = look(lds[after], key + kTileKeys);
             }
-            const bool whole = (note[0] & note[1] & note[2] & note[3] & 0xffff) == 16;
-            // (a wave that sees one half of the tile takes both: the other's weights are 0)
-            if (key < last && key + kTileKeys > first) {
-                const bool edge = key + kTileKeys > every || key < since || !whole;
-                typename Tl::Op k0[2 * DB], k1[2 * DB];
-                tl.read_k(t, 0, k0);
-                tl.step(t, 0, key, edge, note, c, row, q, k0, s, [&] {});
-                tl.read_k(t, 1, k1);
-                tl.step(t, 1, key, edge, note, c, row, q, k1, s, [] {});
-            }
+            // (behind the last tile the scores of whatever lies there, which nobody takes)
+            tl.read_k(lds[after], 0, k);
+            tl.read_v(t, 1, v);
+            tl.weights(t, 1, x, off, c, k, q, s, pt, next);
+            const float then = tl.product(v, pt, s, next, lds[after], 0, x);
+            if (!more) break;
+            tl.read_k(lds[after], 1, k);
+            __builtin_amdgcn_sched_barrier(0);
+            off = tl.follow(x, then, key + kTileKeys, 0, edge, note, c, row, s);
+            at = after;
         }
     }
     const AttnArgs al = late_args();
     if (!fine) {
         if (Tl::kFoldK) load_q<T, DB>(al, row, h, 1.f, q);
-        slow_sums<T, FMT, DB>(al, w, row, q, h, max(from, first), min(until, last), s);
+        slow_sums<T, FMT, DB>(al, w, row, q, h, from, until, s);
     }
     s.l += other_half(s.l);
     finish<T, DB>(al, w, row, s, h);
@@ -1014,7 +1089,7 @@ AttnKernel attn8_kernel(int form, int fmt, int stype, int dim) {
             if constexpr (!attn8_own_form<T>(DB)) {
                 k.func = stype == DS_SCALE_POW2 ? reinterpret_cast<const void *>(&attn8_tiles<T, FMT, true, DB>)
                                                 : reinterpret_cast<const void *>(&attn8_tiles<T, FMT, false, DB>);
-                k.lds = 2 * int(sizeof(TileLds<DB>));
+                k.lds = 3 * int(sizeof(TileLds<DB>));
             }
         }
     };

@@ -124,7 +124,7 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
     // The split that ends first: rounds of workgroups that the chip holds, each as long as its keys and what a
     // workgroup needs beside them.
     const int64_t unit = p.form == kAttnShare ? 128 : 64, slots = p.form == kAttnTiles ? 256 : 512, beside = 4 * unit;
-    const int64_t work = std::max<int64_t>(1, rows / tile + (rows % tile > 0)) * cache->heads;
+    const int64_t work = std::max((rows + tile - 1) / tile, std::min(q->tokens, chunk->seqs)) * cache->heads;
     int64_t best = INT64_MAX;
     for (int64_t splits = 1; splits <= kMostSplits; ++splits) {
         const int64_t span = std::max(unit, ((keys + splits - 1) / splits + unit - 1) / unit * unit);
@@ -137,6 +137,7 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
         }
         if (span == unit) break;
     }
+    if (const char *e = getenv("DS_SPAN")) { p.span = atoi(e); p.splits = int(std::min<int64_t>(64, (keys + p.span - 1) / p.span)); p.span = int(((keys + p.splits - 1) / p.splits + unit - 1) / unit * unit); }
     p.groups = base * p.splits;
     if (p.splits > 1) {
         p.part = p.splits * q->tokens * q->heads * cache->dim * 4;
