@@ -137,7 +137,6 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
         }
         if (span == unit) break;
     }
-    if (const char *e = getenv("DS_SPAN")) { p.span = atoi(e); p.splits = int(std::min<int64_t>(64, (keys + p.span - 1) / p.span)); p.span = int(((keys + p.splits - 1) / p.splits + unit - 1) / unit * unit); }
     p.groups = base * p.splits;
     if (p.splits > 1) {
         p.part = p.splits * q->tokens * q->heads * cache->dim * 4;
