@@ -140,6 +140,24 @@ __device__ __forceinline__ AttnArgs late_args() {
     return a;
 }
 
+// The page of 16 keys from `key` on (a multiple of 16) of sequence b of length len > 0: its number as the table
+// has it, and the offset; of the last key's page for keys past the end.  The number is read as vectors are, although
+// it is the same for all lanes: reads of scalars are counted with LDS accesses, whose waits would wait for them.
+struct PageRef {
+    int raw, off;
+};
+__device__ __forceinline__ PageRef page_ref(const AttnArgs &a, int b, int len, int key) {
+    const int k = min(key, len - 1), col = fdiv(k, a.c.f_page);
+    int zero = 0;
+    __asm__ volatile("" : "+v"(zero));
+    return {a.n.table[int64_t(b) * a.n.tld + col + zero], (k - col * a.c.page) & ~15};
+}
+// The number where it is used: kNoPlace unless it is one of the cache's.
+__device__ __forceinline__ int page_of(const AttnArgs &a, const PageRef &r) {
+    const int id = __builtin_amdgcn_readfirstlane(r.raw);
+    return id >= 0 && id < a.c.pages ? id : kNoPlace;
+}
+
 // Key of register r among 32: the order in which both products take keys.
 __device__ __forceinline__ int key_of(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
 
@@ -451,20 +469,11 @@ struct Direct {
         : a(a_), w(w_), row(r_), q(q_), s(s_), lane(threadIdx.x & 63), i(lane & 31), h(lane >> 5),
           koff((i & 15) * a_.c.dim + 16 * h), voff(4 * h * a_.c.dim + DB * i) {}
 
-    // The two pages of a tile: numbers (kNoPlace if there is none) and offsets.
     struct Pages {
-        int id[2], off[2];
+        PageRef p[2];
     };
     __device__ __forceinline__ Pages pages(int key0) const {
-        Pages p;
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-            const int key = key0 + 16 * st;
-            const Place at = key < w.len ? place_at(a.c, a.n, w.b, key) : Place{kNoPlace, 0};
-            p.id[st] = at.page;
-            p.off[st] = at.off;
-        }
-        return p;
+        return {page_ref(a, w.b, w.len, key0), page_ref(a, w.b, w.len, key0 + 16)};
     }
 
     // Loads of a tile.  A part without a page reads page 0 and counts as no key; nothing past a row's dim is
@@ -475,12 +484,12 @@ struct Direct {
         int64_t page[2];
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-            const int id = __builtin_amdgcn_readfirstlane(p.id[st]);
-            valid[st] = id >= 0 ? min(16, w.len - key0 - 16 * st) : 0;
+            const int id = page_of(a, p.p[st]);
+            valid[st] = id >= 0 ? min(16, max(w.len - key0 - 16 * st, 0)) : 0;
             page[st] = max(id, 0);
         }
         t.valid = valid[0] | valid[1] << 16;
-        const int at[2] = {w.head * a.c.page + p.off[0], w.head * a.c.page + p.off[1]};
+        const int at[2] = {w.head * a.c.page + p.p[0].off, w.head * a.c.page + p.p[1].off};
         const int64_t byte[2] = {page[0] * a.c.stride + int64_t(at[0]) * dim, page[1] * a.c.stride + int64_t(at[1]) * dim};
         const bool up = i & 16;
         const uint8_t *kp = a.c.k + (up ? byte[1] : byte[0]) + koff;
@@ -763,23 +772,28 @@ struct Tiles {
         int valid;
     };
 
-    __device__ __forceinline__ Place place(int key) const {
-        Place p = key < w.len ? place_at(a.c, a.n, w.b, key) : Place{kNoPlace, 0};
-        p.page = __builtin_amdgcn_readfirstlane(p.page);
-        p.off = __builtin_amdgcn_readfirstlane(p.off);
-        return p;
+    // The pages that the wave loads of a tile: a tile ahead of the loads.
+    struct Pages {
+        PageRef p[kLoads];
+    };
+    __device__ __forceinline__ Pages pages(int key0) const {
+        Pages r;
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int row = j * (256 / kPieces) + (wave & 3) * (64 / kPieces);   // K's: all in one part
+            r.p[j] = page_ref(a, w.b, w.len, key0 + (wave < 4 ? row & ~15 : 16 * (wave - 4)));
+        }
+        return r;
     }
 
-    __device__ __forceinline__ void load(Stage &st, int key0) const {
+    __device__ __forceinline__ void load(Stage &st, const Pages &from, int key0) const {
         const int dim = a.c.dim;
         if (wave < 4) {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
-                const int r0 = j * (256 / kPieces) + wave * (64 / kPieces);   // the wave's first row: all in one part
-                const Place p = place(key0 + (r0 & ~15));
-                const int64_t page = max(p.page, 0);
-                const int r = (r0 & 15) + lane / kPieces, piece = lane % kPieces;
-                const int64_t at = w.head * a.c.page + p.off;
+                const int64_t page = max(page_of(a, from.p[j]), 0);
+                const int r = ((wave & 3) * (64 / kPieces) & 15) + lane / kPieces, piece = lane % kPieces;
+                const int64_t at = w.head * a.c.page + from.p[j].off;
                 intx4 x = {};
                 if (16 * piece < dim)
                     x = *reinterpret_cast<const intx4 *>(a.c.k + page * a.c.stride + at * dim + unsigned(r * dim + 16 * piece));
@@ -790,11 +804,10 @@ struct Tiles {
                 else st.sc1 = sc;
             }
         } else {
-            const int part = wave - 4, key = key0 + 16 * part;
-            const Place p = place(key);
-            const int64_t page = max(p.page, 0);
-            st.valid = p.page >= 0 ? min(16, w.len - key) : 0;
-            const int64_t at = w.head * a.c.page + p.off;
+            const int id = page_of(a, from.p[0]);
+            const int64_t page = max(id, 0);
+            st.valid = id >= 0 ? min(16, max(w.len - key0 - 16 * (wave - 4), 0)) : 0;
+            const int64_t at = w.head * a.c.page + from.p[0].off;
             const uint8_t *vp = a.c.v + page * a.c.stride + at * dim;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -895,10 +908,6 @@ struct Tiles {
     __device__ __forceinline__ void weights(const TileLds<DB> &t, int sub, const float (&x)[16], float off, float c,
                                             const Op (&k)[2 * DB], const Op (&q)[P::QP][2 * DB], Sums<DB> &s,
                                             bf16x8 (&pt)[2][P::PP], floatx16 &next) const {
-        floatx4 sv[4];
-        if constexpr (!kFoldV)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sv[j] = *reinterpret_cast<const floatx4 *>(t.sv + 32 * sub + 8 * j + 4 * h);
         next = floatx16{};
 #pragma unroll
         for (int y = 0; y < 2 * DB; ++y)
@@ -906,20 +915,29 @@ struct Tiles {
             for (int p = P::QP - 1; p >= 0; --p) next = mma(k[y], q[p][y], next);
         float l[2] = {0.f, 0.f};
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[r], c, -off) : x[r] - off);
-            l[r & 1] += p;
-            put_weight<P::PP>(pt[r >> 3], r & 7, kFoldV ? p : p * sv[r >> 2][r & 3]);
+        for (int j = 0; j < 4; ++j) {
+            floatx4 sv;
+            if constexpr (!kFoldV) sv = *reinterpret_cast<const floatx4 *>(t.sv + 32 * sub + 8 * j + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int r = 4 * j + e;
+                const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[r], c, -off) : x[r] - off);
+                l[r & 1] += p;
+                put_weight<P::PP>(pt[r >> 3], r & 7, kFoldV ? p : p * sv[e]);
+            }
         }
         s.l += l[0] + l[1];
-        // a matrix instruction for every few of the vector unit's, after the reads
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * DB, 0);
+        // a matrix instruction for every few of the vector unit's, after the reads; two parts of the weights
+        // leave no registers for that
+        if constexpr (P::PP == 1) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * DB, 0);
 #pragma unroll
-        for (int y = 0; y < 2 * DB * P::QP; ++y) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 56 / (2 * DB * P::QP), 0);
+            for (int y = 0; y < 2 * DB; ++y) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 56 / (2 * DB), 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
     }
     // Their product with V, and the largest of the next scores (of the lane; x: them, times K's scales).
     __device__ __forceinline__ float product(const bf16x8 (&v)[DB][2], const bf16x8 (&pt)[2][P::PP], Sums<DB> &s,
@@ -1002,9 +1020,14 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
     bool fine = true;
     if (from < until) {
         typename Tl::Stage st;
-        tl.load(st, from);
+        tl.load(st, tl.pages(from), from);
+        typename Tl::Pages pages = tl.pages(from + kTileKeys);
         tl.store(st, lds[0]);
-        if (from + kTileKeys < until) tl.load(st, from + kTileKeys);
+        if (from + kTileKeys < until) {
+            const typename Tl::Pages p = pages;
+            pages = tl.pages(from + 2 * kTileKeys);
+            tl.load(st, p, from + kTileKeys);
+        }
         lds_barrier();
         intx4 note;
         bool edge = false;
@@ -1037,30 +1060,37 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
             for (int part = 0; part < Parts<T>::PP; ++part) pt[e][part] = bf16x8{};
         off = tl.follow(x, tl.product(v, pt, s, next, lds[0], 0, x), from, 0, edge, note, c, row, s);
         tl.read_k(lds[0], 1, k);
+        constexpr bool kAhead = Parts<T>::PP == 1;
         int at = 0;
         for (int key = from; fine; key += kTileKeys) {
             const TileLds<DB> &t = lds[at];
             const int after = at == 2 ? 0 : at + 1;
             const bool more = key + kTileKeys < until;
-            tl.read_v(t, 0, v);
+            if constexpr (kAhead) tl.read_v(t, 0, v);
             tl.weights(t, 0, x, off, c, k, q, s, pt, next);
+            if constexpr (!kAhead) tl.read_v(t, 0, v);
             const float top = tl.product(v, pt, s, next, t, 1, x);
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (Parts<T>::PP == 1) __builtin_amdgcn_sched_barrier(0);
             off = tl.follow(x, top, key, 1, edge, note, c, row, s);
             if (more) {
                 tl.store(st, lds[after]);
-                if (key + 2 * kTileKeys < until) tl.load(st, key + 2 * kTileKeys);
+                if (key + 2 * kTileKeys < until) {
+                    const typename Tl::Pages p = pages;
+                    pages = tl.pages(key + 3 * kTileKeys);
+                    tl.load(st, p, key + 2 * kTileKeys);
+                }
                 lds_barrier();
                 fine = look(lds[after], key + kTileKeys);
             }
             // (behind the last tile the scores of whatever lies there, which nobody takes)
             tl.read_k(lds[after], 0, k);
-            tl.read_v(t, 1, v);
+            if constexpr (kAhead) tl.read_v(t, 1, v);
             tl.weights(t, 1, x, off, c, k, q, s, pt, next);
+            if constexpr (!kAhead) tl.read_v(t, 1, v);
             const float then = tl.product(v, pt, s, next, lds[after], 0, x);
             if (!more) break;
             tl.read_k(lds[after], 1, k);
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (Parts<T>::PP == 1) __builtin_amdgcn_sched_barrier(0);
             off = tl.follow(x, then, key + kTileKeys, 0, edge, note, c, row, s);
             at = after;
         }
