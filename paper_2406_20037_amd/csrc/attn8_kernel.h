@@ -436,16 +436,20 @@ struct Tile {
     int valid;                            // keys of each 16 that exist: low and high half word
 };
 
-// The lane's DB bytes of a row of V, 0 past its end.
+// Where the lane's DB bytes of a row of V begin; lanes past a row's end take its last ones, for sums that nobody
+// stores.
 template <int DB>
-__device__ __forceinline__ void load_v(const uint8_t *p, unsigned at, bool is, unsigned (&w)[DB == 8 ? 2 : 1]) {
+__device__ __forceinline__ int v_column(int i, int dim) {
+    return min(DB * i, dim - DB);
+}
+template <int DB>
+__device__ __forceinline__ void load_v(const uint8_t *p, unsigned at, unsigned (&w)[DB == 8 ? 2 : 1]) {
     if constexpr (DB == 2) {
-        w[0] = is ? *reinterpret_cast<const uint16_t *>(p + at) : 0;
+        w[0] = *reinterpret_cast<const uint16_t *>(p + at);
     } else if constexpr (DB == 4) {
-        w[0] = is ? *reinterpret_cast<const unsigned *>(p + at) : 0;
+        w[0] = *reinterpret_cast<const unsigned *>(p + at);
     } else {
-        intx2 x = {};
-        if (is) x = *reinterpret_cast<const intx2 *>(p + at);
+        const intx2 x = *reinterpret_cast<const intx2 *>(p + at);
         w[0] = x[0];
         w[1] = x[1];
     }
@@ -467,7 +471,7 @@ struct Direct {
     __device__ __forceinline__ Direct(const AttnArgs &a_, const Work &w_, const Row &r_, const Op (&q_)[P::QP][2 * DB],
                                       Sums<DB> &s_)
         : a(a_), w(w_), row(r_), q(q_), s(s_), lane(threadIdx.x & 63), i(lane & 31), h(lane >> 5),
-          koff((i & 15) * a_.c.dim + 16 * h), voff(4 * h * a_.c.dim + DB * i) {}
+          koff((i & 15) * a_.c.dim), voff(4 * h * a_.c.dim + v_column<DB>(i, a_.c.dim)) {}
 
     struct Pages {
         PageRef p[2];
@@ -476,8 +480,8 @@ struct Direct {
         return {page_ref(a, w.b, w.len, key0), page_ref(a, w.b, w.len, key0 + 16)};
     }
 
-    // Loads of a tile.  A part without a page reads page 0 and counts as no key; nothing past a row's dim is
-    // read, and the rows of a part past the sequence's end are the page's own.
+    // Loads of a tile.  A part without a page reads page 0 and counts as no key; past a row's dim its last
+    // bytes are read again, and the rows of a part past the sequence's end are the page's own.
     __device__ __forceinline__ void load(Tile<DB> &t, const Pages &p, int key0) const {
         const int dim = a.c.dim;
         int valid[2];
@@ -494,15 +498,12 @@ struct Direct {
         const bool up = i & 16;
         const uint8_t *kp = a.c.k + (up ? byte[1] : byte[0]) + koff;
 #pragma unroll
-        for (int c = 0; c < DB; ++c) {
-            t.k[c] = intx4{};
-            if (32 * c + 16 * h < dim) t.k[c] = *reinterpret_cast<const intx4 *>(kp + 32 * c);
-        }
+        for (int c = 0; c < DB; ++c) t.k[c] = *reinterpret_cast<const intx4 *>(kp + min(32 * c + 16 * h, dim - 16));
 #pragma unroll
         for (int st = 0; st < 2; ++st)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                load_v<DB>(a.c.v + byte[st] + (e < 4 ? e : e + 4) * dim, voff, DB * i < dim, t.v[st][e]);
+                load_v<DB>(a.c.v + byte[st] + (e < 4 ? e : e + 4) * dim, voff, t.v[st][e]);
         const int64_t se = (up ? page[1] : page[0]) * a.c.sstride + (up ? at[1] : at[0]) + (i & 15);
         t.s = load_scale(h ? a.c.vs : a.c.ks, a.c.stype, se);
     }
@@ -533,6 +534,10 @@ struct Direct {
         if (edge) sc = (i & 15) < (i & 16 ? valid[1] : valid[0]) ? sc : 0.f;
         lds[lane] = h ? sc : sc * a.scale;
         __builtin_amdgcn_wave_barrier();
+        if (a.c.dim < 32 * DB)                // (a number that is none times Q's 0 is no 0)
+#pragma unroll
+            for (int c = 0; c < DB; ++c)
+                if (32 * c + 16 * h >= a.c.dim) t.k[c] = intx4{};
         floatx16 sum = {};
 #pragma unroll
         for (int c = 0; c < DB; ++c)
@@ -794,9 +799,8 @@ struct Tiles {
                 const int64_t page = max(page_of(a, from.p[j]), 0);
                 const int r = ((wave & 3) * (64 / kPieces) & 15) + lane / kPieces, piece = lane % kPieces;
                 const int64_t at = w.head * a.c.page + from.p[j].off;
-                intx4 x = {};
-                if (16 * piece < dim)
-                    x = *reinterpret_cast<const intx4 *>(a.c.k + page * a.c.stride + at * dim + unsigned(r * dim + 16 * piece));
+                const intx4 x = *reinterpret_cast<const intx4 *>(a.c.k + page * a.c.stride + at * dim +
+                                                                 unsigned(r * dim + min(16 * piece, dim - 16)));
 #pragma unroll
                 for (int e = 0; e < 4; ++e) st.raw[4 * j + e] = x[e];
                 const unsigned sc = load_scale(a.c.ks, POW2 ? DS_SCALE_POW2 : DS_SCALE_F32, page * a.c.sstride + at + r);
@@ -812,7 +816,7 @@ struct Tiles {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 unsigned x[W];
-                load_v<DB>(vp + (e < 4 ? e : e + 4) * dim, unsigned(4 * h * dim + DB * i), DB * i < dim, x);
+                load_v<DB>(vp + (e < 4 ? e : e + 4) * dim, unsigned(4 * h * dim + v_column<DB>(i, dim)), x);
 #pragma unroll
                 for (int word = 0; word < W; ++word) st.raw[e * W + word] = x[word];
             }
@@ -832,6 +836,9 @@ struct Tiles {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
                 const int r = j * (256 / kPieces) + wave * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
+                if (a.c.dim < 32 * DB && 16 * piece >= a.c.dim)      // (a number that is none times Q's 0 is no 0)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) st.raw[4 * j + e] = 0;
                 const float by = scale_of(j == 0 ? st.sc0 : st.sc1, POW2 ? DS_SCALE_POW2 : DS_SCALE_F32);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
