@@ -140,17 +140,17 @@ __device__ __forceinline__ AttnArgs late_args() {
     return a;
 }
 
-// The page of 16 keys from `key` on (a multiple of 16) of sequence b of length len > 0: its number as the table
-// has it, and the offset; of the last key's page for keys past the end.  The number is read as vectors are, although
+// The page of 16 keys from `key` on (a multiple of 16) of a sequence of length len > 0: its number as its row of the
+// table has it, and the offset; of the last key's page for keys past the end.  The number is read as vectors are, although
 // it is the same for all lanes: reads of scalars are counted with LDS accesses, whose waits would wait for them.
 struct PageRef {
     int raw, off;
 };
-__device__ __forceinline__ PageRef page_ref(const AttnArgs &a, int b, int len, int key) {
+__device__ __forceinline__ PageRef page_ref(const AttnArgs &a, const int32_t *table, int len, int key) {
     const int k = min(key, len - 1), col = fdiv(k, a.c.f_page);
-    int zero = 0;
-    __asm__ volatile("" : "+v"(zero));
-    return {a.n.table[int64_t(b) * a.n.tld + col + zero], (k - col * a.c.page) & ~15};
+    unsigned at = col;
+    __asm__ volatile("" : "+v"(at));
+    return {table[at], (k - col * a.c.page) & ~15};
 }
 // The number where it is used: kNoPlace unless it is one of the cache's.
 __device__ __forceinline__ int page_of(const AttnArgs &a, const PageRef &r) {
@@ -274,6 +274,8 @@ __device__ __forceinline__ void load_q(const AttnArgs &a, const Row &row, int h,
 
 // ---- a row's sums -----------------------------------------------------------------------------
 
+constexpr float kLoose = 12.f;
+
 // Register r of block blk is value DB * i + blk of the lane's row, i = key_of(r, h).
 template <int DB>
 struct Sums {
@@ -286,10 +288,10 @@ struct Sums {
 #pragma unroll
         for (int blk = 0; blk < DB; ++blk) o[blk] = floatx16{};
     }
-    // The running maximum follows `top` only by steps of 2^8 or more: any number near it serves, as weights
-    // of up to 2^8 lose nothing in fp32 or bf16.  Returns what weights are taken from.
-    __device__ __forceinline__ float follow(float top) {
-        if (__any(top > m + 8.f || (m == -INFINITY && top > -INFINITY))) {
+    // The running maximum follows `top`, if that is above it by kLoose or more: any number near it serves, as weights
+    // of up to 2^kLoose lose nothing in fp32 or bf16.
+    __device__ __forceinline__ void follow(float top) {
+        if (__any(top > m + kLoose || (m == -INFINITY && top > -INFINITY))) {
             const float now = fmaxf(m, top);
             const float by = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
             m = now;
@@ -299,8 +301,9 @@ struct Sums {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[blk][r] *= by;
         }
-        return m == -INFINITY ? 0.f : m;
     }
+    // What weights are taken from.
+    __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.f : m; }
 };
 
 // w in parts of bf16, element e of an operand.
@@ -477,7 +480,8 @@ struct Direct {
         PageRef p[2];
     };
     __device__ __forceinline__ Pages pages(int key0) const {
-        return {page_ref(a, w.b, w.len, key0), page_ref(a, w.b, w.len, key0 + 16)};
+        const int32_t *table = a.n.table + int64_t(w.b) * a.n.tld;
+        return {page_ref(a, table, w.len, key0), page_ref(a, table, w.len, key0 + 16)};
     }
 
     // Loads of a tile.  A part without a page reads page 0 and counts as no key; past a row's dim its last
@@ -586,7 +590,8 @@ struct Direct {
         float top = fmaxf(x[0], x[1]);
 #pragma unroll
         for (int r = 2; r < 16; r += 2) top = fmaxf(fmaxf(top, x[r]), x[r + 1]);
-        const float off = s.follow(fmaxf(top, other_half(top)));
+        s.follow(fmaxf(top, other_half(top)));
+        const float off = s.base();
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             x[r] = __builtin_amdgcn_exp2f(x[r] - off);
@@ -765,77 +770,83 @@ struct Tiles {
     static constexpr int kPieces = 2 * DB;                         // 16-byte pieces of a row of K
     static constexpr int kLoads = DB / 2;                          // of a thread
     static_assert(kLoads <= 2, "a thread holds two scales");
+    static constexpr bool kEarly = P::PP == 1 && POW2;             // registers for V's operands before the weights are there
 
     const AttnArgs &a;
     const Work &w;
     const int lane, i, h, wave;
 
-    // What a thread of waves 0 to 3 holds of K, or one of waves 4 to 7 of V (wave 4 + st: keys 16 st and on).
+    // What a thread holds of a tile.  Waves 0 to 3 take K's keys 16 wave and on, waves 4 to 7 V's: one page each.
     struct Stage {
         unsigned raw[8 * W];
         unsigned sc0, sc1;                // scales as stored: of a K thread's loads, of a V thread's keys
         int valid;
     };
-
-    // The pages that the wave loads of a tile: a tile ahead of the loads.
-    struct Pages {
-        PageRef p[kLoads];
+    // What does not change from tile to tile: where the wave's head begins in page 0, and the lane's bytes there.
+    struct Where {
+        const uint8_t *rows;
+        const void *scales;
+        const int32_t *table;
+        unsigned lane;
+        int part;                         // the wave's keys of a tile: 16 part and on
     };
-    __device__ __forceinline__ Pages pages(int key0) const {
-        Pages r;
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) {
-            const int row = j * (256 / kPieces) + (wave & 3) * (64 / kPieces);   // K's: all in one part
-            r.p[j] = page_ref(a, w.b, w.len, key0 + (wave < 4 ? row & ~15 : 16 * (wave - 4)));
-        }
-        return r;
+    __device__ __forceinline__ Where where() const {
+        const int64_t head = int64_t(w.head) * a.c.page;
+        const int dim = a.c.dim, part = wave & 3;
+        const void *sp = wave < 4 ? a.c.ks : a.c.vs;
+        const unsigned at = wave < 4 ? unsigned(lane / kPieces * dim + min(16 * (lane % kPieces), dim - 16))
+                                     : unsigned(4 * h * dim + v_column<DB>(i, dim));
+        return {(wave < 4 ? a.c.k : a.c.v) + head * dim,
+                POW2 ? static_cast<const void *>(static_cast<const uint8_t *>(sp) + head)
+                     : static_cast<const void *>(static_cast<const unsigned *>(sp) + head),
+                a.n.table + int64_t(w.b) * a.n.tld, at, part};
+    }
+    // The page that the wave loads of a tile: a tile ahead of the loads.
+    __device__ __forceinline__ PageRef page(const Where &to, int key0) const {
+        return page_ref(a, to.table, w.len, key0 + 16 * to.part);
     }
 
-    __device__ __forceinline__ void load(Stage &st, const Pages &from, int key0) const {
-        const int dim = a.c.dim;
+    __device__ __forceinline__ void load(Stage &st, const Where &to, const PageRef &from, int key0) const {
+        const int dim = a.c.dim, id = page_of(a, from);
+        st.valid = id >= 0 ? min(16, max(w.len - key0 - 16 * to.part, 0)) : 0;
+        const int64_t page = max(id, 0);
+        const uint8_t *rows = to.rows + page * a.c.stride + from.off * dim;
+        const int64_t se = page * a.c.sstride + from.off;
         if (wave < 4) {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
-                const int64_t page = max(page_of(a, from.p[j]), 0);
-                const int r = ((wave & 3) * (64 / kPieces) & 15) + lane / kPieces, piece = lane % kPieces;
-                const int64_t at = w.head * a.c.page + from.p[j].off;
-                const intx4 x = *reinterpret_cast<const intx4 *>(a.c.k + page * a.c.stride + at * dim +
-                                                                 unsigned(r * dim + min(16 * piece, dim - 16)));
+                const intx4 x = *reinterpret_cast<const intx4 *>(rows + j * (64 / kPieces) * dim + to.lane);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) st.raw[4 * j + e] = x[e];
-                const unsigned sc = load_scale(a.c.ks, POW2 ? DS_SCALE_POW2 : DS_SCALE_F32, page * a.c.sstride + at + r);
+                const unsigned sc = load_scale(to.scales, POW2 ? DS_SCALE_POW2 : DS_SCALE_F32, se + j * (64 / kPieces) + lane / kPieces);
                 if (j == 0) st.sc0 = sc;
                 else st.sc1 = sc;
             }
         } else {
-            const int id = page_of(a, from.p[0]);
-            const int64_t page = max(id, 0);
-            st.valid = id >= 0 ? min(16, max(w.len - key0 - 16 * (wave - 4), 0)) : 0;
-            const int64_t at = w.head * a.c.page + from.p[0].off;
-            const uint8_t *vp = a.c.v + page * a.c.stride + at * dim;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 unsigned x[W];
-                load_v<DB>(vp + (e < 4 ? e : e + 4) * dim, unsigned(4 * h * dim + v_column<DB>(i, dim)), x);
+                load_v<DB>(rows + (e < 4 ? e : e + 4) * dim, to.lane, x);
 #pragma unroll
                 for (int word = 0; word < W; ++word) st.raw[e * W + word] = x[word];
             }
-            const int64_t se = page * a.c.sstride + at;
             if constexpr (kFoldV) {
-                const uint8_t *sp = static_cast<const uint8_t *>(a.c.vs) + se + 4 * h;
+                const uint8_t *sp = static_cast<const uint8_t *>(to.scales) + se + 4 * h;
                 __builtin_memcpy(&st.sc0, sp, 4);
                 __builtin_memcpy(&st.sc1, sp + 8, 4);
             } else {
-                st.sc0 = static_cast<const unsigned *>(a.c.vs)[se + (lane & 15)];
+                st.sc0 = static_cast<const unsigned *>(to.scales)[se + (lane & 15)];
             }
         }
     }
 
-    __device__ __forceinline__ void store(Stage &st, TileLds<DB> &t) const {
+    // edge: some row of the workgroup does not see some key of the tile.
+    __device__ __forceinline__ void store(Stage &st, TileLds<DB> &t, bool edge) const {
+        const int part = wave & 3;
         if (wave < 4) {
 #pragma unroll
             for (int j = 0; j < kLoads; ++j) {
-                const int r = j * (256 / kPieces) + wave * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
+                const int r = 16 * part + j * (64 / kPieces) + lane / kPieces, piece = lane % kPieces;
                 if (a.c.dim < 32 * DB && 16 * piece >= a.c.dim)      // (a number that is none times Q's 0 is no 0)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) st.raw[4 * j + e] = 0;
@@ -848,11 +859,14 @@ struct Tiles {
                 if (!kFoldK && piece == 0) t.sk[r] = by * a.scale;
             }
         } else {
-            const int part = wave - 4;
             float by[8];
             if constexpr (kFoldV) {
+                // (the conversion looks at the exponent alone)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) by[e] = scale_of((e < 4 ? st.sc0 : st.sc1) >> (8 * (e & 3)) & 0xff, DS_SCALE_POW2);
+                for (int e = 0; e < 8; ++e) {
+                    const unsigned sc = e < 4 ? st.sc0 : st.sc1;
+                    by[e] = __uint_as_float((e % 4 == 3 ? sc >> 1 : sc << (23 - 8 * (e % 4))) & 0x7f800000u);
+                }
             }
             if (st.valid < 16) {
                 int has = st.valid - 4 * h;
@@ -865,9 +879,13 @@ struct Tiles {
                         for (int word = 0; word < W; ++word) st.raw[e * W + word] = 0;
                     }
             }
-            unsigned bad = 0;
+            int note = st.valid;
+            if (edge) {
+                unsigned bad = 0;
 #pragma unroll
-            for (int e = 0; e < 8 * W; ++e) bad |= not_finite<FMT>(st.raw[e]);
+                for (int e = 0; e < 8 * W; ++e) bad |= not_finite<FMT>(st.raw[e]);
+                note |= __any(bad != 0) ? 1 << 16 : 0;
+            }
 #pragma unroll
             for (int word = 0; word < W; ++word)
 #pragma unroll
@@ -890,7 +908,6 @@ struct Tiles {
                     }
                 }
             if (!kFoldV && lane < 16) t.sv[16 * part + lane] = lane < st.valid ? __uint_as_float(st.sc0) : 0.f;
-            const int note = max(st.valid, 0) | (__any(bad != 0) ? 1 << 16 : 0);
             if (lane == 0) t.note[part] = note;
         }
     }
@@ -901,68 +918,77 @@ struct Tiles {
         for (int x = 0; x < 2 * DB; ++x)
             k[x] = __builtin_bit_cast(Op, t.k[unit_at<4 * DB>(32 * sub + i, 4 * (x >> 1) + 2 * h + (x & 1))]);
     }
-    __device__ __forceinline__ void read_v(const TileLds<DB> &t, int sub, bf16x8 (&v)[DB][2]) const {
-#pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-            for (int blk = 0; blk < DB; ++blk)
-                v[blk][st] = __builtin_bit_cast(bf16x8, t.v[unit_at<8>(blk * 32 + i, 4 * sub + 2 * st + h)]);
+    __device__ __forceinline__ bf16x8 read_v(const TileLds<DB> &t, int sub, int st, int blk) const {
+        return __builtin_bit_cast(bf16x8, t.v[unit_at<8>(blk * 32 + i, 4 * sub + 2 * st + h)]);
     }
 
     // A step takes 32 keys in two parts, in each of which the matrix unit works on one thing and the vector unit on another:
-    // the weights of these keys beside the scores of the next, and the product with V beside the next scores' maximum.
-    // The row's weights of scores x, with off from follow(), and the scores of the next keys.
-    __device__ __forceinline__ void weights(const TileLds<DB> &t, int sub, const float (&x)[16], float off, float c,
+    // the weights of these keys beside the scores of the next, and the product with V beside the next scores' scales.
+    // The row's weights of scores x, and the scores of the next keys.  Weights that come out at 2^kLoose or more say
+    // that the running maximum is too far behind, and are taken again; without them it is not looked at.
+    __device__ __forceinline__ void weights(const TileLds<DB> &t, int sub, const float (&x)[16], float c,
                                             const Op (&k)[2 * DB], const Op (&q)[P::QP][2 * DB], Sums<DB> &s,
-                                            bf16x8 (&pt)[2][P::PP], floatx16 &next) const {
-        next = floatx16{};
+                                            bf16x8 (&pt)[2][P::PP], floatx16 &next, bf16x8 (&v)[DB][2]) const {
+        // V's operands for what follows: half of them in the registers that K's leave
+        if constexpr (kEarly)
 #pragma unroll
-        for (int y = 0; y < 2 * DB; ++y)
+            for (int blk = 0; blk < DB; ++blk) v[blk][0] = read_v(t, sub, 0, blk);
+        const float off = s.base();
+        next = floatx16{};
+        float l[2] = {0.f, 0.f};
+        floatx4 sv;
+        const auto weigh = [&](int r, float from) {
+            if constexpr (!kFoldV)
+                if (r % 4 == 0) sv = *reinterpret_cast<const floatx4 *>(t.sv + 32 * sub + 2 * r + 4 * h);
+            const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[r], c, -from) : x[r] - from);
+            l[r & 1] += p;
+            put_weight<P::PP>(pt[r >> 3], r & 7, kFoldV ? p : p * sv[r & 3]);
+        };
+        // (in this order: a wave that waits for its own matrix instructions would leave the vector unit idle)
+        constexpr int kEach = 16 / (2 * DB);
+#pragma unroll
+        for (int y = 0; y < 2 * DB; ++y) {
 #pragma unroll
             for (int p = P::QP - 1; p >= 0; --p) next = mma(k[y], q[p][y], next);
-        float l[2] = {0.f, 0.f};
+            if (kEarly && y >= DB) v[y - DB][1] = read_v(t, sub, 1, y - DB);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            floatx4 sv;
-            if constexpr (!kFoldV) sv = *reinterpret_cast<const floatx4 *>(t.sv + 32 * sub + 8 * j + 4 * h);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = 4 * j + e;
-                const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[r], c, -off) : x[r] - off);
-                l[r & 1] += p;
-                put_weight<P::PP>(pt[r >> 3], r & 7, kFoldV ? p : p * sv[e]);
-            }
-        }
-        s.l += l[0] + l[1];
-        // a matrix instruction for every few of the vector unit's, after the reads; two parts of the weights
-        // leave no registers for that
-        if constexpr (P::PP == 1) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 2 * DB, 0);
-#pragma unroll
-            for (int y = 0; y < 2 * DB; ++y) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 56 / (2 * DB), 0);
-            }
+            for (int r = kEach * y; r < kEach * (y + 1); ++r) weigh(r, off);
             __builtin_amdgcn_sched_barrier(0);
         }
-    }
-    // Their product with V, and the largest of the next scores (of the lane; x: them, times K's scales).
-    __device__ __forceinline__ float product(const bf16x8 (&v)[DB][2], const bf16x8 (&pt)[2][P::PP], Sums<DB> &s,
-                                             const floatx16 &next, const TileLds<DB> &t, int sub, float (&x)[16]) const {
+        if (__any(l[0] + l[1] >= float(1 << int(kLoose)))) {
+            float top = largest(x);
+            top = fmaxf(top, other_half(top));
+            s.follow(kFoldK ? top * c : top);
+            l[0] = l[1] = 0.f;
+            const float now = s.base();
 #pragma unroll
-        for (int st = 0; st < 2; ++st)
-#pragma unroll
-            for (int part = P::PP - 1; part >= 0; --part)
-#pragma unroll
-                for (int blk = 0; blk < DB; ++blk) s.o[blk] = mma(v[blk][st], pt[st][part], s.o[blk]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            floatx4 sk;
-            if constexpr (!kFoldK) sk = *reinterpret_cast<const floatx4 *>(t.sk + 32 * sub + 8 * j + 4 * h);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[4 * j + e] = kFoldK ? next[4 * j + e] : next[4 * j + e] * sk[e];
+            for (int r = 0; r < 16; ++r) weigh(r, now);
         }
-        return largest(x);
+        s.l += l[0] + l[1];
+        if constexpr (!kEarly)
+#pragma unroll
+            for (int blk = 0; blk < DB; ++blk)
+#pragma unroll
+                for (int st = 0; st < 2; ++st) v[blk][st] = read_v(t, sub, st, blk);
+    }
+    // Their product with V, and x: the next scores, times K's scales.
+    __device__ __forceinline__ void product(const bf16x8 (&v)[DB][2], const bf16x8 (&pt)[2][P::PP], Sums<DB> &s,
+                                            const floatx16 &next, const TileLds<DB> &t, int sub, float (&x)[16]) const {
+        floatx4 sk;
+        constexpr int kEach = 16 / (2 * DB);
+#pragma unroll
+        for (int y = 0; y < 2 * DB; ++y) {
+            const int st = y / DB, blk = y % DB;
+#pragma unroll
+            for (int part = P::PP - 1; part >= 0; --part) s.o[blk] = mma(v[blk][st], pt[st][part], s.o[blk]);
+#pragma unroll
+            for (int r = kEach * y; r < kEach * (y + 1); ++r) {
+                if constexpr (!kFoldK)
+                    if (r % 4 == 0) sk = *reinterpret_cast<const floatx4 *>(t.sk + 32 * sub + 2 * r + 4 * h);
+                x[r] = kFoldK ? next[r] : next[r] * sk[r & 3];
+            }
+            if constexpr (!kFoldK) __builtin_amdgcn_sched_barrier(0);
+        }
     }
     __device__ __forceinline__ float largest(const float (&x)[16]) const {
         float top = fmaxf(x[0], x[1]);
@@ -971,23 +997,24 @@ struct Tiles {
         return top;
     }
     // The scores that the row does not see out of x (edge: there are some in the wave), and the maximum followed.
-    __device__ __forceinline__ float follow(float (&x)[16], float top, int key0, int sub, bool edge, const intx4 &note,
-                                            float c, const Row &row, Sums<DB> &s) const {
+    // True when all rows of the wave have seen some key.
+    __device__ __forceinline__ bool mask(float (&x)[16], int key0, int sub, bool edge, const intx4 &note, float c,
+                                         const Row &row, Sums<DB> &s) const {
         if (edge) {
-            // (known here alone, so that this stays a branch: tiles that all rows see spend nothing on it)
             const int at = key0 + 32 * sub + 4 * h;
-            int low = row.low - at, lim = row.lim - at, has = (note[2 * sub] & 0xffff) - 4 * h, has1 = (note[2 * sub + 1] & 0xffff) - 4 * h;
-            __asm__ volatile("" : "+v"(low), "+v"(lim), "+v"(has), "+v"(has1));
+            const int low = row.low - at, lim = row.lim - at;
+            const int has = (note[2 * sub] & 0xffff) - 4 * h, has1 = (note[2 * sub + 1] & 0xffff) - 4 * h;
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int k1 = key_of(r, 0);
                 const bool sees = k1 >= low && k1 < lim && (k1 & 15) < (r < 8 ? has : has1);
                 x[r] = sees ? x[r] : -INFINITY;
             }
-            top = largest(x);
         }
+        float top = largest(x);
         top = fmaxf(top, other_half(top));
-        return s.follow(kFoldK ? top * c : top);
+        s.follow(kFoldK ? top * c : top);
+        return __all(s.m > -INFINITY);
     }
 };
 
@@ -1027,13 +1054,15 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
     bool fine = true;
     if (from < until) {
         typename Tl::Stage st;
-        tl.load(st, tl.pages(from), from);
-        typename Tl::Pages pages = tl.pages(from + kTileKeys);
-        tl.store(st, lds[0]);
+        const typename Tl::Where to = tl.where();
+        const auto wg_edge = [&](int key) { return key + kTileKeys > wg_every || key < wg_since; };
+        tl.load(st, to, tl.page(to, from), from);
+        PageRef page = tl.page(to, from + kTileKeys);
+        tl.store(st, lds[0], wg_edge(from));
         if (from + kTileKeys < until) {
-            const typename Tl::Pages p = pages;
-            pages = tl.pages(from + 2 * kTileKeys);
-            tl.load(st, p, from + kTileKeys);
+            const PageRef p = page;
+            page = tl.page(to, from + 2 * kTileKeys);
+            tl.load(st, to, p, from + kTileKeys);
         }
         lds_barrier();
         intx4 note;
@@ -1044,61 +1073,53 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) note[e] = __builtin_amdgcn_readfirstlane(note[e]);
             edge = key + kTileKeys > every || key < since || (note[0] & note[1] & note[2] & note[3] & 0xffff) != 16;
-            return !((note[0] | note[1] | note[2] | note[3]) >> 16 && (key + kTileKeys > wg_every || key < wg_since));
+            return !((note[0] | note[1] | note[2] | note[3]) >> 16);
         };
         typename Tl::Op k[2 * DB];
         bf16x8 v[DB][2], pt[2][Parts<T>::PP];
-        floatx16 next;
-        float x[16], off;
+        floatx16 next = {};
+        float x[16];
+        bool begun = false;                // all rows have a maximum
         fine = look(lds[0], from);
         tl.read_k(lds[0], 0, k);
-        next = floatx16{};
 #pragma unroll
         for (int y = 0; y < 2 * DB; ++y)
 #pragma unroll
             for (int p = Parts<T>::QP - 1; p >= 0; --p) next = mma(k[y], q[p][y], next);
 #pragma unroll
-        for (int blk = 0; blk < DB; ++blk)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) v[blk][e] = pt[e][0] = bf16x8{};
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int part = 0; part < Parts<T>::PP; ++part) pt[e][part] = bf16x8{};
-        off = tl.follow(x, tl.product(v, pt, s, next, lds[0], 0, x), from, 0, edge, note, c, row, s);
+        for (int r = 0; r < 16; ++r) x[r] = Tl::kFoldK ? next[r] : next[r] * lds[0].sk[key_of(r, h)];
         tl.read_k(lds[0], 1, k);
-        constexpr bool kAhead = Parts<T>::PP == 1;
         int at = 0;
         for (int key = from; fine; key += kTileKeys) {
             const TileLds<DB> &t = lds[at];
             const int after = at == 2 ? 0 : at + 1;
             const bool more = key + kTileKeys < until;
-            if constexpr (kAhead) tl.read_v(t, 0, v);
-            tl.weights(t, 0, x, off, c, k, q, s, pt, next);
-            if constexpr (!kAhead) tl.read_v(t, 0, v);
-            const float top = tl.product(v, pt, s, next, t, 1, x);
-            if constexpr (Parts<T>::PP == 1) __builtin_amdgcn_sched_barrier(0);
-            off = tl.follow(x, top, key, 1, edge, note, c, row, s);
+            if (edge || !begun) begun = tl.mask(x, key, 0, edge, note, c, row, s);
             if (more) {
-                tl.store(st, lds[after]);
+                tl.store(st, lds[after], wg_edge(key + kTileKeys));
                 if (key + 2 * kTileKeys < until) {
-                    const typename Tl::Pages p = pages;
-                    pages = tl.pages(key + 3 * kTileKeys);
-                    tl.load(st, p, key + 2 * kTileKeys);
+                    const PageRef p = page;
+                    page = tl.page(to, key + 3 * kTileKeys);
+                    tl.load(st, to, p, key + 2 * kTileKeys);
                 }
+            }
+            tl.weights(t, 0, x, c, k, q, s, pt, next, v);
+            const bool hidden = edge;
+            const intx4 now = note;
+            if (more) {
                 lds_barrier();
                 fine = look(lds[after], key + kTileKeys);
             }
             // (behind the last tile the scores of whatever lies there, which nobody takes)
-            tl.read_k(lds[after], 0, k);
-            if constexpr (kAhead) tl.read_v(t, 1, v);
-            tl.weights(t, 1, x, off, c, k, q, s, pt, next);
-            if constexpr (!kAhead) tl.read_v(t, 1, v);
-            const float then = tl.product(v, pt, s, next, lds[after], 0, x);
+            if constexpr (Tl::kEarly) tl.read_k(lds[after], 0, k);
+            tl.product(v, pt, s, next, t, 1, x);
+            if constexpr (!Tl::kEarly) tl.read_k(lds[after], 0, k);
+            if (hidden || !begun) begun = tl.mask(x, key, 1, hidden, now, c, row, s);
+            tl.weights(t, 1, x, c, k, q, s, pt, next, v);
+            if constexpr (Tl::kEarly) tl.read_k(lds[after], 1, k);
+            tl.product(v, pt, s, next, lds[after], 0, x);
+            if constexpr (!Tl::kEarly) tl.read_k(lds[after], 1, k);
             if (!more) break;
-            tl.read_k(lds[after], 1, k);
-            if constexpr (Parts<T>::PP == 1) __builtin_amdgcn_sched_barrier(0);
-            off = tl.follow(x, then, key + kTileKeys, 0, edge, note, c, row, s);
             at = after;
         }
     }
