@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 try:
     # PyTorch ships its own HIP runtime (same soname).  Loading it before the
@@ -927,15 +928,21 @@ class Chunk:
         self._p = C.addressof(self._c)
 
 
+# the bytes of a ds_heads and of a ds_attn8_cfg (a third of the time of the ctypes structure)
+_pack_heads = struct.Struct("@Pqqqqqii").pack
+_pack_cfg = struct.Struct("@diiqq").pack
+
+
 def _heads(t):
     """The C form of a tensor [tokens, heads, dim] whose rows' elements are side by side."""
-    if t.dtype not in _PLAIN:
+    kind = _PLAIN.get(t.dtype)
+    if kind is None:
         raise TypeError(f"fp32, fp16 or bf16, not {t.dtype}")
     tokens, heads, dim = t.shape
     ld, hld, one = t.stride()
     if one != 1 and dim > 1:
         raise ValueError(f"elements of a row are {one} apart, not side by side")
-    return ds_heads(t.data_ptr(), tokens, heads, dim, ld, hld, _PLAIN[t.dtype], 0)
+    return _pack_heads(t.data_ptr(), tokens, heads, dim, ld, hld, kind, 0)
 
 
 def _list(t, dtype, n, what):
@@ -956,9 +963,10 @@ def ds_rotary(x, pos, freqs, y=None, *, pairs=False, scale=1.0, inverse=False, s
             return ds_rotary(x, pos, freqs, y, pairs=pairs, scale=scale, inverse=inverse, stream=stream)
     mode = (DS_ROTARY_PAIRS if pairs else DS_ROTARY_HALVES) + (DS_ROTARY_INVERSE if inverse else 0)
     n = freqs.numel()
-    return check("ds_rotary", lib.ds_rotary(C.byref(_heads(x)), _list(pos, _torch.int32, x.shape[0], "pos"),
+    hx = _heads(x)
+    return check("ds_rotary", lib.ds_rotary(hx, _list(pos, _torch.int32, x.shape[0], "pos"),
                                             _list(freqs, _torch.float32, n, "freqs"), 2 * n, mode, scale,
-                                            C.byref(_heads(y)), _q8_stream(stream, dev)))
+                                            hx if y is x else _heads(y), _q8_stream(stream, dev)))
 
 
 def _cache8_rows(name, cache, chunk, k, v, stream):
@@ -966,8 +974,7 @@ def _cache8_rows(name, cache, chunk, k, v, stream):
     if dev != _torch.cuda.current_device():
         with _torch.cuda.device(dev):
             return _cache8_rows(name, cache, chunk, k, v, stream)
-    return check(name, getattr(lib, name)(cache._p, chunk._p, C.byref(_heads(k)), C.byref(_heads(v)),
-                                          _q8_stream(stream, dev)))
+    return check(name, getattr(lib, name)(cache._p, chunk._p, _heads(k), _heads(v), _q8_stream(stream, dev)))
 
 
 def ds_cache8_write(cache, chunk, k, v, stream=None):
@@ -984,8 +991,8 @@ def ds_cache8_read(cache, chunk, k, v, stream=None):
 def ds_attn8_work(q, cache, chunk, *, scale=None, causal=True, window=0, max_len=0):
     """Bytes of the workspace of ds_attn8 with these arguments."""
     n = C.c_int64()
-    cfg = ds_attn8_cfg(q.shape[2] ** -0.5 if scale is None else scale, causal, 0, window, max_len)
-    check("ds_attn8_work", lib.ds_attn8_work(C.byref(_heads(q)), cache._p, chunk._p, C.byref(cfg), C.byref(n)))
+    cfg = _pack_cfg(q.shape[2] ** -0.5 if scale is None else scale, causal, 0, window, max_len)
+    check("ds_attn8_work", lib.ds_attn8_work(_heads(q), cache._p, chunk._p, cfg, C.byref(n)))
     return n.value
 
 
@@ -1002,8 +1009,8 @@ def ds_attn8(q, cache, chunk, out, lse=None, *, scale=None, causal=True, window=
         with _torch.cuda.device(dev):
             return ds_attn8(q, cache, chunk, out, lse, scale=scale, causal=causal, window=window, max_len=max_len,
                             work=work, stream=stream)
-    cfg = C.byref(ds_attn8_cfg(q.shape[2] ** -0.5 if scale is None else scale, causal, 0, window, max_len))
-    qh, oh = C.byref(_heads(q)), C.byref(_heads(out))
+    cfg = _pack_cfg(q.shape[2] ** -0.5 if scale is None else scale, causal, 0, window, max_len)
+    qh, oh = _heads(q), _heads(out)
     if lse is not None and (lse.dtype != _torch.float32 or tuple(lse.shape) != tuple(q.shape[:2]) or
                             not lse.is_contiguous()):
         raise ValueError(f"lse: {lse.dtype} of shape {tuple(lse.shape)}, not float32 of {tuple(q.shape[:2])}")

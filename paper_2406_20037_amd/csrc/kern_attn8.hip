@@ -126,7 +126,8 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
     const int64_t unit = p.form == kAttnShare ? 128 : 64, slots = p.form == kAttnTiles ? 256 : 512, beside = 4 * unit;
     const int64_t work = std::max((rows + tile - 1) / tile, std::min(q->tokens, chunk->seqs)) * cache->heads;
     int64_t best = INT64_MAX;
-    for (int64_t splits = 1; splits <= kMostSplits; ++splits) {
+    for (const int64_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+        static_assert(kMostSplits == 64, "the last of these");
         const int64_t span = std::max(unit, ((keys + splits - 1) / splits + unit - 1) / unit * unit);
         const int64_t n = std::max<int64_t>(1, (keys + span - 1) / span);
         const int64_t time = (work * n + slots - 1) / slots * (span + beside) + (n > 1 ? beside : 0);
