@@ -21,7 +21,7 @@ struct AttnArgs {
     int causal, window, len;              // len: most keys of a sequence that are seen
     int splits, span;                     // keys of a split
     int vec_q, vec_o;                     // rows of 16-byte groups
-    FastDiv f_group, f_kv, f_splits;
+    FastDiv f_group, f_kv, f_splits, f_dim4;
 };
 
 // Three forms of the kernel (attn8_kernel.h): waves that share 32 rows and split the keys; waves of 32 rows

@@ -29,6 +29,7 @@ namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
 
 constexpr int kKeys = 32;                 // keys of a matrix instruction's tile
 constexpr float kLn2 = 0.69314718055994530942f;
@@ -395,7 +396,6 @@ __device__ __forceinline__ void finish(const AttnArgs &a, const Work &w, const R
             if (d < a.c.dim) {
 #pragma unroll
                 for (int blk = 0; blk < DB; blk += 2) {
-                    typedef float floatx2 __attribute__((ext_vector_type(2)));
                     *reinterpret_cast<floatx2 *>(to + d + blk) = floatx2{s.o[blk][r], s.o[blk + 1][r]};
                 }
             }
@@ -659,21 +659,28 @@ struct Direct {
 template <typename T, int DB>
 constexpr int waves_of = DB <= 4 && !std::is_same_v<T, float> ? 2 : 1;
 
-// Four waves share 32 rows and take tiles of keys in turn.
+// Four waves share 32 rows and take tiles of keys in turn.  Their sums meet in LDS, some rows at a time, and
+// all threads join four values each.
 template <typename T, int FMT, int DB>
 __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a) {
-    constexpr int kSlot = 64 + 64 * 16 * DB;
+    constexpr int kJoin = DB == 8 ? 8 : 16, kLine = 32 * DB + 4;      // rows at a time, floats between them
     __shared__ __attribute__((aligned(16))) float scales[4 * 64];
-    __shared__ float join[2 * kSlot];
+    __shared__ __attribute__((aligned(16))) float sums[4][kJoin][kLine];
+    __shared__ float2 ml[4][32];
     Work w;
     if (!find_work<32>(a, w)) return;
     const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Row row = find_row(a, w, w.row0 + i);
-    typename Parts<T>::Op q[Parts<T>::QP][2 * DB];
-    load_q<T, DB>(a, row, h, 1.f, q);
     int from, until;
     w.keys(a, w.row0 + 31, from, until);
+    if (a.splits > 1 && from >= until) {   // a split past the sequence's end
+        if (wave == 0 && h == 0 && row.is)
+            a.ml[(int64_t(w.split) * a.n.tokens + row.tok) * a.heads + row.head] = make_float2(-INFINITY, 0.f);
+        return;
+    }
+    typename Parts<T>::Op q[Parts<T>::QP][2 * DB];
+    load_q<T, DB>(a, row, h, 1.f, q);
     Sums<DB> s;
     const bool fine = Direct<T, FMT, DB>(a, w, row, q, s)
                           .template walk<4 * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
@@ -683,36 +690,58 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a
         if (wave == 0) slow_sums<T, FMT, DB>(late_args(), w, row, q, h, from, until, s);
     }
     s.l += other_half(s.l);
-    // four waves' sums of the same rows: two waves take another's each, then one
+    if (h == 0) ml[wave][i] = make_float2(s.m, s.l);
+    const AttnArgs al = late_args();
+    const int rows = min(32, w.rows - w.row0);
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += kJoin) {
+        if (r0 > 0) __syncthreads();
+        if (i >= r0 && i < r0 + kJoin) {
+            float *to = sums[wave][i - r0];
 #pragma unroll
-    for (int half = 2; half > 0; half /= 2) {
-        __syncthreads();
-        if (wave >= half && wave < 2 * half) {
-            float *to = join + (wave - half) * kSlot;
-            if (h == 0) {
-                to[i] = s.m;
-                to[32 + i] = s.l;
-            }
+            for (int r = 0; r < 16; ++r)
 #pragma unroll
-            for (int blk = 0; blk < DB; ++blk)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) to[64 + (blk * 16 + r) * 64 + lane] = s.o[blk][r];
+                for (int blk = 0; blk < DB; blk += 2)
+                    *reinterpret_cast<floatx2 *>(to + DB * key_of(r, h) + blk) = floatx2{s.o[blk][r], s.o[blk + 1][r]};
         }
         __syncthreads();
-        if (wave < half) {
-            const float *of = join + wave * kSlot;
-            const float om = of[i], ol = of[32 + i], now = fmaxf(s.m, om);
-            const float by = s.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s.m - now);
-            const float bo = om == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(om - now);
-            s.m = now;
-            s.l = s.l * by + ol * bo;
+        const int line = al.c.dim / 4, n = min(kJoin, rows - r0) * line;
+        for (int x = threadIdx.x; x < n; x += 256) {
+            const int r = fdiv(x, al.f_dim4), d = 4 * (x - r * line);
+            const Row out = find_row(al, w, w.row0 + r0 + r);
+            float m = -INFINITY, l = 0.f;
 #pragma unroll
-            for (int blk = 0; blk < DB; ++blk)
+            for (int y = 0; y < 4; ++y) m = fmaxf(m, ml[y][r0 + r].x);
+            floatx4 sum = {};
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s.o[blk][r] = s.o[blk][r] * by + of[64 + (blk * 16 + r) * 64 + lane] * bo;
+            for (int y = 0; y < 4; ++y) {
+                const float2 of = ml[y][r0 + r];
+                const float by = of.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of.x - m);
+                l += of.y * by;
+                sum += by * *reinterpret_cast<const floatx4 *>(&sums[y][r][d]);
+            }
+            const int64_t at = int64_t(out.tok) * al.heads + out.head;
+            if (al.splits > 1) {
+                const int64_t p = int64_t(w.split) * al.n.tokens * al.heads + at;
+                if (d == 0) al.ml[p] = make_float2(m, l);
+                *reinterpret_cast<floatx4 *>(al.part + p * al.c.dim + d) = sum;
+                continue;
+            }
+            const float by = l == 0.f ? 0.f : 1.f / l;
+            if (al.lse && d == 0) al.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+            T y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = T(l == 0.f ? 0.f : sum[e] * by);
+            T *to = static_cast<T *>(al.out) + out.tok * al.ldo + out.head * al.hldo + d;
+            if (al.vec_o) {
+                typedef int intv __attribute__((ext_vector_type(sizeof(T))));
+                *reinterpret_cast<intv *>(to) = *reinterpret_cast<const intv *>(y);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to[e] = y[e];
+            }
         }
     }
-    if (wave == 0) finish<T, DB>(late_args(), w, row, s, h);
 }
 
 // Each wave has rows of its own and reads keys by itself.

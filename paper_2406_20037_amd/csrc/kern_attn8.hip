@@ -235,6 +235,7 @@ int ds_attn8(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, c
     a.f_group = make_fastdiv(a.group);
     a.f_kv = make_fastdiv(cache->heads);
     a.f_splits = make_fastdiv(a.splits);
+    a.f_dim4 = make_fastdiv(cache->dim / 4);
     a.vec_q = heads16(q);
     a.vec_o = heads16(out);
     if (q->type == DS_TYPE_F32) return run<float>(p, a, stream);
