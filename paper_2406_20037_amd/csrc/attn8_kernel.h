@@ -236,42 +236,65 @@ __device__ __forceinline__ Row find_row(const AttnArgs &a, const Work &w, int r)
     return {w.s0 + t, w.head * a.group + min(r, w.rows - 1) - t * a.group, r < w.rows, w.low(a, t), w.lim(a, t)};
 }
 
-// The row of Q as operands: operand 2 c + u of a lane has values 32 c + 16 h + 8 u and on.
-template <typename T, int DB>
-__device__ __forceinline__ void load_q(const AttnArgs &a, const Row &row, int h, float by,
-                                       typename Parts<T>::Op (&q)[Parts<T>::QP][2 * DB]) {
+// Operand c of the row of Q, in parts: values 32 (c / 2) + 16 h + 8 (c % 2) and on.
+template <typename T>
+__device__ __forceinline__ void load_q1(const AttnArgs &a, const Row &row, int h, int c, float by,
+                                        typename Parts<T>::Op (&q)[Parts<T>::QP]) {
     const T *qp = static_cast<const T *>(a.q) + row.tok * a.ldq + row.head * a.hldq;
+    const int d = 32 * (c >> 1) + 16 * h + 8 * (c & 1);
+    T x[8];
 #pragma unroll
-    for (int c = 0; c < 2 * DB; ++c) {
-        const int d = 32 * (c >> 1) + 16 * h + 8 * (c & 1);
-        T x[8];
+    for (int e = 0; e < 8; ++e) x[e] = T(0.f);
+    if (d < a.c.dim) {
+        if (a.vec_q) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = T(0.f);
-        if (d < a.c.dim) {
-            if (a.vec_q) {
+            for (size_t e = 0; e < sizeof(x) / 16; ++e)
+                reinterpret_cast<intx4 *>(x)[e] = reinterpret_cast<const intx4 *>(qp + d)[e];
+        } else {
 #pragma unroll
-                for (size_t e = 0; e < sizeof(x) / 16; ++e)
-                    reinterpret_cast<intx4 *>(x)[e] = reinterpret_cast<const intx4 *>(qp + d)[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = qp[d + e];
-            }
+            for (int e = 0; e < 8; ++e) x[e] = qp[d + e];
         }
+    }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if constexpr (Parts<T>::QP == 1) {
-                q[0][c][e] = T(float(x[e]) * by);
-            } else {
-                float rest = float(x[e]) * by;
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (Parts<T>::QP == 1) {
+            q[0][e] = T(float(x[e]) * by);
+        } else {
+            float rest = float(x[e]) * by;
 #pragma unroll
-                for (int p = 0; p < Parts<T>::QP; ++p) {
-                    q[p][c][e] = __bf16(rest);
-                    rest -= float(q[p][c][e]);
-                }
+            for (int p = 0; p < Parts<T>::QP; ++p) {
+                q[p][e] = __bf16(rest);
+                rest -= float(q[p][e]);
             }
         }
     }
 }
+template <typename T, int DB>
+__device__ __forceinline__ void load_q(const AttnArgs &a, const Row &row, int h, float by,
+                                       typename Parts<T>::Op (&q)[Parts<T>::QP][2 * DB]) {
+#pragma unroll
+    for (int c = 0; c < 2 * DB; ++c) {
+        typename Parts<T>::Op x[Parts<T>::QP];
+        load_q1<T>(a, row, h, c, by, x);
+#pragma unroll
+        for (int p = 0; p < Parts<T>::QP; ++p) q[p][c] = x[p];
+    }
+}
+
+// Q where a wave keeps it: in registers, or in LDS, where waves of the same rows share it and leave registers
+// for keys that are on their way.
+template <typename T, int DB>
+struct HeldQ {
+    typename Parts<T>::Op q[Parts<T>::QP][2 * DB];
+    __device__ __forceinline__ typename Parts<T>::Op get(int p, int c) const { return q[p][c]; }
+};
+template <typename T, int DB>
+struct SharedQ {
+    const intx4 *q;                       // [part][operand][lane]
+    __device__ __forceinline__ typename Parts<T>::Op get(int p, int c) const {
+        return __builtin_bit_cast(typename Parts<T>::Op, q[(p * 2 * DB + c) * 64]);
+    }
+};
 
 // ---- a row's sums -----------------------------------------------------------------------------
 
@@ -320,10 +343,9 @@ __device__ __forceinline__ void put_weight(bf16x8 (&to)[PP], int e, float w) {
 
 // The rows' sums once more, key by key in plain fp32, [key, until): for tiles whose values hold infinities or NaNs
 // where some row does not see all keys, as 0 times those is no 0.  Slow, small and met by broken numbers only.
-template <typename T, int FMT, int DB>
-__device__ __forceinline__ void slow_sums(const AttnArgs &a, const Work &w, const Row &row,
-                                          const typename Parts<T>::Op (&q)[Parts<T>::QP][2 * DB], int h, int key, int until,
-                                          Sums<DB> &s) {
+template <typename T, int FMT, int DB, typename Q>
+__device__ __forceinline__ void slow_sums(const AttnArgs &a, const Work &w, const Row &row, const Q &q, int h, int key,
+                                          int until, Sums<DB> &s) {
     const auto bytes = [](const uint8_t *p, int n) {
         unsigned x = 0;
         for (int e = 0; e < n; ++e) x |= unsigned(p[e]) << (8 * e);
@@ -346,7 +368,7 @@ __device__ __forceinline__ void slow_sums(const AttnArgs &a, const Work &w, cons
             const bf16x8 kd = decode_k<FMT, bf16x8>(int(bytes(k + d, 4)), int(bytes(k + d + 4, 4)));
 #pragma unroll
             for (int p = 0; p < Parts<T>::QP; ++p) {
-                intx4 held = __builtin_bit_cast(intx4, q[p][c]);
+                intx4 held = __builtin_bit_cast(intx4, q.get(p, c));
                 __asm__ volatile("" : "+v"(held));         // (its fp32 values are no registers of the loop's)
                 const auto qd = __builtin_bit_cast(typename Parts<T>::Op, held);
 #pragma unroll
@@ -458,7 +480,8 @@ __device__ __forceinline__ void load_v(const uint8_t *p, unsigned at, unsigned (
     }
 }
 
-template <typename T, int FMT, int DB>
+// TILES: of a lane's registers, one in use and the others on their way.
+template <typename T, int FMT, int DB, typename Q, int TILES>
 struct Direct {
     using P = Parts<T>;
     using Op = typename P::Op;
@@ -466,13 +489,12 @@ struct Direct {
     const AttnArgs &a;
     const Work &w;
     const Row &row;
-    const Op (&q)[P::QP][2 * DB];
+    const Q &q;
     Sums<DB> &s;
     const int lane, i, h;
     const unsigned koff, voff;            // of the lane in a 16-key part of a page
 
-    __device__ __forceinline__ Direct(const AttnArgs &a_, const Work &w_, const Row &r_, const Op (&q_)[P::QP][2 * DB],
-                                      Sums<DB> &s_)
+    __device__ __forceinline__ Direct(const AttnArgs &a_, const Work &w_, const Row &r_, const Q &q_, Sums<DB> &s_)
         : a(a_), w(w_), row(r_), q(q_), s(s_), lane(threadIdx.x & 63), i(lane & 31), h(lane >> 5),
           koff((i & 15) * a_.c.dim), voff(4 * h * a_.c.dim + v_column<DB>(i, a_.c.dim)) {}
 
@@ -549,7 +571,7 @@ struct Direct {
             for (int u = 0; u < 2; ++u) {
                 const Op k = decode_k<FMT, Op>(t.k[c][2 * u], t.k[c][2 * u + 1]);
 #pragma unroll
-                for (int p = P::QP - 1; p >= 0; --p) sum = mma(k, q[p][2 * c + u], sum);
+                for (int p = P::QP - 1; p >= 0; --p) sum = mma(k, q.get(p, 2 * c + u), sum);
             }
         __builtin_amdgcn_sched_barrier(0);
         bf16x8 pt[2][P::PP];
@@ -626,29 +648,31 @@ struct Direct {
             return key + kKeys > every || key < since || t.valid != (16 | 16 << 16);
         };
         s.clear();
-        if constexpr (DB == 8) {
-            // (the registers hold one tile of 256 values a row)
+        if constexpr (TILES == 1) {
             for (; key < until && fine; key += STEP) {
                 Tile<DB> t;
                 load(t, pages(key), key);
                 fine = step(t, key, edge(t), lds);
             }
         } else if (key < until) {
-            Tile<DB> t[2];
-            load(t[0], pages(key), key);
-            Pages next = pages(key + STEP);
-            const auto one = [&](Tile<DB> &now, Tile<DB> &then) {
-                const Pages after = pages(key + 2 * STEP);
-                if (key + STEP < until) load(then, next, key + STEP);
+            Tile<DB> t[TILES];
+            Pages next = pages(key);
+#pragma unroll
+            for (int x = 0; x + 1 < TILES; ++x) {
+                const Pages after = pages(key + (x + 1) * STEP);
+                if (x == 0 || key + x * STEP < until) load(t[x], next, key + x * STEP);
                 next = after;
-                fine = step(now, key, edge(now), lds);
-                key += STEP;
-            };
-            while (true) {
-                one(t[0], t[1]);
-                if (key >= until || !fine) break;
-                one(t[1], t[0]);
-                if (key >= until || !fine) break;
+            }
+            while (fine && key < until) {
+#pragma unroll
+                for (int x = 0; x < TILES; ++x) {
+                    if (!fine || key >= until) break;
+                    const Pages after = pages(key + TILES * STEP);
+                    if (key + (TILES - 1) * STEP < until) load(t[(x + TILES - 1) % TILES], next, key + (TILES - 1) * STEP);
+                    next = after;
+                    fine = step(t[x], key, edge(t[x]), lds);
+                    key += STEP;
+                }
             }
         }
         return fine;
@@ -659,6 +683,10 @@ struct Direct {
 template <typename T, int DB>
 constexpr int waves_of = DB <= 4 && !std::is_same_v<T, float> ? 2 : 1;
 
+// Tiles of keys that a wave of attn8_share has in registers.
+template <typename T, int DB>
+constexpr int share_tiles = DB == 8 ? 2 : 3;
+
 // Four waves share 32 rows and take tiles of keys in turn.  Their sums meet in LDS, some rows at a time, and
 // all threads join four values each.
 template <typename T, int FMT, int DB>
@@ -667,6 +695,7 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a
     __shared__ __attribute__((aligned(16))) float scales[4 * 64];
     __shared__ __attribute__((aligned(16))) float sums[4][kJoin][kLine];
     __shared__ float2 ml[4][32];
+    __shared__ intx4 qs[Parts<T>::QP][2 * DB][64];
     Work w;
     if (!find_work<32>(a, w)) return;
     const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
@@ -679,15 +708,23 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a
             a.ml[(int64_t(w.split) * a.n.tokens + row.tok) * a.heads + row.head] = make_float2(-INFINITY, 0.f);
         return;
     }
-    typename Parts<T>::Op q[Parts<T>::QP][2 * DB];
-    load_q<T, DB>(a, row, h, 1.f, q);
+#pragma unroll
+    for (int y = 0; y < DB / 2; ++y) {
+        typename Parts<T>::Op x[Parts<T>::QP];
+        const int c = wave * (DB / 2) + y;
+        load_q1<T>(a, row, h, c, 1.f, x);
+#pragma unroll
+        for (int p = 0; p < Parts<T>::QP; ++p) qs[p][c][lane] = __builtin_bit_cast(intx4, x[p]);
+    }
+    __syncthreads();
+    const SharedQ<T, DB> q{&qs[0][0][lane]};
     Sums<DB> s;
-    const bool fine = Direct<T, FMT, DB>(a, w, row, q, s)
+    const bool fine = Direct<T, FMT, DB, SharedQ<T, DB>, share_tiles<T, DB>>(a, w, row, q, s)
                           .template walk<4 * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
                                                     w.low(a, w.token(a, w.row0 + 31)), scales + wave * 64);
     if (__syncthreads_or(!fine)) {        // then the first wave takes all keys
         s.clear();
-        if (wave == 0) slow_sums<T, FMT, DB>(late_args(), w, row, q, h, from, until, s);
+        if (wave == 0) slow_sums<T, FMT, DB, SharedQ<T, DB>>(late_args(), w, row, q, h, from, until, s);
     }
     s.l += other_half(s.l);
     if (h == 0) ml[wave][i] = make_float2(s.m, s.l);
@@ -754,16 +791,16 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_own(AttnArgs a) 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = w.row0 + 32 * wave;
     if (row0 >= w.rows) return;
     const Row row = find_row(a, w, row0 + i);
-    typename Parts<T>::Op q[Parts<T>::QP][2 * DB];
-    load_q<T, DB>(a, row, h, 1.f, q);
+    HeldQ<T, DB> q;
+    load_q<T, DB>(a, row, h, 1.f, q.q);
     int from, until;
     w.keys(a, row0 + 31, from, until);
     Sums<DB> s;
     from = max(from, w.low(a, w.token(a, row0)) & ~(kKeys - 1));
-    const bool fine = Direct<T, FMT, DB>(a, w, row, q, s)
+    const bool fine = Direct<T, FMT, DB, HeldQ<T, DB>, DB == 8 ? 1 : 2>(a, w, row, q, s)
                           .template walk<kKeys>(from, until, w.lim(a, w.token(a, row0)), w.low(a, w.token(a, row0 + 31)),
                                                 scales + wave * 64);
-    if (!fine) slow_sums<T, FMT, DB>(late_args(), w, row, q, h, from, until, s);
+    if (!fine) slow_sums<T, FMT, DB, HeldQ<T, DB>>(late_args(), w, row, q, h, from, until, s);
     s.l += other_half(s.l);
     finish<T, DB>(late_args(), w, row, s, h);
 }
@@ -1154,8 +1191,9 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
     }
     const AttnArgs al = late_args();
     if (!fine) {
-        if (Tl::kFoldK) load_q<T, DB>(al, row, h, 1.f, q);
-        slow_sums<T, FMT, DB>(al, w, row, q, h, from, until, s);
+        HeldQ<T, DB> held;
+        load_q<T, DB>(al, row, h, 1.f, held.q);
+        slow_sums<T, FMT, DB, HeldQ<T, DB>>(al, w, row, held, h, from, until, s);
     }
     s.l += other_half(s.l);
     finish<T, DB>(al, w, row, s, h);
