@@ -24,11 +24,11 @@ struct AttnArgs {
     FastDiv f_group, f_kv, f_splits, f_dim4;
 };
 
-// Three forms of the kernel (attn8_kernel.h): waves that share 32 rows and split the keys; waves of 32 rows
+// Four forms of the kernel (attn8_kernel.h): waves that share 16 or 32 rows and split the keys; waves of 32 rows
 // each that read keys by themselves; waves of 32 rows each that share the keys through LDS.
-enum { kAttnShare, kAttnOwn, kAttnTiles };
+enum { kAttnFew, kAttnShare, kAttnOwn, kAttnTiles };
 constexpr int attn8_threads(int form) { return form == kAttnTiles ? 512 : 256; }
-constexpr int attn8_rows(int form) { return form == kAttnShare ? 32 : attn8_threads(form) / 2; }
+constexpr int attn8_rows(int form) { return form == kAttnFew ? 16 : form == kAttnShare ? 32 : attn8_threads(form) / 2; }
 constexpr int attn8_dim_blocks(int dim) { return dim <= 64 ? 2 : dim <= 128 ? 4 : 8; }
 
 // Whether the many rows of a type and width take kAttnOwn (else kAttnTiles): where the registers hold no more

@@ -236,12 +236,11 @@ __device__ __forceinline__ Row find_row(const AttnArgs &a, const Work &w, int r)
     return {w.s0 + t, w.head * a.group + min(r, w.rows - 1) - t * a.group, r < w.rows, w.low(a, t), w.lim(a, t)};
 }
 
-// Operand c of the row of Q, in parts: values 32 (c / 2) + 16 h + 8 (c % 2) and on.
+// Values d to d + 7 of the row of Q as an operand, in parts.
 template <typename T>
-__device__ __forceinline__ void load_q1(const AttnArgs &a, const Row &row, int h, int c, float by,
+__device__ __forceinline__ void load_q1(const AttnArgs &a, const Row &row, int d, float by,
                                         typename Parts<T>::Op (&q)[Parts<T>::QP]) {
     const T *qp = static_cast<const T *>(a.q) + row.tok * a.ldq + row.head * a.hldq;
-    const int d = 32 * (c >> 1) + 16 * h + 8 * (c & 1);
     T x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = T(0.f);
@@ -269,13 +268,15 @@ __device__ __forceinline__ void load_q1(const AttnArgs &a, const Row &row, int h
         }
     }
 }
+// Operand c of a row: values q_at(c, h) and on.
+__device__ __forceinline__ int q_at(int c, int h) { return 32 * (c >> 1) + 16 * h + 8 * (c & 1); }
 template <typename T, int DB>
 __device__ __forceinline__ void load_q(const AttnArgs &a, const Row &row, int h, float by,
                                        typename Parts<T>::Op (&q)[Parts<T>::QP][2 * DB]) {
 #pragma unroll
     for (int c = 0; c < 2 * DB; ++c) {
         typename Parts<T>::Op x[Parts<T>::QP];
-        load_q1<T>(a, row, h, c, by, x);
+        load_q1<T>(a, row, q_at(c, h), by, x);
 #pragma unroll
         for (int p = 0; p < Parts<T>::QP; ++p) q[p][c] = x[p];
     }
@@ -683,6 +684,55 @@ struct Direct {
 template <typename T, int DB>
 constexpr int waves_of = DB <= 4 && !std::is_same_v<T, float> ? 2 : 1;
 
+// The sums of four waves that share rows, JOIN rows at a time: put(r0) writes those from row r0 on, and all
+// threads join four values each, a wave's after another's.
+template <typename T, int JOIN, int LINE, int ROWS, typename Put>
+__device__ __forceinline__ void join_waves(const AttnArgs &a, const Work &w, const float (&sums)[4][JOIN][LINE],
+                                           const float2 (&ml)[4][ROWS], int rows, Put put) {
+#pragma unroll 1
+    for (int r0 = 0; r0 < rows; r0 += JOIN) {
+        if (r0 > 0) __syncthreads();
+        put(r0);
+        __syncthreads();
+        const int line = a.c.dim / 4, n = min(JOIN, rows - r0) * line;
+        for (int x = threadIdx.x; x < n; x += 256) {
+            const int r = fdiv(x, a.f_dim4), d = 4 * (x - r * line);
+            const Row out = find_row(a, w, w.row0 + r0 + r);
+            float m = -INFINITY, l = 0.f;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) m = fmaxf(m, ml[y][r0 + r].x);
+            floatx4 sum = {};
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const float2 of = ml[y][r0 + r];
+                const float by = of.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of.x - m);
+                l += of.y * by;
+                sum += by * *reinterpret_cast<const floatx4 *>(&sums[y][r][d]);
+            }
+            const int64_t at = int64_t(out.tok) * a.heads + out.head;
+            if (a.splits > 1) {
+                const int64_t p = int64_t(w.split) * a.n.tokens * a.heads + at;
+                if (d == 0) a.ml[p] = make_float2(m, l);
+                *reinterpret_cast<floatx4 *>(a.part + p * a.c.dim + d) = sum;
+                continue;
+            }
+            const float by = l == 0.f ? 0.f : 1.f / l;
+            if (a.lse && d == 0) a.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+            T y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = T(l == 0.f ? 0.f : sum[e] * by);
+            T *to = static_cast<T *>(a.out) + out.tok * a.ldo + out.head * a.hldo + d;
+            if (a.vec_o) {
+                typedef int intv __attribute__((ext_vector_type(sizeof(T))));
+                *reinterpret_cast<intv *>(to) = *reinterpret_cast<const intv *>(y);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) to[e] = y[e];
+            }
+        }
+    }
+}
+
 // Tiles of keys that a wave of attn8_share has in registers.
 template <typename T, int DB>
 constexpr int share_tiles = DB == 8 ? 2 : 3;
@@ -712,7 +762,7 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a
     for (int y = 0; y < DB / 2; ++y) {
         typename Parts<T>::Op x[Parts<T>::QP];
         const int c = wave * (DB / 2) + y;
-        load_q1<T>(a, row, h, c, 1.f, x);
+        load_q1<T>(a, row, q_at(c, h), 1.f, x);
 #pragma unroll
         for (int p = 0; p < Parts<T>::QP; ++p) qs[p][c][lane] = __builtin_bit_cast(intx4, x[p]);
     }
@@ -728,11 +778,7 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a
     }
     s.l += other_half(s.l);
     if (h == 0) ml[wave][i] = make_float2(s.m, s.l);
-    const AttnArgs al = late_args();
-    const int rows = min(32, w.rows - w.row0);
-#pragma unroll 1
-    for (int r0 = 0; r0 < rows; r0 += kJoin) {
-        if (r0 > 0) __syncthreads();
+    join_waves<T, kJoin, kLine>(late_args(), w, sums, ml, min(32, w.rows - w.row0), [&](int r0) {
         if (i >= r0 && i < r0 + kJoin) {
             float *to = sums[wave][i - r0];
 #pragma unroll
@@ -741,44 +787,7 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a
                 for (int blk = 0; blk < DB; blk += 2)
                     *reinterpret_cast<floatx2 *>(to + DB * key_of(r, h) + blk) = floatx2{s.o[blk][r], s.o[blk + 1][r]};
         }
-        __syncthreads();
-        const int line = al.c.dim / 4, n = min(kJoin, rows - r0) * line;
-        for (int x = threadIdx.x; x < n; x += 256) {
-            const int r = fdiv(x, al.f_dim4), d = 4 * (x - r * line);
-            const Row out = find_row(al, w, w.row0 + r0 + r);
-            float m = -INFINITY, l = 0.f;
-#pragma unroll
-            for (int y = 0; y < 4; ++y) m = fmaxf(m, ml[y][r0 + r].x);
-            floatx4 sum = {};
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                const float2 of = ml[y][r0 + r];
-                const float by = of.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of.x - m);
-                l += of.y * by;
-                sum += by * *reinterpret_cast<const floatx4 *>(&sums[y][r][d]);
-            }
-            const int64_t at = int64_t(out.tok) * al.heads + out.head;
-            if (al.splits > 1) {
-                const int64_t p = int64_t(w.split) * al.n.tokens * al.heads + at;
-                if (d == 0) al.ml[p] = make_float2(m, l);
-                *reinterpret_cast<floatx4 *>(al.part + p * al.c.dim + d) = sum;
-                continue;
-            }
-            const float by = l == 0.f ? 0.f : 1.f / l;
-            if (al.lse && d == 0) al.lse[at] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-            T y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = T(l == 0.f ? 0.f : sum[e] * by);
-            T *to = static_cast<T *>(al.out) + out.tok * al.ldo + out.head * al.hldo + d;
-            if (al.vec_o) {
-                typedef int intv __attribute__((ext_vector_type(sizeof(T))));
-                *reinterpret_cast<intv *>(to) = *reinterpret_cast<const intv *>(y);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) to[e] = y[e];
-            }
-        }
-    }
+    });
 }
 
 // Each wave has rows of its own and reads keys by itself.
@@ -803,6 +812,289 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_own(AttnArgs a) 
     if (!fine) slow_sums<T, FMT, DB, HeldQ<T, DB>>(late_args(), w, row, q, h, from, until, s);
     s.l += other_half(s.l);
     finish<T, DB>(late_args(), w, row, s, h);
+}
+
+// ---- up to 16 rows -------------------------------------------------------------------------------
+
+// The same on 16x16x32 instructions: half of the weights, and of the sums' registers.  Lane (i, g), i = lane % 16,
+// g = lane / 16, has S of row i and keys 4 g .. 4 g + 3 of each 16, and as the second operand of the second product
+// P of row i and those eight keys.  Both operands of the first product take values 64 c + 16 g + 8 u and on.
+__device__ __forceinline__ floatx4 mma16(bf16x8 a, bf16x8 b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx4 mma16(f16x8 a, f16x8 b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+// Over the four lanes of a row.
+template <typename Fn>
+__device__ __forceinline__ float over_groups(float v, Fn fn) {
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fn(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fn(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+template <typename T, int FMT, bool POW2, int DB>
+struct Few {
+    using P = Parts<T>;
+    using Op = typename P::Op;
+    static constexpr bool kFoldK = POW2 && std::is_same_v<Op, bf16x8>;
+    static constexpr int NB = 2 * DB;                              // blocks of 16 values, a lane's bytes of a key of V
+    static constexpr int W = NB / 4;
+
+    struct Tile {
+        intx4 k[2][DB / 2];
+        unsigned v[8][W];                 // keys 4 g + e of the first 16, then of the second
+        unsigned s;                       // the scale as stored of key lane % 32: K's in lanes 0 to 31, V's in the others
+        int valid[2];
+    };
+    struct Pages {
+        PageRef p[2];
+    };
+
+    const AttnArgs &a;
+    const Work &w;
+    const Row &row;
+    const float c;                        // what sums are multiplied with (powers of two in K's operands)
+    const int lane, i, g;
+    const unsigned koff, voff;
+    const int32_t *table;
+    Op q[P::QP][DB];
+    floatx4 o[NB];
+    float m, l;                           // l: of the lane's keys
+
+    __device__ __forceinline__ Few(const AttnArgs &a_, const Work &w_, const Row &r_)
+        : a(a_), w(w_), row(r_), c(a_.scale == 0.f ? 1.f : fabsf(a_.scale)), lane(threadIdx.x & 63), i(lane & 15),
+          g(lane >> 4), koff(i * a_.c.dim), voff(4 * g * a_.c.dim + min(NB * i, a_.c.dim - NB)),
+          table(a_.n.table + int64_t(w_.b) * a_.n.tld) {
+        const float sign = a.scale < 0.f ? -1.f : a.scale > 0.f ? 1.f : 0.f;
+#pragma unroll
+        for (int x = 0; x < DB; ++x) {
+            Op part[P::QP];
+            load_q1<T>(a, row, 64 * (x >> 1) + 16 * g + 8 * (x & 1), kFoldK ? sign : 1.f, part);
+#pragma unroll
+            for (int p = 0; p < P::QP; ++p) q[p][x] = part[p];
+        }
+        m = -INFINITY;
+        l = 0.f;
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) o[blk] = floatx4{};
+    }
+
+    __device__ __forceinline__ Pages pages(int key0) const {
+        return {page_ref(a, table, w.len, key0), page_ref(a, table, w.len, key0 + 16)};
+    }
+
+    __device__ __forceinline__ void load(Tile &t, const Pages &from, int key0) const {
+        const int dim = a.c.dim;
+        int64_t se[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int id = page_of(a, from.p[b]);
+            t.valid[b] = id >= 0 ? min(16, max(w.len - key0 - 16 * b, 0)) : 0;
+            const int64_t page = max(id, 0), at = w.head * a.c.page + from.p[b].off;
+            const uint8_t *k = a.c.k + page * a.c.stride + at * dim, *v = a.c.v + page * a.c.stride + at * dim;
+#pragma unroll
+            for (int x = 0; x < DB / 2; ++x)
+                t.k[b][x] = *reinterpret_cast<const intx4 *>(k + koff + min(64 * x + 16 * g, dim - 16));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint8_t *vp = v + e * dim + voff;
+                if constexpr (W == 1) {
+                    t.v[4 * b + e][0] = *reinterpret_cast<const unsigned *>(vp);
+                } else {
+                    typedef int intw __attribute__((ext_vector_type(W)));
+                    const intw x = *reinterpret_cast<const intw *>(vp);
+#pragma unroll
+                    for (int word = 0; word < W; ++word) t.v[4 * b + e][word] = x[word];
+                }
+            }
+            se[b] = page * a.c.sstride + at;
+        }
+        t.s = load_scale(lane < 32 ? a.c.ks : a.c.vs, POW2 ? DS_SCALE_POW2 : DS_SCALE_F32, (lane & 16 ? se[1] : se[0]) + i);
+    }
+
+    __device__ __forceinline__ void follow(float top) {
+        if (__any(top > m + kLoose || (m == -INFINITY && top > -INFINITY))) {
+            const float now = fmaxf(m, top);
+            const float by = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - now);
+            m = now;
+            l *= by;
+#pragma unroll
+            for (int blk = 0; blk < NB; ++blk) o[blk] *= by;
+        }
+    }
+    __device__ __forceinline__ float largest(const float (&x)[8]) const {
+        const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        return over_groups(top, [](float y, float z) { return fmaxf(y, z); }) * (kFoldK ? c : 1.f);
+    }
+
+    // One tile of 32 keys; edge: some row does not see some key of it, or some key does not exist.  False where that
+    // needs slow_sums.  begun: all rows have a maximum.
+    __device__ __forceinline__ bool step(Tile &t, int key0, bool edge, bool &begun, float *lds) {
+        float sc = scale_of(t.s, POW2 ? DS_SCALE_POW2 : DS_SCALE_F32);
+        if (edge) sc = i < (lane & 16 ? t.valid[1] : t.valid[0]) ? sc : 0.f;
+        lds[lane] = kFoldK || lane >= 32 ? sc : sc * a.scale;
+        __builtin_amdgcn_wave_barrier();
+        if (a.c.dim < 32 * DB)                // (a number that is none times Q's 0 is no 0)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int x = 0; x < DB / 2; ++x)
+                    if (64 * x + 16 * g >= a.c.dim) t.k[b][x] = intx4{};
+        floatx4 sum[2] = {};
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const float by = kFoldK ? lds[16 * b + i] : 1.f;
+#pragma unroll
+            for (int x = 0; x < DB; ++x) {
+                const Op k = decode_k<FMT, Op>(t.k[b][x >> 1][2 * (x & 1)], t.k[b][x >> 1][2 * (x & 1) + 1], by);
+#pragma unroll
+                for (int p = P::QP - 1; p >= 0; --p) sum[b] = mma16(k, q[p][x], sum[b]);
+            }
+        }
+        float x[8];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            floatx4 sk;
+            if constexpr (!kFoldK) sk = *reinterpret_cast<const floatx4 *>(lds + 16 * b + 4 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[4 * b + r] = kFoldK ? sum[b][r] : sum[b][r] * sk[r];
+        }
+        if (edge) {
+            int low = row.low - key0 - 4 * g, lim = row.lim - key0 - 4 * g, has[2] = {t.valid[0] - 4 * g, t.valid[1] - 4 * g};
+            __asm__ volatile("" : "+v"(low), "+v"(lim), "+v"(has[0]), "+v"(has[1]));
+            unsigned bad = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int k = 16 * (e >> 2) + (e & 3);
+                x[e] = k >= low && k < lim && (e & 3) < has[e >> 2] ? x[e] : -INFINITY;
+#pragma unroll
+                for (int word = 0; word < W; ++word) {
+                    if ((e & 3) >= has[e >> 2]) t.v[e][word] = 0;
+                    bad |= not_finite<FMT>(t.v[e][word]);
+                }
+            }
+            if (__any(bad != 0)) return false;
+        }
+        if (edge || !begun) {
+            follow(largest(x));
+            begun = __all(m > -INFINITY);
+        }
+        const floatx4 sv[2] = {*reinterpret_cast<const floatx4 *>(lds + 32 + 4 * g),
+                               *reinterpret_cast<const floatx4 *>(lds + 48 + 4 * g)};
+        __builtin_amdgcn_wave_barrier();
+        bf16x8 pt[P::PP];
+        float part = 0.f;
+        const auto weigh = [&]() {
+            const float off = m == -INFINITY ? 0.f : m;
+            part = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[e], c, -off) : x[e] - off);
+                part += p;
+                put_weight<P::PP>(pt, e, p * sv[e >> 2][e & 3]);
+            }
+        };
+        weigh();
+        // (see Tiles::weights)
+        if (__any(part >= float(1 << int(kLoose)))) {
+            follow(largest(x));
+            weigh();
+        }
+        l += part;
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk) {
+            const int word = blk >> 2, j = blk & 3;
+            bf16x8 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned pair = __builtin_amdgcn_perm(t.v[2 * e + 1][word], t.v[2 * e][word], j & 2 ? 0x07030602u : 0x05010400u);
+                const bf16x2 y = j & 1 ? decode2<FMT, true>(pair, 1.f) : decode2<FMT, false>(pair, 1.f);
+                v[2 * e] = y[0];
+                v[2 * e + 1] = y[1];
+            }
+#pragma unroll
+            for (int p = P::PP - 1; p >= 0; --p) o[blk] = mma16(v, pt[p], o[blk]);
+        }
+        return true;
+    }
+
+    template <int STEP>
+    __device__ __forceinline__ bool walk(int key, int until, int every, int since, float *lds) {
+        bool fine = true, begun = false;
+        const auto edge = [&](const Tile &t) {
+            return key + kKeys > every || key < since || (t.valid[0] & t.valid[1]) != 16;
+        };
+        if (key >= until) return true;
+        Tile t[2];
+        load(t[0], pages(key), key);
+        Pages next = pages(key + STEP);
+        while (true) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const Pages after = pages(key + 2 * STEP);
+                if (key + STEP < until) load(t[x ^ 1], next, key + STEP);
+                next = after;
+                fine = step(t[x], key, edge(t[x]), begun, lds);
+                key += STEP;
+                if (!fine || key >= until) return fine;
+            }
+        }
+    }
+};
+
+template <typename T, int DB>
+constexpr int few_waves_of = DB == 8 ? 1 : DB == 4 || std::is_same_v<T, float> ? 2 : 4;
+
+// As attn8_share, for up to 16 rows.
+template <typename T, int FMT, bool POW2, int DB>
+__global__ __launch_bounds__(256, (few_waves_of<T, DB>)) void attn8_few(AttnArgs a) {
+    constexpr int kJoin = DB == 8 ? 8 : 16, kLine = 32 * DB + 4;      // rows at a time, floats between them
+    __shared__ __attribute__((aligned(16))) float scales[4 * 64];
+    __shared__ __attribute__((aligned(16))) float sums[4][kJoin][kLine];
+    __shared__ float2 ml[4][16];
+    Work w;
+    if (!find_work<16>(a, w)) return;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Row row = find_row(a, w, w.row0 + (lane & 15));
+    int from, until;
+    w.keys(a, w.row0 + 15, from, until);
+    if (a.splits > 1 && from >= until) {   // a split past the sequence's end
+        if (wave == 0 && lane < 16 && row.is)
+            a.ml[(int64_t(w.split) * a.n.tokens + row.tok) * a.heads + row.head] = make_float2(-INFINITY, 0.f);
+        return;
+    }
+    Few<T, FMT, POW2, DB> s(a, w, row);
+    const bool fine = s.template walk<4 * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
+                                                 w.low(a, w.token(a, w.row0 + 15)), scales + wave * 64);
+    const AttnArgs al = late_args();
+    if (__syncthreads_or(!fine)) {        // then the first wave takes all keys, in the other form's order
+        if (wave > 0) return;
+        row = find_row(al, w, w.row0 + (lane & 31));
+        row.is = row.is && (lane & 31) < 16;
+        HeldQ<T, DB> held;
+        load_q<T, DB>(al, row, lane >> 5, 1.f, held.q);
+        Sums<DB> all;
+        slow_sums<T, FMT, DB, HeldQ<T, DB>>(al, w, row, held, lane >> 5, from, until, all);
+        all.l += other_half(all.l);
+        finish<T, DB>(al, w, row, all, lane >> 5);
+        return;
+    }
+    s.l = over_groups(s.l, [](float x, float y) { return x + y; });
+    if (lane < 16) ml[wave][lane] = make_float2(s.m, s.l);
+    join_waves<T, kJoin, kLine>(al, w, sums, ml, min(16, w.rows - w.row0), [&](int r0) {
+        if (s.i >= r0 && s.i < r0 + kJoin) {
+            float *to = sums[wave][s.i - r0];
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int blk = 0; blk < 2 * DB; blk += 4)
+                    *reinterpret_cast<floatx4 *>(to + 2 * DB * (4 * s.g + r) + blk) =
+                        floatx4{s.o[blk][r], s.o[blk + 1][r], s.o[blk + 2][r], s.o[blk + 3][r]};
+        }
+    });
 }
 
 // ---- keys and values decoded in LDS ---------------------------------------------------------------------
@@ -1206,7 +1498,10 @@ AttnKernel attn8_kernel(int form, int fmt, int stype, int dim) {
     AttnKernel k{nullptr, 0};
     const auto of_dim = [&](auto f, auto db) {
         constexpr int FMT = f.value, DB = db.value;
-        if (form == kAttnShare) {
+        if (form == kAttnFew) {
+            k.func = stype == DS_SCALE_POW2 ? reinterpret_cast<const void *>(&attn8_few<T, FMT, true, DB>)
+                                            : reinterpret_cast<const void *>(&attn8_few<T, FMT, false, DB>);
+        } else if (form == kAttnShare) {
             k.func = reinterpret_cast<const void *>(&attn8_share<T, FMT, DB>);
         } else if (form == kAttnOwn) {
             if constexpr (attn8_own_form<T>(DB)) k.func = reinterpret_cast<const void *>(&attn8_own<T, FMT, DB>);

@@ -116,14 +116,14 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
     const int64_t group = q->heads / cache->heads, rows = q->tokens * group;
     const int db = attn8_dim_blocks(cache->dim);
     const bool own = q->type == DS_TYPE_F32 ? attn8_own_form<float>(db) : attn8_own_form<__bf16>(db);
-    p.form = rows <= 64 * chunk->seqs ? kAttnShare : own ? kAttnOwn : kAttnTiles;
+    p.form = rows <= 16 * chunk->seqs ? kAttnFew : rows <= 64 * chunk->seqs ? kAttnShare : own ? kAttnOwn : kAttnTiles;
     const int tile = attn8_rows(p.form);
     const int64_t base = (rows / tile + chunk->seqs) * cache->heads;
     int64_t keys = most_keys(cache, chunk, cfg);
     if (cfg->window > 0) keys = std::min(keys, cfg->window + tile / group + 1 + 64);
     // The split that ends first: rounds of workgroups that the chip holds, each as long as its keys and what a
     // workgroup needs beside them.
-    const int64_t unit = p.form == kAttnShare ? 128 : 64, slots = p.form == kAttnTiles ? 256 : 512, beside = 4 * unit;
+    const int64_t unit = p.form == kAttnFew || p.form == kAttnShare ? 128 : 64, slots = p.form == kAttnTiles ? 256 : 512, beside = 4 * unit;
     const int64_t work = std::max((rows + tile - 1) / tile, std::min(q->tokens, chunk->seqs)) * cache->heads;
     int64_t best = INT64_MAX;
     for (const int64_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
