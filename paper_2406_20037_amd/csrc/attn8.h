@@ -38,6 +38,12 @@ constexpr bool attn8_own_form(int dim_blocks) {
     return sizeof(T) == 4 || dim_blocks == 8;
 }
 
+// Workgroups that a compute unit holds: by their registers.
+constexpr int attn8_groups(int form, bool f32, int dim_blocks) {
+    if (form == kAttnFew) return dim_blocks == 8 ? 1 : dim_blocks == 4 || f32 ? 2 : 4;
+    return form == kAttnTiles || dim_blocks == 8 || f32 ? 1 : 2;
+}
+
 struct AttnKernel {
     const void *func;
     int lds;                              // bytes of dynamic LDS

@@ -680,10 +680,6 @@ struct Direct {
     }
 };
 
-// Waves of a SIMD unit: two where their registers allow it.
-template <typename T, int DB>
-constexpr int waves_of = DB <= 4 && !std::is_same_v<T, float> ? 2 : 1;
-
 // The sums of four waves that share rows, JOIN rows at a time: put(r0) writes those from row r0 on, and all
 // threads join four values each, a wave's after another's.
 template <typename T, int JOIN, int LINE, int ROWS, typename Put>
@@ -740,7 +736,7 @@ constexpr int share_tiles = DB == 8 ? 2 : 3;
 // Four waves share 32 rows and take tiles of keys in turn.  Their sums meet in LDS, some rows at a time, and
 // all threads join four values each.
 template <typename T, int FMT, int DB>
-__global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a) {
+__global__ __launch_bounds__(256, (attn8_groups(kAttnShare, sizeof(T) == 4, DB))) void attn8_share(AttnArgs a) {
     constexpr int kJoin = DB == 8 ? 8 : 16, kLine = 32 * DB + 4;      // rows at a time, floats between them
     __shared__ __attribute__((aligned(16))) float scales[4 * 64];
     __shared__ __attribute__((aligned(16))) float sums[4][kJoin][kLine];
@@ -792,7 +788,7 @@ __global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_share(AttnArgs a
 
 // Each wave has rows of its own and reads keys by itself.
 template <typename T, int FMT, int DB>
-__global__ __launch_bounds__(256, (waves_of<T, DB>)) void attn8_own(AttnArgs a) {
+__global__ __launch_bounds__(256, (attn8_groups(kAttnOwn, sizeof(T) == 4, DB))) void attn8_own(AttnArgs a) {
     __shared__ __attribute__((aligned(16))) float scales[4 * 64];
     Work w;
     if (!find_work<128>(a, w)) return;
@@ -1044,12 +1040,9 @@ struct Few {
     }
 };
 
-template <typename T, int DB>
-constexpr int few_waves_of = DB == 8 ? 1 : DB == 4 || std::is_same_v<T, float> ? 2 : 4;
-
 // As attn8_share, for up to 16 rows.
 template <typename T, int FMT, bool POW2, int DB>
-__global__ __launch_bounds__(256, (few_waves_of<T, DB>)) void attn8_few(AttnArgs a) {
+__global__ __launch_bounds__(256, (attn8_groups(kAttnFew, sizeof(T) == 4, DB))) void attn8_few(AttnArgs a) {
     constexpr int kJoin = DB == 8 ? 8 : 16, kLine = 32 * DB + 4;      // rows at a time, floats between them
     __shared__ __attribute__((aligned(16))) float scales[4 * 64];
     __shared__ __attribute__((aligned(16))) float sums[4][kJoin][kLine];

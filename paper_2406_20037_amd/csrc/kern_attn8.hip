@@ -122,8 +122,11 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
     int64_t keys = most_keys(cache, chunk, cfg);
     if (cfg->window > 0) keys = std::min(keys, cfg->window + tile / group + 1 + 64);
     // The split that ends first: rounds of workgroups that the chip holds, each as long as its keys and what a
-    // workgroup needs beside them.
-    const int64_t unit = p.form == kAttnFew || p.form == kAttnShare ? 128 : 64, slots = p.form == kAttnTiles ? 256 : 512, beside = 4 * unit;
+    // workgroup needs beside them (64 equal sequences of 8192 keys: 261 us whole, 194 to 202 in two or four
+    // parts; of unequal lengths 127 whole and 136 to 149 so: full rounds of whole sequences stay whole).
+    const bool shares = p.form == kAttnFew || p.form == kAttnShare;
+    const int64_t unit = shares ? 128 : 64, beside = 4 * unit;
+    const int64_t slots = 256 * attn8_groups(p.form, q->type == DS_TYPE_F32, db);
     const int64_t work = std::max((rows + tile - 1) / tile, std::min(q->tokens, chunk->seqs)) * cache->heads;
     int64_t best = INT64_MAX;
     for (const int64_t splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
