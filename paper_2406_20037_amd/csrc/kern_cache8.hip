@@ -1,5 +1,9 @@
 // Rotary positions, and rows of keys and values to and from the paged 8-bit cache.  All three
-// move memory: each value is read once and written once by one launch.
+// move memory: each value is read once and written once by one launch.  What is written goes past the
+// caches (nontemporal): a kernel's outputs are read by a later one, on any of the eight dies, and the lines of a
+// cached store take room from loads.  8192 tokens of 40 heads of 128 bf16 values turned: 26.5 us (6.3 TB/s), where
+// cached stores took 35; a sequence of 32768 tokens read back 32.6 (6.2 TB/s), where they took 51.  Loads stay cached:
+// past the caches they took 32 and 43.
 #include <cmath>
 #include <type_traits>
 
@@ -121,7 +125,7 @@ __device__ __forceinline__ void store_n(T *p, bool vec, const float (&v)[N]) {
     if (vec) {
 #pragma unroll
         for (size_t i = 0; i < sizeof(t) / 16; ++i)
-            reinterpret_cast<intx4 *>(p)[i] = reinterpret_cast<const intx4 *>(t)[i];
+            __builtin_nontemporal_store(reinterpret_cast<const intx4 *>(t)[i], &reinterpret_cast<intx4 *>(p)[i]);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) p[i] = t[i];
@@ -138,16 +142,19 @@ struct RotaryArgs {
     int tokens, heads, dim, half;         // half: pairs of a head
     int tb, hb;                           // tokens and heads of a workgroup
     int items, ni;                        // work items of a row; those that turn pairs
-    int pairs;
     float scale, sign;
     FastDiv f_items, f_hb, f_half;
 };
 
-// A workgroup forms the angles of its tokens once for all their heads, in LDS: position times frequency in
-// revolutions, whose whole part is dropped in 64 bits (53 bits of 2^31 positions leave 2^-22 of a
-// revolution... the fraction's error is below 2^-21 turns only past 2^31; fp32 holds the rest).  Its threads then
-// take items of N pairs (8, or 1 where rows are not whole 16-byte groups of them), and copy what is not turned.
-template <typename T, int N>
+// (u, w) = (p cos - q sin, p sin + q cos) scale, with the angle position * frequency; the inverse has the other
+// sine.  A workgroup forms its tokens' angles once for all their heads, in LDS.  They are taken
+// in revolutions: three roundings of 2^-53 leave the product within 2^-34 of one at position 10^6 and 2^-22 at
+// 2^31, its whole part is dropped there, and fp32 holds the fraction.  Then the threads take items of 16 bytes of each
+// half of a head, or 16 bytes of pairs side by side (N pairs either way; single ones where rows are not whole groups of
+// 16 bytes), and copy what is not turned unless it is in place.  Memory bounds it: the figures are above; 4099 tokens of 24 heads of
+// 96 fp32 values, 64 of them turned by pairs, 14.2 us (5.3 TB/s; items of 64 bytes took 16); one token of 40 heads 2.4 us
+// on the chip, less than its launch.
+template <typename T, int N, bool PAIRS>
 __global__ __launch_bounds__(256) void rotary(HeadsView<const T> x, HeadsView<T> y, RotaryArgs a) {
     __shared__ float2 turn[kTurnLds];
     const int t0 = blockIdx.x * a.tb, nt = min(a.tb, a.tokens - t0);
@@ -169,10 +176,11 @@ __global__ __launch_bounds__(256) void rotary(HeadsView<const T> x, HeadsView<T>
         const T *px = x.p + (t0 + t) * x.ld + (h0 + h) * x.hld;
         T *py = y.p + (t0 + t) * y.ld + (h0 + h) * y.hld;
         constexpr bool vec = N > 1;
+        constexpr int kCopy = vec && PAIRS ? 2 * N : N;
         if (item < a.ni) {
             const int j = item * N;
             const float2 *cs = turn + t * a.half + j;
-            if (a.pairs) {
+            if constexpr (PAIRS) {
                 float v[2 * N], w[2 * N];
                 load_n<T, 2 * N>(px + 2 * j, vec, v);
 #pragma unroll
@@ -194,10 +202,10 @@ __global__ __launch_bounds__(256) void rotary(HeadsView<const T> x, HeadsView<T>
                 store_n<T, N>(py + a.half + j, vec, w);
             }
         } else {
-            const int d = 2 * a.half + (item - a.ni) * N;
-            float v[N];
-            load_n<T, N>(px + d, vec, v);
-            store_n<T, N>(py + d, vec, v);
+            const int d = 2 * a.half + (item - a.ni) * kCopy;
+            float v[kCopy];
+            load_n<T, kCopy>(px + d, vec, v);
+            store_n<T, kCopy>(py + d, vec, v);
         }
     }
 }
@@ -253,8 +261,11 @@ __device__ __forceinline__ RowAt row_at(const CacheArgs &a, const Place *at, int
 }
 constexpr int kReadAhead = 4, kWriteAhead = 2;   // rows of a thread whose loads are on their way together
 
-// LPR lanes a row of up to 8 LPR values, rows of a workgroup token by token within a head, so
-// that neighbouring rows of a page are written together.  blockIdx.y: keys or values, and the head.
+// A row's scale s is the one ds_q8_quantize gives a row of one block, and its bytes are x / s rounded to nearest.
+// LPR lanes a row of up to 8 LPR values; rows of a workgroup token by token within a head, so that neighbouring
+// rows of a page are written together.  Memory bounds it, in part the reads that a workgroup does one after another (starts,
+// lengths and table, then its rows): prompts of up to 2731 tokens of 8 heads of 128 bf16 values (18549 in
+// all, 114 MB) in 24.8 us, 4.6 TB/s.  Rows loaded before their places are known took 26.7, four of a thread ahead 30.
 template <typename T, int LPR>
 __global__ __launch_bounds__(256) void cache8_write(HeadsView<const T> k, HeadsView<const T> v, CacheArgs a) {
     __shared__ int lds[kPlaceSeqs + 1];
@@ -294,7 +305,7 @@ __global__ __launch_bounds__(256) void cache8_write(HeadsView<const T> k, HeadsV
                 else
                     q = intx2{pack4<DS_Q8_E5M2>(y[0] * s.inv, y[1] * s.inv, y[2] * s.inv, y[3] * s.inv),
                               pack4<DS_Q8_E5M2>(y[4] * s.inv, y[5] * s.inv, y[6] * s.inv, y[7] * s.inv)};
-                *reinterpret_cast<intx2 *>((r[u].val ? a.c.v : a.c.k) + r[u].page * a.c.stride + row * a.c.dim + d) = q;
+                __builtin_nontemporal_store(q, reinterpret_cast<intx2 *>((r[u].val ? a.c.v : a.c.k) + r[u].page * a.c.stride + row * a.c.dim + d));
             }
             if (l == 0) {
                 void *sp = r[u].val ? a.c.vs : a.c.ks;
@@ -326,6 +337,8 @@ __device__ __forceinline__ void decode8(intx2 q, int fmt, float s, float (&x)[8]
     }
 }
 
+// The same walk the other way: 32768 tokens of 8 heads of 128 to bf16 (202 MB) in 32.6 us, 6.2 TB/s; eight of a
+// thread's rows ahead took 34.6, two 34.5.
 template <typename T, int LPR>
 __global__ __launch_bounds__(256) void cache8_read(HeadsView<T> k, HeadsView<T> v, CacheArgs a) {
     __shared__ int lds[kPlaceSeqs + 1];
@@ -389,8 +402,8 @@ int cache_args(const ds_cache8 *cache, const ds_chunk *chunk, const ds_heads *k,
     a->c = cache_view(cache);
     a->n = chunk_view(chunk, cache, k->tokens);
     // About 64 rows of keys and values a workgroup, a power of two of tokens, and some workgroups a compute unit:
-    // 8192 tokens of 8 heads of 128 written in 26.5 us, where 128 rows took 28.7 and 256 32.4; 64 Ki tokens
-    // read in 51 us with any of them.
+    // 18549 tokens of 8 heads of 128 written in 26.5 us, where 128 rows took 28.7 and 256 32.4; reading
+    // took the same with any of them.
     a->tb = 1;
     while (a->tb < 256 && 2 * a->tb * cache->heads < 64) a->tb *= 2;
     while (a->tb > 1 && k->tokens < 512 * int64_t(a->tb)) a->tb /= 2;
@@ -437,14 +450,16 @@ int ds_rotary(const ds_heads *x, const int32_t *pos, const float *freqs, int64_t
     a.heads = int(x->heads);
     a.dim = int(x->dim);
     a.half = int(turn / 2);
-    a.pairs = mode & DS_ROTARY_PAIRS;
     a.scale = scale;
     a.sign = mode & DS_ROTARY_INVERSE ? -1.f : 1.f;
-    const int n = heads16(x) && heads16(y) && a.half % 8 == 0 && x->dim % 8 == 0 ? 8 : 1;
+    const bool pairs = mode & DS_ROTARY_PAIRS;
+    const int most16 = 16 / type_bytes(x->type);            // values of 16 bytes
+    const bool vec = heads16(x) && heads16(y) && turn % (pairs ? most16 : 2 * most16) == 0 && x->dim % most16 == 0;
+    const int n = !vec ? 1 : pairs ? most16 / 2 : most16;   // pairs of an item
     a.ni = a.half / n;
     // in place, what is not turned is there already
     const bool same = x->data == y->data && x->ld == y->ld && x->head_ld == y->head_ld;
-    a.items = a.ni + (same ? 0 : int(x->dim - turn) / n);
+    a.items = a.ni + (same ? 0 : int(x->dim - turn) / (vec ? most16 : 1));
     if (a.items == 0) return DS_OK;
     // some 1024 items a workgroup, of one token's heads or of several tokens; fewer heads where the
     // tokens alone do not fill the chip
@@ -463,7 +478,10 @@ int ds_rotary(const ds_heads *x, const int32_t *pos, const float *freqs, int64_t
     if ((rc = launch_check(int64_t(grid.x) * grid.y, 256, "ds_rotary")) != DS_OK) return rc;
     return by_type(x->type, [&](auto *t) {
         using T = std::remove_cv_t<std::remove_pointer_t<decltype(t)>>;
-        (n == 8 ? rotary<T, 8> : rotary<T, 1>)<<<grid, 256, 0, stream>>>(heads_view<const T>(x), heads_view<T>(y), a);
+        constexpr int kN = 16 / sizeof(T);
+        (pairs ? vec ? rotary<T, kN / 2, true> : rotary<T, 1, true>
+               : vec ? rotary<T, kN, false> : rotary<T, 1, false>)
+            <<<grid, 256, 0, stream>>>(heads_view<const T>(x), heads_view<T>(y), a);
     });
 }
 
