@@ -468,14 +468,19 @@ template <int DB>
 __device__ __forceinline__ int v_column(int i, int dim) {
     return min(DB * i, dim - DB);
 }
-template <int DB>
+// (once: rows that no other workgroup reads, past the caches; see Few::load)
+template <int DB, bool ONCE>
 __device__ __forceinline__ void load_v(const uint8_t *p, unsigned at, unsigned (&w)[DB == 8 ? 2 : 1]) {
+    const auto get = [&](const auto *from) {
+        if constexpr (ONCE) return __builtin_nontemporal_load(from);
+        else return *from;
+    };
     if constexpr (DB == 2) {
-        w[0] = *reinterpret_cast<const uint16_t *>(p + at);
+        w[0] = get(reinterpret_cast<const uint16_t *>(p + at));
     } else if constexpr (DB == 4) {
-        w[0] = *reinterpret_cast<const unsigned *>(p + at);
+        w[0] = get(reinterpret_cast<const unsigned *>(p + at));
     } else {
-        const intx2 x = *reinterpret_cast<const intx2 *>(p + at);
+        const intx2 x = get(reinterpret_cast<const intx2 *>(p + at));
         w[0] = x[0];
         w[1] = x[1];
     }
@@ -530,7 +535,7 @@ struct Direct {
         for (int st = 0; st < 2; ++st)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                load_v<DB>(a.c.v + byte[st] + (e < 4 ? e : e + 4) * dim, voff, t.v[st][e]);
+                load_v<DB, std::is_same_v<Q, SharedQ<T, DB>>>(a.c.v + byte[st] + (e < 4 ? e : e + 4) * dim, voff, t.v[st][e]);
         const int64_t se = (up ? page[1] : page[0]) * a.c.sstride + (up ? at[1] : at[0]) + (i & 15);
         t.s = load_scale(h ? a.c.vs : a.c.ks, a.c.stype, se);
     }
@@ -898,14 +903,16 @@ struct Few {
 #pragma unroll
             for (int x = 0; x < DB / 2; ++x)
                 t.k[b][x] = *reinterpret_cast<const intx4 *>(k + koff + min(64 * x + 16 * g, dim - 16));
+            // V's whole lines are read once, and pass the caches by; the halves of K's that two loads share do not (64 sequences
+            // of up to 8192 keys 126.5 -> 120.3 us, K's too 137; of 8192 each 260 -> 241, 245)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint8_t *vp = v + e * dim + voff;
                 if constexpr (W == 1) {
-                    t.v[4 * b + e][0] = *reinterpret_cast<const unsigned *>(vp);
+                    t.v[4 * b + e][0] = __builtin_nontemporal_load(reinterpret_cast<const unsigned *>(vp));
                 } else {
                     typedef int intw __attribute__((ext_vector_type(W)));
-                    const intw x = *reinterpret_cast<const intw *>(vp);
+                    const intw x = __builtin_nontemporal_load(reinterpret_cast<const intw *>(vp));
 #pragma unroll
                     for (int word = 0; word < W; ++word) t.v[4 * b + e][word] = x[word];
                 }
@@ -1182,7 +1189,7 @@ struct Tiles {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 unsigned x[W];
-                load_v<DB>(rows + (e < 4 ? e : e + 4) * dim, to.lane, x);
+                load_v<DB, false>(rows + (e < 4 ? e : e + 4) * dim, to.lane, x);
 #pragma unroll
                 for (int word = 0; word < W; ++word) st.raw[e * W + word] = x[word];
             }
