@@ -27,9 +27,14 @@ struct AttnArgs {
 // Four forms of the kernel (attn8_kernel.h): waves that share 16 or 32 rows and split the keys; waves of 32 rows
 // each that read keys by themselves; waves of 32 rows each that share the keys through LDS.
 enum { kAttnFew, kAttnShare, kAttnOwn, kAttnTiles };
-constexpr int attn8_threads(int form) { return form == kAttnTiles ? 512 : 256; }
-constexpr int attn8_rows(int form) { return form == kAttnFew ? 16 : form == kAttnShare ? 32 : attn8_threads(form) / 2; }
 constexpr int attn8_dim_blocks(int dim) { return dim <= 64 ? 2 : dim <= 128 ? 4 : 8; }
+// (few rows of 65 to 128 values: eight waves of one workgroup in place of four of two; unequal sequences, whose
+// longest one ends last, gain: 64 of up to 8192 keys 122 -> 117 us, 100 of up to 6000 136 -> 122; equal ones
+// of 8192 lose, 167 -> 172)
+constexpr int attn8_threads(int form, int dim_blocks) {
+    return form == kAttnTiles || (form == kAttnFew && dim_blocks == 4) ? 512 : 256;
+}
+constexpr int attn8_rows(int form) { return form == kAttnFew ? 16 : form == kAttnShare ? 32 : form == kAttnTiles ? 256 : 128; }
 
 // Whether the many rows of a type and width take kAttnOwn (else kAttnTiles): where the registers hold no more
 // than one wave a SIMD unit.
@@ -40,7 +45,7 @@ constexpr bool attn8_own_form(int dim_blocks) {
 
 // Workgroups that a compute unit holds: by their registers.
 constexpr int attn8_groups(int form, bool f32, int dim_blocks) {
-    if (form == kAttnFew) return dim_blocks == 8 ? 1 : dim_blocks == 4 || f32 ? 2 : 4;
+    if (form == kAttnFew) return dim_blocks >= 4 ? 1 : f32 ? 2 : 4;
     return form == kAttnTiles || dim_blocks == 8 || f32 ? 1 : 2;
 }
 

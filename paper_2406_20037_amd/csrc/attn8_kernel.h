@@ -197,10 +197,20 @@ struct Work {
 template <int ROWS>
 __device__ __forceinline__ bool find_work(const AttnArgs &a, Work &w) {
     const int lane = threadIdx.x & 63;
-    // heads side by side: workgroups go to the chip's eight parts in turn, so the workgroups of a head
-    // share the caches of as few parts as the number of heads allows
-    const int idx = fdiv(blockIdx.x, a.f_kv);
-    w.head = int(blockIdx.x) - idx * a.c.heads;
+    // Workgroups go to the chip's eight parts in turn.  Heads side by side: the workgroups of a head share the caches
+    // of as few parts as the number of heads allows.  Of few rows none share keys, and a part takes four heads of the
+    // same pages: that lets memory stream (64 sequences of 8192 keys each 242 -> 166 us, 6.5 TB/s; two heads
+    // 244, eight 166, but 100 unequal sequences 145, where one to four take 135).
+    int idx;
+    const int whole = int(gridDim.x) / (8 * a.c.heads) * (8 * a.c.heads);
+    if (ROWS == 16 && a.c.heads % 4 == 0 && int(blockIdx.x) < whole) {
+        const int four = int(blockIdx.x >> 5) * 8 + int(blockIdx.x & 7);       // of the fours of heads
+        idx = fdiv(4 * four, a.f_kv);
+        w.head = 4 * four - idx * a.c.heads + int(blockIdx.x >> 3 & 3);
+    } else {
+        idx = fdiv(blockIdx.x, a.f_kv);
+        w.head = int(blockIdx.x) - idx * a.c.heads;
+    }
     const int tile = fdiv(idx, a.f_splits);
     w.split = idx - tile * a.splits;
     int b = 0;
@@ -685,26 +695,26 @@ struct Direct {
     }
 };
 
-// The sums of four waves that share rows, JOIN rows at a time: put(r0) writes those from row r0 on, and all
+// The sums of waves that share rows, JOIN rows at a time: put(r0) writes those from row r0 on, and all
 // threads join four values each, a wave's after another's.
-template <typename T, int JOIN, int LINE, int ROWS, typename Put>
-__device__ __forceinline__ void join_waves(const AttnArgs &a, const Work &w, const float (&sums)[4][JOIN][LINE],
-                                           const float2 (&ml)[4][ROWS], int rows, Put put) {
+template <typename T, int JOIN, int LINE, int WAVES, int ROWS, typename Put>
+__device__ __forceinline__ void join_waves(const AttnArgs &a, const Work &w, const float (&sums)[WAVES][JOIN][LINE],
+                                           const float2 (&ml)[WAVES][ROWS], int rows, Put put) {
 #pragma unroll 1
     for (int r0 = 0; r0 < rows; r0 += JOIN) {
         if (r0 > 0) __syncthreads();
         put(r0);
         __syncthreads();
         const int line = a.c.dim / 4, n = min(JOIN, rows - r0) * line;
-        for (int x = threadIdx.x; x < n; x += 256) {
+        for (int x = threadIdx.x; x < n; x += 64 * WAVES) {
             const int r = fdiv(x, a.f_dim4), d = 4 * (x - r * line);
             const Row out = find_row(a, w, w.row0 + r0 + r);
             float m = -INFINITY, l = 0.f;
 #pragma unroll
-            for (int y = 0; y < 4; ++y) m = fmaxf(m, ml[y][r0 + r].x);
+            for (int y = 0; y < WAVES; ++y) m = fmaxf(m, ml[y][r0 + r].x);
             floatx4 sum = {};
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
+            for (int y = 0; y < WAVES; ++y) {
                 const float2 of = ml[y][r0 + r];
                 const float by = of.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(of.x - m);
                 l += of.y * by;
@@ -838,8 +848,8 @@ __device__ __forceinline__ float over_groups(float v, Fn fn) {
 template <typename T, int FMT, bool POW2, int DB>
 struct Few {
     // A weight times an fp32 scale takes two parts for bf16 too: a row of one key or of one that outweighs the others
-    // comes out as exact as its value, where a power of two loses nothing of a weight of 1.  It costs 5% (64 sequences
-    // of up to 8192 keys 131 -> 137 us).
+    // comes out as exact as its value, where a power of two loses nothing of a weight of 1.  It costs 5%: 64 sequences
+    // of up to 8192 keys took 131 us before and 137 after it.
     struct P : Parts<T> {
         static constexpr int PP = Parts<T>::PP == 1 && !POW2 ? 2 : Parts<T>::PP;
     };
@@ -1052,13 +1062,14 @@ struct Few {
     }
 };
 
-// As attn8_share, for up to 16 rows.
+// As attn8_share, for up to 16 rows, of four waves or eight.
 template <typename T, int FMT, bool POW2, int DB>
-__global__ __launch_bounds__(256, (attn8_groups(kAttnFew, sizeof(T) == 4, DB))) void attn8_few(AttnArgs a) {
-    constexpr int kJoin = DB == 8 ? 8 : 16, kLine = 32 * DB + 4;      // rows at a time, floats between them
-    __shared__ __attribute__((aligned(16))) float scales[4 * 64];
-    __shared__ __attribute__((aligned(16))) float sums[4][kJoin][kLine];
-    __shared__ float2 ml[4][16];
+__global__ __launch_bounds__(attn8_threads(kAttnFew, DB), (attn8_groups(kAttnFew, sizeof(T) == 4, DB) * attn8_threads(kAttnFew, DB) / 256)) void attn8_few(AttnArgs a) {
+    constexpr int kWaves = attn8_threads(kAttnFew, DB) / 64;
+    constexpr int kJoin = DB >= 4 ? 8 : 16, kLine = 32 * DB + 4;      // rows at a time, floats between them
+    __shared__ __attribute__((aligned(16))) float scales[kWaves * 64];
+    __shared__ __attribute__((aligned(16))) float sums[kWaves][kJoin][kLine];
+    __shared__ float2 ml[kWaves][16];
     Work w;
     if (!find_work<16>(a, w)) return;
     const int lane = threadIdx.x & 63;
@@ -1072,7 +1083,7 @@ __global__ __launch_bounds__(256, (attn8_groups(kAttnFew, sizeof(T) == 4, DB))) 
         return;
     }
     Few<T, FMT, POW2, DB> s(a, w, row);
-    const bool fine = s.template walk<4 * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
+    const bool fine = s.template walk<kWaves * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
                                                  w.low(a, w.token(a, w.row0 + 15)), scales + wave * 64);
     const AttnArgs al = late_args();
     if (__syncthreads_or(!fine)) {        // then the first wave takes all keys, in the other form's order

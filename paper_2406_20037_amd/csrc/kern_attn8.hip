@@ -73,7 +73,7 @@ __global__ __launch_bounds__(64 * kJoinWaves) void attn8_join(AttnArgs a) {
 // ---- host ---------------------------------------------------------------------------
 
 struct AttnPlan {
-    int form, splits, span;
+    int form, threads, splits, span;
     int64_t groups, bytes, part;          // part: bytes of the sums, a multiple of 16
 };
 
@@ -122,10 +122,12 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
     int64_t keys = most_keys(cache, chunk, cfg);
     if (cfg->window > 0) keys = std::min(keys, cfg->window + tile / group + 1 + 64);
     // The split that ends first: rounds of workgroups that the chip holds, each as long as its keys and what a
-    // workgroup needs beside them (64 equal sequences of 8192 keys: 261 us whole, 194 to 202 in two or four
-    // parts; of unequal lengths 127 whole and 136 to 149 so: full rounds of whole sequences stay whole).
+    // workgroup needs beside them (64 equal sequences of 8192 keys: 166 us whole, 176 to 188 in two to four
+    // parts; of unequal lengths 118 whole, 112 in three parts, 136 and 151 in two and four: full rounds of whole
+    // sequences stay whole).
     const bool shares = p.form == kAttnFew || p.form == kAttnShare;
-    const int64_t unit = shares ? 128 : 64, beside = 4 * unit;
+    p.threads = attn8_threads(p.form, db);
+    const int64_t unit = shares ? p.threads / 64 * 32 : 64, beside = 4 * unit;
     const int64_t slots = 256 * attn8_groups(p.form, q->type == DS_TYPE_F32, db);
     const int64_t work = std::max((rows + tile - 1) / tile, std::min(q->tokens, chunk->seqs)) * cache->heads;
     int64_t best = INT64_MAX;
@@ -157,7 +159,7 @@ int run(const AttnPlan &p, AttnArgs a, hipStream_t stream) {
         if (rc != DS_OK) return rc;
     }
     void *argv[] = {&a};
-    if (!hip_ok(hipLaunchKernel(k.func, dim3(unsigned(p.groups)), dim3(attn8_threads(p.form)), argv, k.lds, stream), "ds_attn8"))
+    if (!hip_ok(hipLaunchKernel(k.func, dim3(unsigned(p.groups)), dim3(p.threads), argv, k.lds, stream), "ds_attn8"))
         return DS_EHIP;
     if (p.splits > 1) {
         const int64_t rows = int64_t(a.n.tokens) * a.heads;
@@ -212,7 +214,7 @@ int ds_attn8(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, c
         set_error("%lld tokens of %lld heads a cache head", (long long)q->tokens, (long long)(q->heads / cache->heads));
         return DS_EUNSUPPORTED;
     }
-    if ((rc = launch_check(p.groups, attn8_threads(p.form), "ds_attn8")) != DS_OK ||
+    if ((rc = launch_check(p.groups, p.threads, "ds_attn8")) != DS_OK ||
         (rc = launch_check((q->tokens * q->heads + kJoinWaves - 1) / kJoinWaves, 256, "ds_attn8")) != DS_OK)
         return rc;
     AttnArgs a{};
