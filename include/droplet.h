@@ -768,8 +768,9 @@ typedef struct {
  * a key holds that a token does not see, NaN included, does not reach its row.
  * q, out: fp32, fp16 or bf16 (the same), tokens x q heads x cache dim.  Products of q and k are exact
  * and summed in fp32, softmax and sums are fp32; the weights p enter the second product in bf16, as one
- * part of 8 bits for bf16 (half the rounding of out, on average), as two for fp16 and three for fp32, whose
- * queries are split into three too.
+ * part of 8 bits for bf16 (half the rounding of out, on average; as two for few rows over fp32 scales), as two
+ * for fp16 and three for fp32, whose queries are split into three too.  Weights of up to 2^12 are summed before
+ * they are divided: sums of values past 2^115 may leave fp32's range where their average does not.
  * A few tokens over long sequences split the keys over workgroups and join the parts in order, so two
  * calls give the same bits, in `work` (16-byte aligned, work_bytes of it, as ds_attn8_work
  * says for the same arguments; 0 bytes need no pointer): the caller's, for this call until it is done.

@@ -120,7 +120,7 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
     const int tile = attn8_rows(p.form);
     const int64_t base = (rows / tile + chunk->seqs) * cache->heads;
     int64_t keys = most_keys(cache, chunk, cfg);
-    if (cfg->window > 0) keys = std::min(keys, cfg->window + tile / group + 1 + 64);
+    if (cfg->window > 0) keys = std::min(keys, std::min(cfg->window, kMaxPlaces) + tile / group + 1 + 64);
     // The split that ends first: rounds of workgroups that the chip holds, each as long as its keys and what a
     // workgroup needs beside them (64 equal sequences of 8192 keys: 166 us whole, 176 to 188 in two to four
     // parts; of unequal lengths 118 whole, 112 in three parts, 136 and 151 in two and four: full rounds of whole
