@@ -354,7 +354,7 @@ __device__ __forceinline__ void put_weight(bf16x8 (&to)[PP], int e, float w) {
     }
 }
 
-// The rows' sums once more, key by key in plain fp32, [key, until): for tiles whose values hold infinities or NaNs
+// The rows' sums once more, key by key in plain fp32, [key, until): for tiles whose values (or their scales) hold infinities or NaNs
 // where some row does not see all keys, as 0 times those is no 0.  Slow, small and met by broken numbers only.
 template <typename T, int FMT, int DB, typename Q>
 __device__ __forceinline__ void slow_sums(const AttnArgs &a, const Work &w, const Row &row, const Q &q, int h, int key,
@@ -594,7 +594,7 @@ struct Direct {
         __builtin_amdgcn_sched_barrier(0);
         bf16x8 pt[2][P::PP];
         if (edge) {
-            unsigned bad = 0;
+            unsigned bad = h && !(fabsf(sc) < INFINITY);   // (values' scales)
             int has[2] = {valid[0] - 4 * h, valid[1] - 4 * h};
             __asm__ volatile("" : "+v"(has[0]), "+v"(has[1]));
 #pragma unroll
@@ -984,7 +984,7 @@ struct Few {
         if (edge) {
             int low = row.low - key0 - 4 * g, lim = row.lim - key0 - 4 * g, has[2] = {t.valid[0] - 4 * g, t.valid[1] - 4 * g};
             __asm__ volatile("" : "+v"(low), "+v"(lim), "+v"(has[0]), "+v"(has[1]));
-            unsigned bad = 0;
+            unsigned bad = lane >= 32 && !(fabsf(sc) < INFINITY);    // (values' scales)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int k = 16 * (e >> 2) + (e & 3);
@@ -1257,9 +1257,12 @@ struct Tiles {
             }
             int note = st.valid;
             if (edge) {
-                unsigned bad = 0;
+                unsigned bad = !kFoldV && (lane & 15) < st.valid && (st.sc0 & 0x7f800000u) == 0x7f800000u;
 #pragma unroll
                 for (int e = 0; e < 8 * W; ++e) bad |= not_finite<FMT>(st.raw[e]);
+                if constexpr (kFoldV)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) bad |= __float_as_uint(by[e]) == 0x7f800000u;
                 note |= __any(bad != 0) ? 1 << 16 : 0;
             }
 #pragma unroll

@@ -81,6 +81,36 @@ def test_every_width(env, dim):  # noqa: F811
         p.check(*p.run())
 
 
+@pytest.mark.parametrize("kind", [q8.POW2, q8.F32])
+@pytest.mark.parametrize("form", FORMS)
+def test_scales_of_masked_places(env, form, kind):  # noqa: F811
+    """A scale that is no number, or infinite, of a key or a value reaches the rows that see it and no others."""
+    torch, L = env
+    new, group, dim, name = form
+    lens = [max(new, 90), max(new, 41)]
+    window = 24
+    for odd in (np.nan, np.inf)[:1 if kind == q8.POW2 else 2]:
+        for which in (0, 1):
+            p = Problem(torch, L, np.random.default_rng(6), [new, new], lens, group=group, dim=dim, name=name, kind=kind)
+            # the last key but one of the first sequence, and one before the second's last window
+            marks = [(0, lens[0] - 2), (1, lens[1] - window - 1)]
+            for b, j in marks:
+                p.scales[which][p.table[b, j // 16], :, j % 16] = odd
+            p.put()
+            out, lse = p.run(window=window)
+            rows, broken = set(), []
+            for b, j in marks:
+                for i in range(new):
+                    pos = lens[b] - new + i
+                    if pos - window < j <= pos:
+                        broken.append(b * new + i)
+                    else:
+                        rows |= {(b * new + i, h) for h in range(2 * group)}
+            p.check(out, lse, window=window, rows=rows)
+            if kind == q8.F32 and (which == 1 or np.isnan(odd)):
+                assert not torch.isfinite(out[broken]).any()
+
+
 def test_one_page_for_all(env):  # noqa: F811
     """The same page at several places of a table and in two sequences: each place is a key of its own."""
     torch, L = env
@@ -90,3 +120,14 @@ def test_one_page_for_all(env):  # noqa: F811
         p.table[1, :] = p.table[0, 1]
         p.lists[2].copy_(torch.from_numpy(p.table))
         p.check(*p.run())
+
+
+def test_windows_past_everything(env):  # noqa: F811
+    torch, L = env
+    for new, group in ((1, 4), (4, 6), (40, 2)):
+        p = Problem(torch, L, np.random.default_rng(9), [new, new], [700, 300], group=group)
+        want, lse = p.run()
+        for window in (2 ** 31 - 1, 2 ** 31, 2 ** 63 - 1):
+            got = p.run(window=window, max_len=2 ** 63 - 1)
+            p.check(*got)
+            assert torch.equal(got[0], want) and torch.equal(got[1], lse)
