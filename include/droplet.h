@@ -683,7 +683,8 @@ typedef struct {
 /* Keys and values of sequences in 8 bits, in pages of `page` tokens.  Page p holds the
  * rows of head h and offset i at k + p * stride + (h * page + i) * dim, dim bytes each
  * (v alike), and one scale a row at entry p * scale_stride + h * page + i of k_scale (v_scale).
- * A row's value d is its byte times its scale.  dim: a multiple of 16, up to 256; page: a
+ * A row's value d is its byte times its scale; a power of two's byte 255, which ds_cache8_write never
+ * writes, makes it no number.  dim: a multiple of 16, up to 256; page: a
  * multiple of 16, up to 65536; pages: up to 2^31 - 1; stride: a multiple of 16, at least
  * heads * page * dim, which is below 2^31; scale_stride: at least heads * page.
  * k and v 16-byte aligned; F32 scales 4-byte aligned. */

@@ -106,9 +106,6 @@ __device__ __forceinline__ bf16x2 decode2(unsigned w, float by) {
     else return __builtin_amdgcn_cvt_scalef32_pk_bf16_bf8(int(w), by, HIGH);
 }
 
-__device__ __forceinline__ float scale_of(unsigned stored, int stype) {
-    return stype == DS_SCALE_POW2 ? __uint_as_float(max(stored << 23, 0x400000u)) : __uint_as_float(stored);
-}
 __device__ __forceinline__ unsigned load_scale(const void *p, int stype, int64_t at) {
     return stype == DS_SCALE_POW2 ? static_cast<const uint8_t *>(p)[at] : static_cast<const unsigned *>(p)[at];
 }
@@ -1230,7 +1227,9 @@ struct Tiles {
                 if (a.c.dim < 32 * DB && 16 * piece >= a.c.dim)      // (a number that is none times Q's 0 is no 0)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) st.raw[4 * j + e] = 0;
-                const float by = scale_of(j == 0 ? st.sc0 : st.sc1, POW2 ? DS_SCALE_POW2 : DS_SCALE_F32);
+                const unsigned sc = j == 0 ? st.sc0 : st.sc1;
+                // (the conversion looks at the exponent alone)
+                const float by = kFoldK ? __uint_as_float(sc << 23) : scale_of(sc, POW2 ? DS_SCALE_POW2 : DS_SCALE_F32);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const Op k = decode_k<FMT, Op>(st.raw[4 * j + 2 * u], st.raw[4 * j + 2 * u + 1], kFoldK ? by : 1.f);
@@ -1241,7 +1240,7 @@ struct Tiles {
         } else {
             float by[8];
             if constexpr (kFoldV) {
-                // (the conversion looks at the exponent alone)
+                // (alike)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const unsigned sc = e < 4 ? st.sc0 : st.sc1;

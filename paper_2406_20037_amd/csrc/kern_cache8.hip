@@ -369,7 +369,7 @@ __global__ __launch_bounds__(256) void cache8_read(HeadsView<T> k, HeadsView<T> 
         for (int u = 0; u < kReadAhead; ++u) {
             if (r[u].page == kNoSeq) continue;
             float x[8];
-            const float by = a.c.stype == DS_SCALE_POW2 ? __uint_as_float(max(s[u] << 23, 0x400000u)) : __uint_as_float(s[u]);
+            const float by = scale_of(s[u], a.c.stype);
             decode8(q[u], a.c.fmt, by, x);
             const HeadsView<T> &dst = r[u].val ? v : k;
             store_n<T, 8>(dst.p + (t0 + r[u].t) * dst.ld + r[u].h * dst.hld + d, r[u].val ? a.vec_v : a.vec_k, x);

@@ -73,6 +73,13 @@ __device__ __forceinline__ BlockScale block_scale(unsigned amax, int fmt, int st
     return {1.f / s, __float_as_uint(s)};
 }
 
+// A stored scale of a cache's row.  The byte 255 stands for no number, and a conversion by 2^(255 - 127) makes none of
+// any byte.
+__device__ __forceinline__ float scale_of(unsigned stored, int stype) {
+    if (stype != DS_SCALE_POW2) return __uint_as_float(stored);
+    return __uint_as_float(stored == 255u ? 0x7fc00000u : max(stored << 23, 0x400000u));
+}
+
 __device__ __forceinline__ void store_scale(const Q8View &m, int64_t i, unsigned bits) {
     if (m.stype == DS_SCALE_POW2) static_cast<uint8_t *>(m.scale)[i] = uint8_t(bits);
     else static_cast<unsigned *>(m.scale)[i] = bits;
