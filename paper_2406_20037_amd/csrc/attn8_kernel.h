@@ -92,6 +92,12 @@ __device__ __forceinline__ float other_half(float v) {
     return __uint_as_float(threadIdx.x & 32 ? a[0] : a[1]);
 }
 
+// Whether a number in parts, times one of the format, can come to none where the whole does not: in three parts, which are 0
+// or of either sign, times an infinity, which only e5m2 has (of two parts see put_weight).  Sums that are no number are
+// then taken by slow_sums; a number that is none among the values leads there too.
+template <typename T, int FMT>
+constexpr bool kPartsApart = FMT == DS_Q8_E5M2 && Parts<T>::PP == 3;
+
 // Any byte of the word that stands for no finite number.
 template <int FMT>
 __device__ __forceinline__ unsigned not_finite(unsigned w) {
@@ -338,11 +344,28 @@ struct Sums {
     }
     // What weights are taken from.
     __device__ __forceinline__ float base() const { return m == -INFINITY ? 0.f : m; }
+    // Whether a sum of the wave's is no number.
+    __device__ __forceinline__ bool none() const {
+        bool is = l != l;
+#pragma unroll
+        for (int blk = 0; blk < DB; ++blk)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) is |= o[blk][r] != o[blk][r];
+        return __any(is);
+    }
 };
 
-// w in parts of bf16, element e of an operand.
-template <int PP>
+// w in parts of bf16, element e of an operand.  Two parts that may meet an infinity (of e5m2) are cut, not rounded, and the
+// last of w's 24 bits is set: so neither is 0 or of the other sign, and their sum is the infinity.  The cut doubles the
+// second part's rounding, to 2^-16 of w at most.
+template <int PP, int FMT>
 __device__ __forceinline__ void put_weight(bf16x8 (&to)[PP], int e, float w) {
+    if constexpr (PP == 2 && FMT == DS_Q8_E5M2) {
+        const unsigned all = __float_as_uint(w) | 1u;
+        to[0][e] = __builtin_bit_cast(__bf16, uint16_t(all >> 16));
+        to[1][e] = __bf16(__uint_as_float(all) - __uint_as_float(all & 0xffff0000u));
+        return;
+    }
 #pragma unroll
     for (int part = 0; part < PP; ++part) {
         const __bf16 top8 = __bf16(w);
@@ -352,7 +375,9 @@ __device__ __forceinline__ void put_weight(bf16x8 (&to)[PP], int e, float w) {
 }
 
 // The rows' sums once more, key by key in plain fp32, [key, until): for tiles whose values (or their scales) hold infinities or NaNs
-// where some row does not see all keys, as 0 times those is no 0.  Slow, small and met by broken numbers only.
+// where some row does not see all keys, as 0 times those is no 0, and for infinities that meet parts (kPartsApart).  Slow, small and
+// met by broken numbers only: 3 us a key and wave, so that one infinity among 8192 keys takes a prompt of fp16
+// queries from 824 us to 1035, for the rows at whose edge it is.
 template <typename T, int FMT, int DB, typename Q>
 __device__ __forceinline__ void slow_sums(const AttnArgs &a, const Work &w, const Row &row, const Q &q, int h, int key,
                                           int until, Sums<DB> &s) {
@@ -376,14 +401,17 @@ __device__ __forceinline__ void slow_sums(const AttnArgs &a, const Work &w, cons
             const int d = 32 * (c >> 1) + 16 * h + 8 * (c & 1);
             if (d >= a.c.dim) continue;
             const bf16x8 kd = decode_k<FMT, bf16x8>(int(bytes(k + d, 4)), int(bytes(k + d + 4, 4)));
+            float whole[8] = {};                           // (parts add up to the value without rounding)
 #pragma unroll
-            for (int p = 0; p < Parts<T>::QP; ++p) {
+            for (int p = Parts<T>::QP - 1; p >= 0; --p) {
                 intx4 held = __builtin_bit_cast(intx4, q.get(p, c));
                 __asm__ volatile("" : "+v"(held));         // (its fp32 values are no registers of the loop's)
                 const auto qd = __builtin_bit_cast(typename Parts<T>::Op, held);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x += float(kd[e]) * float(qd[e]);
+                for (int e = 0; e < 8; ++e) whole[e] += float(qd[e]);
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x += float(kd[e]) * whole[e];
         }
         x = (x + other_half(x)) * sk;
         if (key < row.low || key >= row.lim) continue;
@@ -638,7 +666,7 @@ struct Direct {
         for (int j = 0; j < 4; ++j) {
             const floatx4 sv = *reinterpret_cast<const floatx4 *>(lds + 32 + 8 * j + 4 * h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) put_weight<P::PP>(pt[j >> 1], 4 * (j & 1) + e, x[4 * j + e] * sv[e]);
+            for (int e = 0; e < 4; ++e) put_weight<P::PP, FMT>(pt[j >> 1], 4 * (j & 1) + e, x[4 * j + e] * sv[e]);
         }
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_sched_barrier(0);
@@ -780,9 +808,10 @@ __global__ __launch_bounds__(256, (attn8_groups(kAttnShare, sizeof(T) == 4, DB))
     __syncthreads();
     const SharedQ<T, DB> q{&qs[0][0][lane]};
     Sums<DB> s;
-    const bool fine = Direct<T, FMT, DB, SharedQ<T, DB>, share_tiles<T, DB>>(a, w, row, q, s)
+    bool fine = Direct<T, FMT, DB, SharedQ<T, DB>, share_tiles<T, DB>>(a, w, row, q, s)
                           .template walk<4 * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
                                                     w.low(a, w.token(a, w.row0 + 31)), scales + wave * 64);
+    if constexpr (kPartsApart<T, FMT>) fine = fine && !s.none();
     if (__syncthreads_or(!fine)) {        // then the first wave takes all keys
         s.clear();
         if (wave == 0) slow_sums<T, FMT, DB, SharedQ<T, DB>>(late_args(), w, row, q, h, from, until, s);
@@ -820,9 +849,10 @@ __global__ __launch_bounds__(256, (attn8_groups(kAttnOwn, sizeof(T) == 4, DB))) 
     w.keys(a, row0 + 31, from, until);
     Sums<DB> s;
     from = max(from, w.low(a, w.token(a, row0)) & ~(kKeys - 1));
-    const bool fine = Direct<T, FMT, DB, HeldQ<T, DB>, DB == 8 ? 1 : 2>(a, w, row, q, s)
+    bool fine = Direct<T, FMT, DB, HeldQ<T, DB>, DB == 8 ? 1 : 2>(a, w, row, q, s)
                           .template walk<kKeys>(from, until, w.lim(a, w.token(a, row0)), w.low(a, w.token(a, row0 + 31)),
                                                 scales + wave * 64);
+    if constexpr (kPartsApart<T, FMT>) fine = fine && !s.none();
     if (!fine) slow_sums<T, FMT, DB, HeldQ<T, DB>>(late_args(), w, row, q, h, from, until, s);
     s.l += other_half(s.l);
     finish<T, DB>(late_args(), w, row, s, h);
@@ -945,6 +975,15 @@ struct Few {
             for (int blk = 0; blk < NB; ++blk) o[blk] *= by;
         }
     }
+    // Whether a sum of the wave's is no number.
+    __device__ __forceinline__ bool none() const {
+        bool is = l != l;
+#pragma unroll
+        for (int blk = 0; blk < NB; ++blk)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) is |= o[blk][r] != o[blk][r];
+        return __any(is);
+    }
     __device__ __forceinline__ float largest(const float (&x)[8]) const {
         const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
         return over_groups(top, [](float y, float z) { return fmaxf(y, z); }) * (kFoldK ? c : 1.f);
@@ -1014,7 +1053,7 @@ struct Few {
             for (int e = 0; e < 8; ++e) {
                 const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[e], c, -off) : x[e] - off);
                 part += p;
-                put_weight<P::PP>(pt, e, p * sv[e >> 2][e & 3]);
+                put_weight<P::PP, FMT>(pt, e, p * sv[e >> 2][e & 3]);
             }
         };
         weigh();
@@ -1086,8 +1125,9 @@ __global__ __launch_bounds__(attn8_threads(kAttnFew, DB), (attn8_groups(kAttnFew
         return;
     }
     Few<T, FMT, POW2, DB> s(a, w, row);
-    const bool fine = s.template walk<kWaves * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
+    bool fine = s.template walk<kWaves * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
                                                  w.low(a, w.token(a, w.row0 + 15)), scales + wave * 64);
+    if constexpr (kPartsApart<T, FMT>) fine = fine && !s.none();
     const AttnArgs al = late_args();
     if (__syncthreads_or(!fine)) {        // then the first wave takes all keys, in the other form's order
         if (wave > 0) return;
@@ -1327,7 +1367,7 @@ struct Tiles {
                 if (r % 4 == 0) sv = *reinterpret_cast<const floatx4 *>(t.sv + 32 * sub + 2 * r + 4 * h);
             const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[r], c, -from) : x[r] - from);
             l[r & 1] += p;
-            put_weight<P::PP>(pt[r >> 3], r & 7, kFoldV ? p : p * sv[r & 3]);
+            put_weight<P::PP, FMT>(pt[r >> 3], r & 7, kFoldV ? p : p * sv[r & 3]);
         };
         // (in this order: a wave that waits for its own matrix instructions would leave the vector unit idle)
         constexpr int kEach = 16 / (2 * DB);
@@ -1510,6 +1550,7 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
             at = after;
         }
     }
+    if constexpr (kPartsApart<T, FMT>) fine = fine && !s.none();
     const AttnArgs al = late_args();
     if (!fine) {
         HeldQ<T, DB> held;
