@@ -769,8 +769,9 @@ typedef struct {
  * a key holds that a token does not see, NaN included, does not reach its row.
  * q, out: fp32, fp16 or bf16 (the same), tokens x q heads x cache dim.  Products of q and k are exact
  * and summed in fp32, softmax and sums are fp32; the weights p enter the second product in bf16, as one
- * part of 8 bits for bf16 (half the rounding of out, on average; as two for few rows over fp32 scales), as two
- * for fp16 and three for fp32, whose queries are split into three too.  Weights of up to 2^12 are summed before
+ * part of 8 bits for bf16 (off by up to 2^-8, as out is by its own rounding), as two for fp16 and for bf16 over
+ * fp32 scales (2^-16), and as three for fp32 (2^-24), whose queries are split into three too.  These go by the
+ * types alone, whatever else is in the call.  Weights of up to 2^12 are summed before
  * they are divided: sums of values past 2^115 may leave fp32's range where their average does not.
  * A few tokens over long sequences split the keys over workgroups and join the parts in order, so two
  * calls give the same bits, in `work` (16-byte aligned, work_bytes of it, as ds_attn8_work

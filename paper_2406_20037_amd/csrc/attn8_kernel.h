@@ -36,7 +36,7 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 constexpr int kKeys = 32;                 // keys of a matrix instruction's tile
 constexpr float kLn2 = 0.69314718055994530942f;
 
-// How the types compute: Q in QP parts of operand type, P in PP parts of bf16.
+// How the types compute: Q in QP parts of operand type, P in PP parts of bf16 or more (see attn8_kernel).
 template <typename T>
 struct Parts;
 template <>
@@ -524,7 +524,7 @@ __device__ __forceinline__ void load_v(const uint8_t *p, unsigned at, unsigned (
 }
 
 // TILES: of a lane's registers, one in use and the others on their way.
-template <typename T, int FMT, int DB, typename Q, int TILES>
+template <typename T, int FMT, int PP, int DB, typename Q, int TILES>
 struct Direct {
     using P = Parts<T>;
     using Op = typename P::Op;
@@ -617,7 +617,7 @@ struct Direct {
                 for (int p = P::QP - 1; p >= 0; --p) sum = mma(k, q.get(p, 2 * c + u), sum);
             }
         __builtin_amdgcn_sched_barrier(0);
-        bf16x8 pt[2][P::PP];
+        bf16x8 pt[2][PP];
         if (edge) {
             unsigned bad = h && !(fabsf(sc) < INFINITY);   // (values' scales)
             int has[2] = {valid[0] - 4 * h, valid[1] - 4 * h};
@@ -666,7 +666,7 @@ struct Direct {
         for (int j = 0; j < 4; ++j) {
             const floatx4 sv = *reinterpret_cast<const floatx4 *>(lds + 32 + 8 * j + 4 * h);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) put_weight<P::PP, FMT>(pt[j >> 1], 4 * (j & 1) + e, x[4 * j + e] * sv[e]);
+            for (int e = 0; e < 4; ++e) put_weight<PP, FMT>(pt[j >> 1], 4 * (j & 1) + e, x[4 * j + e] * sv[e]);
         }
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_sched_barrier(0);
@@ -676,7 +676,7 @@ struct Direct {
             for (int st = 0; st < 2; ++st) {
                 const bf16x8 v = decode_v(t, st, blk);
 #pragma unroll
-                for (int part = P::PP - 1; part >= 0; --part) s.o[blk] = mma(v, pt[st][part], s.o[blk]);
+                for (int part = PP - 1; part >= 0; --part) s.o[blk] = mma(v, pt[st][part], s.o[blk]);
             }
         }
         return true;
@@ -778,7 +778,7 @@ constexpr int share_tiles = DB == 8 ? 2 : 3;
 // Four waves share 32 rows and take tiles of keys in turn.  Their sums meet in LDS, some rows at a time, and
 // all threads join four values each.  Memory's latency bounds it: three tiles of a wave in registers, one in use, which
 // Q in LDS makes room for.  64 sequences of up to 8192 keys of 8 heads of 128, four tokens and 8 query heads each: 134 to 143 us, 3.8 TB/s.
-template <typename T, int FMT, int DB>
+template <typename T, int FMT, int PP, int DB>
 __global__ __launch_bounds__(256, (attn8_groups(kAttnShare, sizeof(T) == 4, DB))) void attn8_share(AttnArgs a) {
     constexpr int kJoin = DB == 8 ? 8 : 16, kLine = 32 * DB + 4;      // rows at a time, floats between them
     __shared__ __attribute__((aligned(16))) float scales[4 * 64];
@@ -808,7 +808,7 @@ __global__ __launch_bounds__(256, (attn8_groups(kAttnShare, sizeof(T) == 4, DB))
     __syncthreads();
     const SharedQ<T, DB> q{&qs[0][0][lane]};
     Sums<DB> s;
-    bool fine = Direct<T, FMT, DB, SharedQ<T, DB>, share_tiles<T, DB>>(a, w, row, q, s)
+    bool fine = Direct<T, FMT, PP, DB, SharedQ<T, DB>, share_tiles<T, DB>>(a, w, row, q, s)
                           .template walk<4 * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
                                                     w.low(a, w.token(a, w.row0 + 31)), scales + wave * 64);
     if constexpr (kPartsApart<T, FMT>) fine = fine && !s.none();
@@ -834,7 +834,7 @@ __global__ __launch_bounds__(256, (attn8_groups(kAttnShare, sizeof(T) == 4, DB))
 // three parts) leave one wave a SIMD unit, so that none would wait beside another at a tile's barrier.  The vector unit's
 // decoding bounds it, once a wave: four prompts of 2048 tokens of 32 heads over 8 of 256 take 845 us, 326 TFLOP/s;
 // one in fp32, of 128, 195 us, 177.
-template <typename T, int FMT, int DB>
+template <typename T, int FMT, int PP, int DB>
 __global__ __launch_bounds__(256, (attn8_groups(kAttnOwn, sizeof(T) == 4, DB))) void attn8_own(AttnArgs a) {
     __shared__ __attribute__((aligned(16))) float scales[4 * 64];
     Work w;
@@ -849,7 +849,7 @@ __global__ __launch_bounds__(256, (attn8_groups(kAttnOwn, sizeof(T) == 4, DB))) 
     w.keys(a, row0 + 31, from, until);
     Sums<DB> s;
     from = max(from, w.low(a, w.token(a, row0)) & ~(kKeys - 1));
-    bool fine = Direct<T, FMT, DB, HeldQ<T, DB>, DB == 8 ? 1 : 2>(a, w, row, q, s)
+    bool fine = Direct<T, FMT, PP, DB, HeldQ<T, DB>, DB == 8 ? 1 : 2>(a, w, row, q, s)
                           .template walk<kKeys>(from, until, w.lim(a, w.token(a, row0)), w.low(a, w.token(a, row0 + 31)),
                                                 scales + wave * 64);
     if constexpr (kPartsApart<T, FMT>) fine = fine && !s.none();
@@ -878,14 +878,9 @@ __device__ __forceinline__ float over_groups(float v, Fn fn) {
     return fn(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
-template <typename T, int FMT, bool POW2, int DB>
+template <typename T, int FMT, bool POW2, int PP, int DB>
 struct Few {
-    // A weight times an fp32 scale takes two parts for bf16 too: a row of one key or of one that outweighs the others
-    // comes out as exact as its value, where a power of two loses nothing of a weight of 1.  It costs 5%: 64 sequences
-    // of up to 8192 keys took 131 us before and 137 after it.
-    struct P : Parts<T> {
-        static constexpr int PP = Parts<T>::PP == 1 && !POW2 ? 2 : Parts<T>::PP;
-    };
+    using P = Parts<T>;
     using Op = typename P::Op;
     static constexpr bool kFoldK = POW2 && std::is_same_v<Op, bf16x8>;
     static constexpr int NB = 2 * DB;                              // blocks of 16 values, a lane's bytes of a key of V
@@ -1044,7 +1039,7 @@ struct Few {
         const floatx4 sv[2] = {*reinterpret_cast<const floatx4 *>(lds + 32 + 4 * g),
                                *reinterpret_cast<const floatx4 *>(lds + 48 + 4 * g)};
         __builtin_amdgcn_wave_barrier();
-        bf16x8 pt[P::PP];
+        bf16x8 pt[PP];
         float part = 0.f;
         const auto weigh = [&]() {
             const float off = m == -INFINITY ? 0.f : m;
@@ -1053,7 +1048,7 @@ struct Few {
             for (int e = 0; e < 8; ++e) {
                 const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[e], c, -off) : x[e] - off);
                 part += p;
-                put_weight<P::PP, FMT>(pt, e, p * sv[e >> 2][e & 3]);
+                put_weight<PP, FMT>(pt, e, p * sv[e >> 2][e & 3]);
             }
         };
         weigh();
@@ -1075,7 +1070,7 @@ struct Few {
                 v[2 * e + 1] = y[1];
             }
 #pragma unroll
-            for (int p = P::PP - 1; p >= 0; --p) o[blk] = mma16(v, pt[p], o[blk]);
+            for (int p = PP - 1; p >= 0; --p) o[blk] = mma16(v, pt[p], o[blk]);
         }
         return true;
     }
@@ -1105,7 +1100,7 @@ struct Few {
 };
 
 // As attn8_share, for up to 16 rows, of four waves or eight (figures above).
-template <typename T, int FMT, bool POW2, int DB>
+template <typename T, int FMT, bool POW2, int PP, int DB>
 __global__ __launch_bounds__(attn8_threads(kAttnFew, DB), (attn8_groups(kAttnFew, sizeof(T) == 4, DB) * attn8_threads(kAttnFew, DB) / 256)) void attn8_few(AttnArgs a) {
     constexpr int kWaves = attn8_threads(kAttnFew, DB) / 64;
     constexpr int kJoin = DB >= 4 ? 8 : 16, kLine = 32 * DB + 4;      // rows at a time, floats between them
@@ -1124,7 +1119,7 @@ __global__ __launch_bounds__(attn8_threads(kAttnFew, DB), (attn8_groups(kAttnFew
             a.ml[(int64_t(w.split) * a.n.tokens + row.tok) * a.heads + row.head] = make_float2(-INFINITY, 0.f);
         return;
     }
-    Few<T, FMT, POW2, DB> s(a, w, row);
+    Few<T, FMT, POW2, PP, DB> s(a, w, row);
     bool fine = s.template walk<kWaves * kKeys>(from + wave * kKeys, until, w.lim(a, w.token(a, w.row0)),
                                                  w.low(a, w.token(a, w.row0 + 15)), scales + wave * 64);
     if constexpr (kPartsApart<T, FMT>) fine = fine && !s.none();
@@ -1178,7 +1173,7 @@ struct TileLds {
 };
 
 // Powers of two go into the operands: into V's (bf16), and into K's if those are bf16 too.
-template <typename T, int FMT, bool POW2, int DB>
+template <typename T, int FMT, bool POW2, int PP, int DB>
 struct Tiles {
     using P = Parts<T>;
     using Op = typename P::Op;
@@ -1187,7 +1182,7 @@ struct Tiles {
     static constexpr int kPieces = 2 * DB;                         // 16-byte pieces of a row of K
     static constexpr int kLoads = DB / 2;                          // of a thread
     static_assert(kLoads <= 2, "a thread holds two scales");
-    static constexpr bool kEarly = P::PP == 1 && POW2;             // registers for V's operands before the weights are there
+    static constexpr bool kEarly = PP == 1 && POW2;             // registers for V's operands before the weights are there
 
     const AttnArgs &a;
     const Work &w;
@@ -1353,7 +1348,7 @@ struct Tiles {
     // that the running maximum is too far behind, and are taken again; without them it is not looked at.
     __device__ __forceinline__ void weights(const TileLds<DB> &t, int sub, const float (&x)[16], float c,
                                             const Op (&k)[2 * DB], const Op (&q)[P::QP][2 * DB], Sums<DB> &s,
-                                            bf16x8 (&pt)[2][P::PP], floatx16 &next, bf16x8 (&v)[DB][2]) const {
+                                            bf16x8 (&pt)[2][PP], floatx16 &next, bf16x8 (&v)[DB][2]) const {
         // V's operands for what follows: half of them in the registers that K's leave
         if constexpr (kEarly)
 #pragma unroll
@@ -1367,7 +1362,7 @@ struct Tiles {
                 if (r % 4 == 0) sv = *reinterpret_cast<const floatx4 *>(t.sv + 32 * sub + 2 * r + 4 * h);
             const float p = __builtin_amdgcn_exp2f(kFoldK ? __builtin_fmaf(x[r], c, -from) : x[r] - from);
             l[r & 1] += p;
-            put_weight<P::PP, FMT>(pt[r >> 3], r & 7, kFoldV ? p : p * sv[r & 3]);
+            put_weight<PP, FMT>(pt[r >> 3], r & 7, kFoldV ? p : p * sv[r & 3]);
         };
         // (in this order: a wave that waits for its own matrix instructions would leave the vector unit idle)
         constexpr int kEach = 16 / (2 * DB);
@@ -1397,7 +1392,7 @@ struct Tiles {
                 for (int st = 0; st < 2; ++st) v[blk][st] = read_v(t, sub, st, blk);
     }
     // Their product with V, and x: the next scores, times K's scales.
-    __device__ __forceinline__ void product(const bf16x8 (&v)[DB][2], const bf16x8 (&pt)[2][P::PP], Sums<DB> &s,
+    __device__ __forceinline__ void product(const bf16x8 (&v)[DB][2], const bf16x8 (&pt)[2][PP], Sums<DB> &s,
                                             const floatx16 &next, const TileLds<DB> &t, int sub, float (&x)[16]) const {
         floatx4 sk;
         constexpr int kEach = 16 / (2 * DB);
@@ -1405,7 +1400,7 @@ struct Tiles {
         for (int y = 0; y < 2 * DB; ++y) {
             const int st = y / DB, blk = y % DB;
 #pragma unroll
-            for (int part = P::PP - 1; part >= 0; --part) s.o[blk] = mma(v[blk][st], pt[st][part], s.o[blk]);
+            for (int part = PP - 1; part >= 0; --part) s.o[blk] = mma(v[blk][st], pt[st][part], s.o[blk]);
 #pragma unroll
             for (int r = kEach * y; r < kEach * (y + 1); ++r) {
                 if constexpr (!kFoldK)
@@ -1451,15 +1446,15 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // Eight waves of 32 rows each, which all walk over the workgroup's keys.  The matrix unit (40% of the time) and the vector
-// unit (as much) bound it: a prompt of 8192 tokens of 32 heads over 8 of 128 takes 585 to 602 us in bf16, 757 with fp32
-// scales (a product a weight and score more), 908 in fp16 (weights in two parts); of 64 values 462.  Three tiles in LDS: one is used, the next is written
+// unit (as much) bound it: a prompt of 8192 tokens of 32 heads over 8 of 128 takes 585 to 602 us in bf16, 895 with fp32
+// scales (weights in two parts, a product a weight and score more), 830 in fp16 (weights in two parts); of 64 values 453.  Three tiles in LDS: one is used, the next is written
 // (the one after is on its way from memory), and the third may still be read by a wave that is behind: one
 // barrier a tile.
-template <typename T, int FMT, bool POW2, int DB>
+template <typename T, int FMT, bool POW2, int PP, int DB>
 __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds_bytes[];
     TileLds<DB> *lds = reinterpret_cast<TileLds<DB> *>(lds_bytes);
-    using Tl = Tiles<T, FMT, POW2, DB>;
+    using Tl = Tiles<T, FMT, POW2, PP, DB>;
     Work w;
     if (!find_work<256>(a, w)) return;
     const int lane = threadIdx.x & 63, i = lane & 31, h = lane >> 5;
@@ -1503,7 +1498,7 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
             return !((note[0] | note[1] | note[2] | note[3]) >> 16);
         };
         typename Tl::Op k[2 * DB];
-        bf16x8 v[DB][2], pt[2][Parts<T>::PP];
+        bf16x8 v[DB][2], pt[2][PP];
         floatx16 next = {};
         float x[16];
         bool begun = false;                // all rows have a maximum
@@ -1566,22 +1561,30 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
 template <typename T>
 AttnKernel attn8_kernel(int form, int fmt, int stype, int dim) {
     AttnKernel k{nullptr, 0};
-    const auto of_dim = [&](auto f, auto db) {
-        constexpr int FMT = f.value, DB = db.value;
+    const auto of_parts = [&](auto f, auto pow2, auto parts, auto db) {
+        constexpr int FMT = f.value, PP = parts.value, DB = db.value;
+        constexpr bool POW2 = pow2.value;
         if (form == kAttnFew) {
-            k.func = stype == DS_SCALE_POW2 ? reinterpret_cast<const void *>(&attn8_few<T, FMT, true, DB>)
-                                            : reinterpret_cast<const void *>(&attn8_few<T, FMT, false, DB>);
+            k.func = reinterpret_cast<const void *>(&attn8_few<T, FMT, POW2, PP, DB>);
         } else if (form == kAttnShare) {
-            k.func = reinterpret_cast<const void *>(&attn8_share<T, FMT, DB>);
+            k.func = reinterpret_cast<const void *>(&attn8_share<T, FMT, PP, DB>);
         } else if (form == kAttnOwn) {
-            if constexpr (attn8_own_form<T>(DB)) k.func = reinterpret_cast<const void *>(&attn8_own<T, FMT, DB>);
+            if constexpr (attn8_own_form<T>(DB)) k.func = reinterpret_cast<const void *>(&attn8_own<T, FMT, PP, DB>);
         } else {
             if constexpr (!attn8_own_form<T>(DB)) {
-                k.func = stype == DS_SCALE_POW2 ? reinterpret_cast<const void *>(&attn8_tiles<T, FMT, true, DB>)
-                                                : reinterpret_cast<const void *>(&attn8_tiles<T, FMT, false, DB>);
+                k.func = reinterpret_cast<const void *>(&attn8_tiles<T, FMT, POW2, PP, DB>);
                 k.lds = 3 * int(sizeof(TileLds<DB>));
             }
         }
+    };
+    // A weight's parts go by the types alone, so that a token's rounding is the same beside any others.  Times an fp32 scale
+    // a weight takes two parts for bf16 too: a row of one key comes out as exact as its value, where a power of two
+    // loses nothing of a weight of 1.  That costs 64 sequences of up to 8192 keys 5% (one token each) and 10% (four), and a
+    // prompt of 8192 tokens 33% (675 us in one part, 895 in two), of heads of 256 13%.
+    const auto of_dim = [&](auto f, auto db) {
+        constexpr int kLess = Parts<T>::PP, kMore = kLess < 2 ? 2 : kLess;
+        if (stype == DS_SCALE_POW2) of_parts(f, std::true_type{}, std::integral_constant<int, kLess>{}, db);
+        else of_parts(f, std::false_type{}, std::integral_constant<int, kMore>{}, db);
     };
     const auto of_fmt = [&](auto f) {
         const int db = attn8_dim_blocks(dim);
