@@ -933,8 +933,8 @@ _pack_heads = struct.Struct("@Pqqqqqii").pack
 _pack_cfg = struct.Struct("@diiqq").pack
 
 
-def _heads(t):
-    """The C form of a tensor [tokens, heads, dim] whose rows' elements are side by side."""
+def _heads(t, more=0):
+    """The C form of a tensor [tokens, heads, dim] whose rows' elements are side by side; more: added to its type."""
     kind = _PLAIN.get(t.dtype)
     if kind is None:
         raise TypeError(f"fp32, fp16 or bf16, not {t.dtype}")
@@ -942,7 +942,7 @@ def _heads(t):
     ld, hld, one = t.stride()
     if one != 1 and dim > 1:
         raise ValueError(f"elements of a row are {one} apart, not side by side")
-    return _pack_heads(t.data_ptr(), tokens, heads, dim, ld, hld, kind, 0)
+    return _pack_heads(t.data_ptr(), tokens, heads, dim, ld, hld, kind + more, 0)
 
 
 def _list(t, dtype, n, what):
@@ -988,29 +988,30 @@ def ds_cache8_read(cache, chunk, k, v, stream=None):
     return _cache8_rows("ds_cache8_read", cache, chunk, k, v, stream)
 
 
-def ds_attn8_work(q, cache, chunk, *, scale=None, causal=True, window=0, max_len=0):
+def ds_attn8_work(q, cache, chunk, *, scale=None, causal=True, window=0, max_len=0, exact=False):
     """Bytes of the workspace of ds_attn8 with these arguments."""
     n = C.c_int64()
     cfg = _pack_cfg(q.shape[2] ** -0.5 if scale is None else scale, causal, 0, window, max_len)
-    check("ds_attn8_work", lib.ds_attn8_work(_heads(q), cache._p, chunk._p, cfg, C.byref(n)))
+    check("ds_attn8_work", lib.ds_attn8_work(_heads(q, DS_EXACT_SUMS if exact else 0), cache._p, chunk._p, cfg, C.byref(n)))
     return n.value
 
 
 def ds_attn8(q, cache, chunk, out, lse=None, *, scale=None, causal=True, window=0, max_len=0, work=None,
-             stream=None):
+             stream=None, exact=False):
     """Attention of q [tokens, heads, dim] over the keys and values of the tokens' sequences in the cache, in
     out; log of the sums in lse [tokens, heads] (fp32) unless that is None.  scale: dim ** -0.5 unless given.
     causal: keys up to the token's own position, the latest ``window`` of them if that is not 0.  max_len: no sequence
     is longer (0: what the table holds); a low one keeps the split of few tokens' work even.
-    work: a uint8 tensor of ds_attn8_work bytes, this call's until it is done; allocated if None."""
+    work: a uint8 tensor of ds_attn8_work bytes, this call's until it is done; allocated if None.
+    exact: weights in two parts for bf16 q over powers of two, as all other types have them."""
     dev = _q8_device(q.get_device(), cache._device, chunk._device, out.get_device(), lse if lse is None else lse.get_device(),
                      work if work is None else work.get_device())
     if dev != _torch.cuda.current_device():
         with _torch.cuda.device(dev):
             return ds_attn8(q, cache, chunk, out, lse, scale=scale, causal=causal, window=window, max_len=max_len,
-                            work=work, stream=stream)
+                            work=work, stream=stream, exact=exact)
     cfg = _pack_cfg(q.shape[2] ** -0.5 if scale is None else scale, causal, 0, window, max_len)
-    qh, oh = _heads(q), _heads(out)
+    qh, oh = _heads(q, DS_EXACT_SUMS if exact else 0), _heads(out)
     if lse is not None and (lse.dtype != _torch.float32 or tuple(lse.shape) != tuple(q.shape[:2]) or
                             not lse.is_contiguous()):
         raise ValueError(f"lse: {lse.dtype} of shape {tuple(lse.shape)}, not float32 of {tuple(q.shape[:2])}")

@@ -53,8 +53,8 @@ struct AttnKernel {
     const void *func;
     int lds;                              // bytes of dynamic LDS
 };
-// The kernel of a type (float, _Float16, __bf16).
+// The kernel of a type (float, _Float16, __bf16); exact: weights of 16 bits at least.
 template <typename T>
-AttnKernel attn8_kernel(int form, int fmt, int stype, int dim);
+AttnKernel attn8_kernel(int form, int fmt, int stype, int dim, bool exact);
 
 }  // namespace ds

@@ -1559,7 +1559,7 @@ __global__ __launch_bounds__(512, 2) void attn8_tiles(AttnArgs a) {
 }  // namespace
 
 template <typename T>
-AttnKernel attn8_kernel(int form, int fmt, int stype, int dim) {
+AttnKernel attn8_kernel(int form, int fmt, int stype, int dim, bool exact) {
     AttnKernel k{nullptr, 0};
     const auto of_parts = [&](auto f, auto pow2, auto parts, auto db) {
         constexpr int FMT = f.value, PP = parts.value, DB = db.value;
@@ -1577,14 +1577,16 @@ AttnKernel attn8_kernel(int form, int fmt, int stype, int dim) {
             }
         }
     };
-    // A weight's parts go by the types alone, so that a token's rounding is the same beside any others.  Times an fp32 scale
+    // A weight's parts go by the types (and the caller's choice) alone, so that a token's rounding is the same beside any others.  Times an fp32 scale
     // a weight takes two parts for bf16 too: a row of one key comes out as exact as its value, where a power of two
     // loses nothing of a weight of 1.  That costs 64 sequences of up to 8192 keys 5% (one token each) and 10% (four), and a
-    // prompt of 8192 tokens 33% (675 us in one part, 895 in two), of heads of 256 13%.
+    // prompt of 8192 tokens 33% (675 us in one part, 895 in two), of heads of 256 13%; over powers of two, where the caller
+    // may ask for it, 4%, 11%, 34% (593 and 795) and 10%.
     const auto of_dim = [&](auto f, auto db) {
         constexpr int kLess = Parts<T>::PP, kMore = kLess < 2 ? 2 : kLess;
-        if (stype == DS_SCALE_POW2) of_parts(f, std::true_type{}, std::integral_constant<int, kLess>{}, db);
-        else of_parts(f, std::false_type{}, std::integral_constant<int, kMore>{}, db);
+        if (stype != DS_SCALE_POW2) of_parts(f, std::false_type{}, std::integral_constant<int, kMore>{}, db);
+        else if (exact) of_parts(f, std::true_type{}, std::integral_constant<int, kMore>{}, db);
+        else of_parts(f, std::true_type{}, std::integral_constant<int, kLess>{}, db);
     };
     const auto of_fmt = [&](auto f) {
         const int db = attn8_dim_blocks(dim);

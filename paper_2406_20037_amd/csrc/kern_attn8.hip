@@ -78,6 +78,15 @@ struct AttnPlan {
     int64_t groups, bytes, part;          // part: bytes of the sums, a multiple of 16
 };
 
+// q without DS_EXACT_SUMS in its type (null where q is); exact: whether that was there.
+const ds_heads *plain_type(const ds_heads *q, ds_heads *of, bool *exact) {
+    if (!q) return nullptr;
+    *of = *q;
+    *exact = (q->type & DS_EXACT_SUMS) != 0;
+    of->type &= ~DS_EXACT_SUMS;
+    return of;
+}
+
 int attn_check(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg) {
     int rc;
     if ((rc = heads_check(q, "q", false)) != DS_OK || (rc = cache8_check(cache)) != DS_OK ||
@@ -153,8 +162,8 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
 }
 
 template <typename T>
-int run(const AttnPlan &p, AttnArgs a, hipStream_t stream) {
-    const AttnKernel k = attn8_kernel<T>(p.form, a.c.fmt, a.c.stype, a.c.dim);
+int run(const AttnPlan &p, AttnArgs a, bool exact, hipStream_t stream) {
+    const AttnKernel k = attn8_kernel<T>(p.form, a.c.fmt, a.c.stype, a.c.dim, exact);
     if (k.lds) {
         const int rc = ensure_lds_attr(k.func, k.lds);
         if (rc != DS_OK) return rc;
@@ -180,6 +189,9 @@ extern "C" {
 
 int ds_attn8_work(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg,
                   int64_t *bytes) {
+    ds_heads of;
+    bool exact;
+    q = plain_type(q, &of, &exact);
     const int rc = attn_check(q, cache, chunk, cfg);
     if (rc != DS_OK) return rc;
     if (!bytes) {
@@ -192,6 +204,9 @@ int ds_attn8_work(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chu
 
 int ds_attn8(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, const ds_attn8_cfg *cfg,
              const ds_heads *out, float *lse, void *work, int64_t work_bytes, hipStream_t stream) {
+    ds_heads of;
+    bool exact;
+    q = plain_type(q, &of, &exact);
     int rc = attn_check(q, cache, chunk, cfg);
     if (rc != DS_OK || (rc = heads_check(out, "out", true)) != DS_OK) return rc;
     if (out->tokens != q->tokens || out->heads != q->heads || out->dim != q->dim || out->type != q->type) {
@@ -244,9 +259,9 @@ int ds_attn8(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *chunk, c
     a.f_dim4 = make_fastdiv(cache->dim / 4);
     a.vec_q = heads16(q);
     a.vec_o = heads16(out);
-    if (q->type == DS_TYPE_F32) return run<float>(p, a, stream);
-    if (q->type == DS_TYPE_F16) return run<_Float16>(p, a, stream);
-    return run<__bf16>(p, a, stream);
+    if (q->type == DS_TYPE_F32) return run<float>(p, a, exact, stream);
+    if (q->type == DS_TYPE_F16) return run<_Float16>(p, a, exact, stream);
+    return run<__bf16>(p, a, exact, stream);
 }
 
 }  // extern "C"

@@ -43,3 +43,30 @@ def test_fp32_scales(env, form, monkeypatch):  # noqa: F811
     for factor in (lambda x: 1.0, lambda x: 1 + 600 * x, lambda x: 9.0 if 0.7 < x < 0.71 else 1.0):
         p = steep(env, form, q8.F32, factor)
         p.check(*p.run())
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_exact(env, form, monkeypatch):  # noqa: F811
+    """bf16 queries over powers of two take two parts if the caller asks; where there are as many anyway, nothing changes."""
+    torch, L = env
+    monkeypatch.setitem(test_gpu_attn8.WEIGHT, "bfloat16", TWO)
+    for factor in (lambda x: 1.0, lambda x: 1 + 600 * x, lambda x: 8.0 if 0.7 < x < 0.71 else 1.0):
+        p = steep(env, form, q8.POW2, factor)
+        p.check(*p.run(exact=True))
+    if form[3] != "bfloat16":
+        assert all(torch.equal(a, b) for a, b in zip(p.run(), p.run(exact=True)))
+    p = steep(env, form, q8.F32, lambda x: 1.0)
+    assert all(torch.equal(a, b) for a, b in zip(p.run(), p.run(exact=True)))
+
+
+def test_exact_split(env, monkeypatch):  # noqa: F811
+    torch, L = env
+    monkeypatch.setitem(test_gpu_attn8.WEIGHT, "bfloat16", TWO)
+    for new, heads, group in ((1, 4, 4), (70, 1, 4)):
+        p = Problem(torch, L, np.random.default_rng(5), [new], [9000], heads=heads, group=group, dim=128, page=64)
+        work = torch.empty(L.ds_attn8_work(p.q, p.cache, p.chunk, exact=True), dtype=torch.uint8, device="cuda")
+        assert work.numel() > 0
+        out, lse = p.run(exact=True, work=work)
+        p.check(out, lse, rows={(t, h) for t in (0, new - 1) for h in (0, heads * group - 1)})
+        again = p.run(exact=True)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
