@@ -46,6 +46,9 @@ class Attention8:
                  dtype=torch.float8_e4m3fn, scale=None, seed=0, device="cuda"):
         if window < 0 or most < 1:
             raise ValueError(f"window {window}, up to {most} tokens")
+        freqs = rotary_freqs(dim if turn is None else turn) if freqs is None else freqs
+        if 2 * freqs.numel() > dim:
+            raise ValueError(f"{2 * freqs.numel()} turned values of {dim}")
         self.width, self.heads, self.kv_heads, self.dim = width, heads, kv_heads, dim
         self.seqs, self.window, self.pairs, self.device = seqs, window, pairs, device
         self.page, self.cols = page, -(-most // page)
@@ -57,7 +60,7 @@ class Attention8:
         L.ds_q8_quantize(w, self.q)
         L.ds_q8_quantize(wo, self.qo)
         self.act_scale = scale
-        self.freqs = (rotary_freqs(dim if turn is None else turn) if freqs is None else freqs).to(device)
+        self.freqs = freqs.to(device)
         self.cache = L.Cache8(seqs * self.cols, kv_heads, dim, page, dtype, scale=scale, device=device)
         # pages are given out as sequences grow, the lowest free one first
         self.free = list(range(seqs * self.cols - 1, -1, -1))
@@ -71,22 +74,32 @@ class Attention8:
         self.held[seq], self.lengths[seq] = [], 0
 
     def _grow(self, new):
-        """Chunk and positions of so many new tokens of each sequence."""
+        """Chunk and positions of so many new tokens of each sequence, their lengths with them and the pages that each
+        takes more, which are theirs once _grown says that their rows are written."""
         if len(new) != self.seqs or min(new) < 0:
             raise ValueError(f"new tokens of {self.seqs} sequences, not {list(new)}")
         for seq, n in enumerate(new):
             if self.lengths[seq] + n > self.cols * self.page:
                 raise ValueError(f"sequence {seq} would have {self.lengths[seq] + n} tokens, of {self.cols * self.page}")
         pos, starts = [], [0]
-        for seq, n in enumerate(new):
-            first, self.lengths[seq] = self.lengths[seq], self.lengths[seq] + n
-            while len(self.held[seq]) * self.page < self.lengths[seq]:
-                self.table[seq, len(self.held[seq])] = self.free[-1]
-                self.held[seq].append(self.free.pop())
+        lengths, more, taken = [], [], 0
+        for seq, (first, n) in enumerate(zip(self.lengths, new)):
+            lengths.append(first + n)
+            more.append([])
+            for col in range(len(self.held[seq]), -(-lengths[seq] // self.page)):
+                taken += 1
+                more[seq].append(self.free[-taken])
+                self.table[seq, col] = self.free[-taken]         # (past what the sequence has, where nobody looks yet)
             pos.append(torch.arange(first, first + n, dtype=torch.int32))
             starts.append(starts[-1] + n)
-        lists = (torch.tensor(starts, dtype=torch.int32), torch.tensor(self.lengths, dtype=torch.int32), self.table)
-        return L.Chunk(*(t.to(self.device) for t in lists)), torch.cat(pos).to(self.device)
+        lists = (torch.tensor(starts, dtype=torch.int32), torch.tensor(lengths, dtype=torch.int32), self.table)
+        return L.Chunk(*(t.to(self.device) for t in lists)), torch.cat(pos).to(self.device), lengths, more
+
+    def _grown(self, lengths, more):
+        self.lengths = lengths
+        for held, pages in zip(self.held, more):
+            held += pages
+            del self.free[len(self.free) - len(pages):]
 
     def forward(self, x, new):
         """y [tokens, width] in bf16 of x [tokens, width], new[b] tokens of sequence b after another."""
@@ -103,15 +116,16 @@ class Attention8:
             return m
         qkv = room((heads + 2 * kv) * self.dim)
         L.ds_q8_matmul(eight(x), self.q, qkv)
-        chunk, pos = self._grow(new)
+        chunk, pos, lengths, more = self._grow(new)
         qkv = qkv.view(tokens, heads + 2 * kv, self.dim)
         q, k, v = qkv.split([heads, kv, kv], 1)
         L.ds_rotary(qkv[:, :heads + kv], pos, self.freqs, pairs=self.pairs)
         L.ds_cache8_write(self.cache, chunk, k, v)
         out = torch.empty(tokens, heads, self.dim, dtype=torch.bfloat16, device=self.device)
-        L.ds_attn8(q, self.cache, chunk, out, window=self.window, max_len=max(1, *self.lengths))
+        L.ds_attn8(q, self.cache, chunk, out, window=self.window, max_len=max(1, *lengths))
         y = room(self.width)
         L.ds_q8_matmul(eight(out.view(tokens, heads * self.dim)), self.qo, y)
+        self._grown(lengths, more)
         return y
 
 
