@@ -141,6 +141,9 @@ def main(argv=None):
     ap.add_argument("--tokens", type=int, default=32, help="tokens answered")
     ap.add_argument("--window", type=int, default=0)
     args = ap.parse_args(argv)
+    for name, least in dict(width=1, heads=1, kv_heads=1, dim=1, seqs=1, prompt=0, chunk=1, tokens=0, window=0).items():
+        if getattr(args, name) < least:
+            ap.error(f"--{name.replace('_', '-')} {getattr(args, name)}: {least} or more")
 
     def layer():
         return Attention8(args.width, args.heads, args.kv_heads, args.dim, seqs=args.seqs,
