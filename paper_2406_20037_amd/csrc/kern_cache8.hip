@@ -36,7 +36,8 @@ int heads_check(const ds_heads *t, const char *what, bool output) {
     if (output && t->tokens > 0) {
         const bool inside = t->heads == 1 || t->head_ld >= t->dim, apart = t->tokens == 1 || t->ld >= t->dim;
         const bool tokens_first = t->tokens == 1 || t->ld >= (t->heads - 1) * t->head_ld + t->dim;
-        const bool heads_first = t->heads == 1 || t->head_ld >= (t->tokens - 1) * t->ld + t->dim;
+        // (up to 2^71)
+        const bool heads_first = t->heads == 1 || t->head_ld >= __int128(t->tokens - 1) * t->ld + t->dim;
         if (!inside || !apart || !(tokens_first || heads_first)) {
             set_error("%s: rows %lld (tokens) and %lld (heads) elements apart overlap", what, (long long)t->ld,
                       (long long)t->head_ld);
