@@ -236,7 +236,7 @@ __device__ __forceinline__ bool find_work(const AttnArgs &a, Work &w) {
     // the last rows, which see most keys, first
     w.row0 = (a.causal ? all - 1 - mine : mine) * ROWS;
     w.len = min(max(length, 0), a.len);
-    w.shift = int64_t(length) - (s1 - w.s0);
+    w.shift = int64_t(length) - end + w.s0;  // (of all its tokens, also of those that the call does not have)
     return true;
 }
 
