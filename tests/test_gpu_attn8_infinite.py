@@ -10,9 +10,10 @@ from test_gpu_attn8_scores import FORMS
 pytestmark = pytest.mark.gpu
 
 
+@pytest.mark.parametrize("exact", [False, True])
 @pytest.mark.parametrize("kind", [q8.POW2, q8.F32])
 @pytest.mark.parametrize("form", FORMS)
-def test_values(env, form, kind):  # noqa: F811
+def test_values(env, form, kind, exact):  # noqa: F811
     """A column with an infinity is infinite, with two of either sign no number; the others are as without."""
     torch, L = env
     new, group, dim, name = form
@@ -25,7 +26,7 @@ def test_values(env, form, kind):  # noqa: F811
         page, off = attn8.place(p.table[0], j, 16, p.pages)
         p.codes[1][page, :, off, d] = code
     p.put()
-    out, lse = p.run()
+    out, lse = p.run(exact=exact)
     got, sums = out.double().cpu().numpy(), lse.double().cpu().numpy()
     (k, _), (v, _) = p.values(0, 0, length), p.values(1, 0, length)
     v = np.where(np.isfinite(v), v, 0.0)
