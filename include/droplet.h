@@ -766,7 +766,7 @@ typedef struct {
  * k_j and v_j of cache head h / (q heads / cache heads).  lse [tokens, q heads] (fp32, or null):
  * log sum_j exp(scale * q.k_j), with which parts over several caches are joined.  A row that sees no key (or
  * only places without a page) gives zeros and -infinity; rows of no sequence stay as they were. What
- * a key holds that a token does not see, NaN included, does not reach its row.
+ * a key holds that a token does not see, NaN included, does not reach its row.  q and out share no memory.
  * q, out: fp32, fp16 or bf16 (the same), tokens x q heads x cache dim.  Products of q and k are exact
  * and summed in fp32, softmax and sums are fp32; the weights p enter the second product in bf16, as one
  * part of 8 bits for bf16 (off by up to 2^-8, as out is by its own rounding), as two for fp16 and for bf16 over

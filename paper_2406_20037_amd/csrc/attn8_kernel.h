@@ -11,12 +11,12 @@
 // Few rows: memory bounds it.  Keys and values come from memory as they lie, without LDS and without a barrier: a lane's 16
 // bytes of a key's row are the first operand of two instructions (Q in the same order of values), and its 4 or 8 bytes
 // of eight keys' rows are those of four or eight, transposed by byte permutes, a value and its
-// neighbour key's in one conversion.  64 tokens of 64 query heads over 8192 keys of 8 heads of 128 each: 172 us, 6.3
-// TB/s; over up to 8192, 115 to 119 us, 4.6 TB/s; four tokens each, on 32 rows, 134.
+// neighbour key's in one conversion.  64 tokens of 64 query heads over 8192 keys of 8 heads of 128 each: 170 us, 6.4
+// TB/s; over up to 8192, 116 us, 4.7 TB/s; four tokens each, on 32 rows, 136.
 //
 // Many rows: the matrix and the vector unit bound it, and decoding is a third of the vector unit's work if each wave does it.
 // So eight waves share decoded tiles of 64 keys in LDS, K by rows and V by columns.  A prompt of 8192 tokens of 32
-// heads over 8 of 128: 585 to 602 us, 915 to 940 TFLOP/s.
+// heads over 8 of 128: 590 to 602 us, 914 to 932 TFLOP/s.
 #pragma once
 
 #include <cmath>
@@ -204,7 +204,7 @@ __device__ __forceinline__ bool find_work(const AttnArgs &a, Work &w) {
     const int lane = threadIdx.x & 63;
     // Workgroups go to the chip's eight parts in turn.  Heads side by side: the workgroups of a head share the caches
     // of as few parts as the number of heads allows.  Of few rows none share keys, and a part takes four heads of the
-    // same pages: that lets memory stream (64 sequences of 8192 keys each 242 -> 166 us, 6.5 TB/s; two heads
+    // same pages: that lets memory stream (64 sequences of 8192 keys each, four waves a workgroup: 242 -> 166 us, 6.5 TB/s; two heads
     // 244, eight 166, but 100 unequal sequences 145, where one to four take 135).
     int idx;
     const int whole = int(gridDim.x) / (8 * a.c.heads) * (8 * a.c.heads);
@@ -505,7 +505,7 @@ template <int DB>
 __device__ __forceinline__ int v_column(int i, int dim) {
     return min(DB * i, dim - DB);
 }
-// (once: rows that no other workgroup reads, past the caches; see Few::load)
+// (once: past the caches; see Few::load)
 template <int DB, bool ONCE>
 __device__ __forceinline__ void load_v(const uint8_t *p, unsigned at, unsigned (&w)[DB == 8 ? 2 : 1]) {
     const auto get = [&](const auto *from) {
@@ -777,7 +777,7 @@ constexpr int share_tiles = DB == 8 ? 2 : 3;
 
 // Four waves share 32 rows and take tiles of keys in turn.  Their sums meet in LDS, some rows at a time, and
 // all threads join four values each.  Memory's latency bounds it: three tiles of a wave in registers, one in use, which
-// Q in LDS makes room for.  64 sequences of up to 8192 keys of 8 heads of 128, four tokens and 8 query heads each: 134 to 143 us, 3.8 TB/s.
+// Q in LDS makes room for.  64 sequences of up to 8192 keys of 8 heads of 128, four tokens and 8 query heads each: 136 us, 4.0 TB/s.
 template <typename T, int FMT, int PP, int DB>
 __global__ __launch_bounds__(256, (attn8_groups(kAttnShare, sizeof(T) == 4, DB))) void attn8_share(AttnArgs a) {
     constexpr int kJoin = DB == 8 ? 8 : 16, kLine = 32 * DB + 4;      // rows at a time, floats between them
@@ -832,8 +832,8 @@ __global__ __launch_bounds__(256, (attn8_groups(kAttnShare, sizeof(T) == 4, DB))
 
 // Each wave has rows of its own and reads keys by itself: where its registers (sums of 256 values, or fp32 queries in
 // three parts) leave one wave a SIMD unit, so that none would wait beside another at a tile's barrier.  The vector unit's
-// decoding bounds it, once a wave: four prompts of 2048 tokens of 32 heads over 8 of 256 take 845 us, 326 TFLOP/s;
-// one in fp32, of 128, 195 us, 177.
+// decoding bounds it, once a wave: four prompts of 2048 tokens of 32 heads over 8 of 256 take 848 to 856 us, 325
+// TFLOP/s; one in fp32, of 128, 173 us, 199.
 template <typename T, int FMT, int PP, int DB>
 __global__ __launch_bounds__(256, (attn8_groups(kAttnOwn, sizeof(T) == 4, DB))) void attn8_own(AttnArgs a) {
     __shared__ __attribute__((aligned(16))) float scales[4 * 64];
@@ -941,8 +941,10 @@ struct Few {
 #pragma unroll
             for (int x = 0; x < DB / 2; ++x)
                 t.k[b][x] = *reinterpret_cast<const intx4 *>(k + koff + min(64 * x + 16 * g, dim - 16));
-            // V's whole lines are read once, and pass the caches by; the halves of K's that two loads share do not (64 sequences
-            // of up to 8192 keys 126.5 -> 120.3 us, K's too 137; of 8192 each 260 -> 241, 245)
+            // V's whole lines pass the caches by: where a sequence's rows are one tile, as the form is chosen for, no other
+            // workgroup reads them (a sequence of more rows than the average does, and reads them from memory again for each
+            // tile).  The halves of K's that two loads share do not (64 sequences of up to 8192 keys 126.5 -> 120.3 us, K's
+            // too 137; of 8192 each 260 -> 241, 245; four waves a workgroup)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint8_t *vp = v + e * dim + voff;
@@ -1446,8 +1448,8 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // Eight waves of 32 rows each, which all walk over the workgroup's keys.  The matrix unit (40% of the time) and the vector
-// unit (as much) bound it: a prompt of 8192 tokens of 32 heads over 8 of 128 takes 585 to 602 us in bf16, 895 with fp32
-// scales (weights in two parts, a product a weight and score more), 830 in fp16 (weights in two parts); of 64 values 453.  Three tiles in LDS: one is used, the next is written
+// unit (as much) bound it: a prompt of 8192 tokens of 32 heads over 8 of 128 takes 590 to 602 us in bf16, 888 to 895 with fp32
+// scales (weights in two parts, a product a weight and score more), 829 to 845 in fp16 (weights in two parts); of 64 values 453.  Three tiles in LDS: one is used, the next is written
 // (the one after is on its way from memory), and the third may still be read by a wave that is behind: one
 // barrier a tile.
 template <typename T, int FMT, bool POW2, int PP, int DB>

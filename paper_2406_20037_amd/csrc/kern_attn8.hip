@@ -13,7 +13,7 @@ constexpr float kLn2 = 0.69314718055994530942f;
 
 // A wave joins the parts of a row: LPR lanes take four values each of every 64 / LPR-th split, four at a
 // time (their loads together), and the groups of lanes are added up in order.  One token's 32 rows of 16 splits 4.0
-// us, latency; 1024 tokens of 32 heads of 128 in two splits 12.9 us, 44 MB.
+// us, latency; 1024 tokens of 32 heads of 128 in two splits 13.2 us, 44 MB.
 template <typename T, int LPR>
 __global__ __launch_bounds__(64 * kJoinWaves) void attn8_join(AttnArgs a) {
     const int lane = threadIdx.x & 63;
@@ -132,7 +132,7 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
     int64_t keys = most_keys(cache, chunk, cfg);
     if (cfg->window > 0) keys = std::min(keys, std::min(cfg->window, kMaxPlaces) + tile / group + 1 + 64);
     // The split that ends first: rounds of workgroups that the chip holds, each as long as its keys and what a
-    // workgroup needs beside them (64 equal sequences of 8192 keys: 166 us whole, 176 to 188 in two to four
+    // workgroup needs beside them (in workgroups of four waves, 64 equal sequences of 8192 keys: 166 us whole, 176 to 188 in two to four
     // parts; of unequal lengths 118 whole, 112 in three parts, 136 and 151 in two and four: full rounds of whole
     // sequences stay whole).
     const bool shares = p.form == kAttnFew || p.form == kAttnShare;

@@ -1,8 +1,8 @@
 // Rotary positions, and rows of keys and values to and from the paged 8-bit cache.  All three
 // move memory: each value is read once and written once by one launch.  What is written goes past the
 // caches (nontemporal): a kernel's outputs are read by a later one, on any of the eight dies, and the lines of a
-// cached store take room from loads.  8192 tokens of 40 heads of 128 bf16 values turned: 26.5 us (6.3 TB/s), where
-// cached stores took 35; a sequence of 32768 tokens read back 32.6 (6.2 TB/s), where they took 51.  Loads stay cached:
+// cached store take room from loads.  8192 tokens of 40 heads of 128 bf16 values turned: 25.9 us (6.5 TB/s), where
+// cached stores took 35; a sequence of 32768 tokens read back 31.6 (6.4 TB/s), where they took 51.  Loads stay cached:
 // past the caches they took 32 and 43.
 #include <cmath>
 #include <type_traits>
@@ -153,7 +153,7 @@ struct RotaryArgs {
 // 2^31, its whole part is dropped there, and fp32 holds the fraction.  Then the threads take items of 16 bytes of each
 // half of a head, or 16 bytes of pairs side by side (N pairs either way; single ones where rows are not whole groups of
 // 16 bytes), and copy what is not turned unless it is in place.  Memory bounds it: the figures are above; 4099 tokens of 24 heads of
-// 96 fp32 values, 64 of them turned by pairs, 14.2 us (5.3 TB/s; items of 64 bytes took 16); one token of 40 heads 2.4 us
+// 96 fp32 values, 64 of them turned by pairs, 13.7 us (5.5 TB/s; items of 64 bytes took 16); one token of 40 heads 2.1 us
 // on the chip, less than its launch.
 template <typename T, int N, bool PAIRS>
 __global__ __launch_bounds__(256) void rotary(HeadsView<const T> x, HeadsView<T> y, RotaryArgs a) {
@@ -266,7 +266,7 @@ constexpr int kReadAhead = 4, kWriteAhead = 2;   // rows of a thread whose loads
 // LPR lanes a row of up to 8 LPR values; rows of a workgroup token by token within a head, so that neighbouring
 // rows of a page are written together.  Memory bounds it, in part the reads that a workgroup does one after another (starts,
 // lengths and table, then its rows): prompts of up to 2731 tokens of 8 heads of 128 bf16 values (18549 in
-// all, 114 MB) in 24.8 us, 4.6 TB/s.  Rows loaded before their places are known took 26.7, four of a thread ahead 30.
+// all, 114 MB) in 23.4 to 25.3 us, 4.9 TB/s.  Rows loaded before their places are known took 26.7, four of a thread ahead 30.
 template <typename T, int LPR>
 __global__ __launch_bounds__(256) void cache8_write(HeadsView<const T> k, HeadsView<const T> v, CacheArgs a) {
     __shared__ int lds[kPlaceSeqs + 1];
@@ -338,7 +338,7 @@ __device__ __forceinline__ void decode8(intx2 q, int fmt, float s, float (&x)[8]
     }
 }
 
-// The same walk the other way: 32768 tokens of 8 heads of 128 to bf16 (202 MB) in 32.6 us, 6.2 TB/s; eight of a
+// The same walk the other way: 32768 tokens of 8 heads of 128 to bf16 (202 MB) in 31.6 us, 6.4 TB/s; eight of a
 // thread's rows ahead took 34.6, two 34.5.
 template <typename T, int LPR>
 __global__ __launch_bounds__(256) void cache8_read(HeadsView<T> k, HeadsView<T> v, CacheArgs a) {
