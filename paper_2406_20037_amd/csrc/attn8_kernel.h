@@ -204,8 +204,8 @@ __device__ __forceinline__ bool find_work(const AttnArgs &a, Work &w) {
     const int lane = threadIdx.x & 63;
     // Workgroups go to the chip's eight parts in turn.  Heads side by side: the workgroups of a head share the caches
     // of as few parts as the number of heads allows.  Of few rows none share keys, and a part takes four heads of the
-    // same pages: that lets memory stream (64 sequences of 8192 keys each, four waves a workgroup: 242 -> 166 us, 6.5 TB/s; two heads
-    // 244, eight 166, but 100 unequal sequences 145, where one to four take 135).
+    // same pages: that lets memory stream (four waves a workgroup, 64 sequences of 8192 keys each: 242 -> 166 us, 6.5
+    // TB/s; two heads 244, eight 166, but 100 unequal sequences 145, where one to four take 135).
     int idx;
     const int whole = int(gridDim.x) / (8 * a.c.heads) * (8 * a.c.heads);
     if (ROWS == 16 && a.c.heads % 4 == 0 && int(blockIdx.x) < whole) {
@@ -1184,7 +1184,7 @@ struct Tiles {
     static constexpr int kPieces = 2 * DB;                         // 16-byte pieces of a row of K
     static constexpr int kLoads = DB / 2;                          // of a thread
     static_assert(kLoads <= 2, "a thread holds two scales");
-    static constexpr bool kEarly = PP == 1 && POW2;             // registers for V's operands before the weights are there
+    static constexpr bool kEarly = PP == 1 && POW2;                // registers for V's operands before the weights are there
 
     const AttnArgs &a;
     const Work &w;
@@ -1449,7 +1449,8 @@ __device__ __forceinline__ void lds_barrier() {
 
 // Eight waves of 32 rows each, which all walk over the workgroup's keys.  The matrix unit (40% of the time) and the vector
 // unit (as much) bound it: a prompt of 8192 tokens of 32 heads over 8 of 128 takes 590 to 602 us in bf16, 888 to 895 with fp32
-// scales (weights in two parts, a product a weight and score more), 829 to 845 in fp16 (weights in two parts); of 64 values 453.  Three tiles in LDS: one is used, the next is written
+// scales (weights in two parts, a product a weight and score more), 829 to 845 in fp16 (weights in two parts); of 64
+// values 453.  Three tiles in LDS: one is used, the next is written
 // (the one after is on its way from memory), and the third may still be read by a wave that is behind: one
 // barrier a tile.
 template <typename T, int FMT, bool POW2, int PP, int DB>
@@ -1579,9 +1580,9 @@ AttnKernel attn8_kernel(int form, int fmt, int stype, int dim, bool exact) {
             }
         }
     };
-    // A weight's parts go by the types (and the caller's choice) alone, so that a token's rounding is the same beside any others.  Times an fp32 scale
-    // a weight takes two parts for bf16 too: a row of one key comes out as exact as its value, where a power of two
-    // loses nothing of a weight of 1.  That costs 64 sequences of up to 8192 keys 5% (one token each) and 10% (four), and a
+    // A weight's parts go by the types (and the caller's choice) alone, so that a token's rounding is the same beside any
+    // others.  Times an fp32 scale a weight takes two parts for bf16 too: a row of one key comes out as exact as its value,
+    // where a power of two loses nothing of a weight of 1.  That costs 64 sequences of up to 8192 keys 5% (one token each) and 10% (four), and a
     // prompt of 8192 tokens 33% (675 us in one part, 895 in two), of heads of 256 13%; over powers of two, where the caller
     // may ask for it, 4%, 11%, 34% (593 and 795) and 10%.
     const auto of_dim = [&](auto f, auto db) {

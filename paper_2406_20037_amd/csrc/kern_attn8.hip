@@ -132,9 +132,9 @@ AttnPlan attn_plan(const ds_heads *q, const ds_cache8 *cache, const ds_chunk *ch
     int64_t keys = most_keys(cache, chunk, cfg);
     if (cfg->window > 0) keys = std::min(keys, std::min(cfg->window, kMaxPlaces) + tile / group + 1 + 64);
     // The split that ends first: rounds of workgroups that the chip holds, each as long as its keys and what a
-    // workgroup needs beside them (in workgroups of four waves, 64 equal sequences of 8192 keys: 166 us whole, 176 to 188 in two to four
-    // parts; of unequal lengths 118 whole, 112 in three parts, 136 and 151 in two and four: full rounds of whole
-    // sequences stay whole).
+    // workgroup needs beside them (in workgroups of four waves, 64 equal sequences of 8192 keys: 166 us whole, 176 to
+    // 188 in two to four parts; of unequal lengths 118 whole, 112 in three parts, 136 and 151 in two and four: full
+    // rounds of whole sequences stay whole).
     const bool shares = p.form == kAttnFew || p.form == kAttnShare;
     p.threads = attn8_threads(p.form, db);
     const int64_t unit = shares ? p.threads / 64 * 32 : 64, beside = 4 * unit;
